@@ -303,6 +303,115 @@ structkv_status structkv_transition_scores(const double* entropy, const double* 
                                            int32_t n_layers, double w1, double w2, double w3, double* t_out,
                                            int32_t* pivot_layer_out);
 
+/* ---- a layer's cache in use: fresh tokens come, attend, are accepted, and tokens are evicted ------------------------
+ *
+ * Sequence b owns the slots cu_slots[b] .. cu_slots[b+1]-1 of the cache (its capacity; slots below are counted from its first
+ * one), of which the first lens[b] are in use.  The capacities are host values and size the launches; the lengths live on the
+ * device, so that a captured step can be replayed while they change.  Slots are in no particular order (an eviction fills holes),
+ * which attention does not mind: keys carry their positions' rotation, and `pos` says where a slot's token stood.
+ * `mass` is what eviction goes by: the attention weight that each token has gathered, the in-degree of Eq. 2 carried on with the
+ * decay of Eq. 3.  mass and pos come as one plane for all KV heads, or as one per KV head, whose slots then hold different tokens.
+ * The contents of slots that are not in use are never read and may hold anything (NaN among it); no call but structkv_cache_append
+ * writes them.
+ * Two arrays of lengths are needed: a call that changes them reads cache->lens and writes lens_out, which must be another array.
+ * A length outside [0, capacity] is taken as the nearer bound.
+ */
+typedef struct {
+  void* k;                 /* DEVICE: element (g, slot s of the cache, c) at k[g*stride_head + s*stride_slot + c], c contiguous */
+  void* v;                 /* DEVICE: likewise, the same strides */
+  int64_t stride_head;     /* >= head_dim (with one KV head: any) */
+  int64_t stride_slot;     /* >= head_dim */
+  int32_t n_kv_heads;      /* G >= 1 */
+  int32_t head_dim;        /* d: 1..256 */
+  int32_t dtype;           /* STRUCTKV_DTYPE_F32 or STRUCTKV_DTYPE_BF16: of k, v, queries and outputs */
+  int32_t planes;          /* of mass and pos: 1, or n_kv_heads */
+  float* mass;             /* DEVICE [planes][slots of the cache], or NULL */
+  int32_t* pos;            /* DEVICE [planes][slots of the cache], positions >= 0, or NULL */
+  const int32_t* lens;     /* DEVICE [batch] */
+  const int64_t* cu_slots; /* HOST [batch+1], cu_slots[0] = 0, non-decreasing, capacities below 2^31 */
+  int32_t batch;           /* 0 .. STRUCTKV_MAX_BATCH */
+} structkv_cache;
+
+/* Most fresh tokens of a sequence in structkv_cache_attend and structkv_cache_accept. */
+#define STRUCTKV_MAX_DRAFTS 64
+
+/*
+ * Bytes of scratch that structkv_cache_attend, for new_tokens fresh tokens in all (however they spread over the sequences), and
+ * structkv_cache_evict need on this cache.  0 on invalid arguments.  The workspace must be 256-byte aligned; it needs no
+ * initialisation, nothing in it outlives a call, and calls that may overlap in time need one each.
+ */
+size_t structkv_cache_workspace_bytes(const structkv_cache* cache, int32_t n_q_heads, int64_t new_tokens);
+
+/*
+ * Store rows in the free slots behind those in use, with r = cu_new[b] + t, t < T_b = cu_new[b+1] - cu_new[b]:
+ *   k[g][slot lens[b] + t] = k_new[g][r],  v likewise (bit-exact);   lens_out[b] = lens[b] + T_b
+ *   pos[p][same slot]  = pos_new[p*new_stride_plane + r]               (both NULL: positions are not kept)
+ *   mass[p][same slot] = mass_new ? mass_new[p*new_stride_plane + r] : 0   (skipped where the cache keeps no mass)
+ * For a prefill's compact cache (k_dst, v_dst, idx_out of structkv_layer_step) as for the tokens of a decoding step.
+ * A sequence whose rows do not fit its capacity is left as it was, lens_out[b] = lens[b].
+ * k_new, v_new: element (g, r, c) at g*new_stride_head + r*new_stride_tok + c.  cu_new: HOST [batch+1], cu_new[0] = 0,
+ * non-decreasing.  new_stride_plane: 0 where the planes share pos_new and mass_new.  The new rows must not overlap the cache.
+ */
+structkv_status structkv_cache_append(const structkv_cache* cache, const void* k_new, const void* v_new,
+                                      int64_t new_stride_head, int64_t new_stride_tok, const int64_t* cu_new,
+                                      const int32_t* pos_new, const float* mass_new, int64_t new_stride_plane,
+                                      int32_t* lens_out, void* stream);
+
+/*
+ * Attention of fresh tokens over the cache.  The T_b = cu_new[b+1] - cu_new[b] fresh tokens of sequence b (0 .. STRUCTKV_MAX_DRAFTS)
+ * have been appended: they are its last T_b slots in use, B_b = lens[b] - T_b the slots before them.  For row r = cu_new[b] + t,
+ * query head h, KV head g = h / (H_q/G):
+ *   y = scale * q[r][h] . k[g][s],  z = softcap > 0 ? softcap * tanh(y / softcap) : y
+ *   x_s = slopes ? z - slopes[h] * (pos[slot B_b + t] - pos[slot s]) : z
+ *   out[r][h] = sum_s a_s v[g][s],  a = softmax_s(x),  lse_out[r][h] = ln sum_s e^{x_s}
+ * over the slots s that row t sees: all s < B_b, and B_b + j where bit j of tree_mask[r] is set (a tree of drafts: a draft's
+ * ancestors and itself); tree_mask NULL: B_b + j for j <= t.  A row that sees nothing gets out 0 and lse_out -infinity.  Bits from
+ * T_b on are ignored.  What fresh slots hold, NaN among it, does not reach rows that do not see them.
+ * lambda in (0, 1] (only with T_b <= 1 everywhere): the weights are gathered,
+ *   mass[p][s] = lambda * mass[p][s] + sum of a_s over the plane's query heads, for the slots in use of sequences with T_b = 1.
+ * lambda = 0: mass stays as it is.  Drafts gather theirs when they are accepted (structkv_cache_accept).
+ * q: element (r, h, c) at r*q_stride_tok + h*q_stride_head + c; out [new][H_q][d] contiguous; lse_out [new][H_q] fp32.
+ * scale: >= 0, 0 selects 1/sqrt(head_dim).  slopes: DEVICE fp32 [H_q] or NULL, needs pos.  cu_new: HOST [batch+1].
+ * A sequence with lens[b] < T_b is one whose rows see nothing.
+ * Deterministic.  bf16 with head_dim 64 or 128, 16-byte aligned pointers and strides of whole 16 bytes goes through the bf16
+ * matrix kernels, the rest through fp32 ones.
+ */
+structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_heads, float scale, float softcap,
+                                      const float* slopes, const void* q, int64_t q_stride_tok, int64_t q_stride_head,
+                                      const int64_t* cu_new, const uint64_t* tree_mask, float lambda, void* out,
+                                      float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The verified part of the drafts stays.  path[cu_new[b] + i], i < A_b = n_accept[b], are the accepted fresh tokens t of
+ * sequence b (path NULL: i; n_accept NULL: all T_b):
+ *   mass[p][s] = lambda * mass[p][s] + sum over i and the plane's query heads of e^{x_s - lse[cu_new[b] + path[i]][h]},
+ *                s < lens[b], x and what a row sees as in structkv_cache_attend, which gave lse   (lambda = 0: left out)
+ *   slot B_b + i  <-  slot B_b + path[i]   for keys, values, mass and pos, as if all were read before any is written
+ *   lens_out[b] = B_b + A_b
+ * The other drafts' slots are no longer in use.  q, strides, cu_new, tree_mask, scale, softcap, slopes as in the attend call;
+ * with lambda = 0 q and lse may be NULL.  path, n_accept, lse: DEVICE.  A row whose lse is -infinity adds nothing; path entries
+ * outside [0, T_b) and n_accept outside [0, T_b] are taken as the nearer bound; a sequence with lens[b] < T_b is left as it was.
+ */
+structkv_status structkv_cache_accept(const structkv_cache* cache, int32_t n_q_heads, float scale, float softcap,
+                                      const float* slopes, const void* q, int64_t q_stride_tok, int64_t q_stride_head,
+                                      const float* lse, const int64_t* cu_new, const uint64_t* tree_mask,
+                                      const int32_t* path, const int32_t* n_accept, float lambda, int32_t* lens_out,
+                                      void* stream);
+
+/*
+ * Eviction: a sequence with lens[b] > budget[b] comes down to budget[b] slots, in every plane by itself.  Slots whose position is
+ * greater than the plane's largest in use minus keep_tail rank above all others (the recent ones; keep_tail = 0: none), the others
+ * by scores[p][s], larger first, ties to the lower slot; the budget[b] first ones stay (the order of the scores is that of
+ * structkv_select_topk).  In place: the kept slots below budget[b] stay where they are, and the j-th evicted slot below budget[b]
+ * takes keys, values, mass and pos of the j-th kept slot from budget[b] on, both counted in ascending order.
+ * lens_out[b] = min(lens[b], budget[b]).
+ * scores: DEVICE fp32 [planes][slots of the cache], or NULL for cache->mass.  budget: HOST [batch], >= 0.
+ * keep_tail > 0 needs pos.  The moved rows of one plane's heads move together (one plane: all KV heads).
+ */
+structkv_status structkv_cache_evict(const structkv_cache* cache, const float* scores, const int64_t* budget,
+                                     int32_t keep_tail, int32_t* lens_out, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
 #ifdef __cplusplus
 }
 #endif

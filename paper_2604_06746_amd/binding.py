@@ -23,6 +23,7 @@ STRUCTKV_DTYPE_F32 = 0
 STRUCTKV_DTYPE_BF16 = 1
 STRUCTKV_MAX_BATCH = 64
 STRUCTKV_STATIC_TOPK_MAX_TOKENS = 1048576
+STRUCTKV_MAX_DRAFTS = 64
 
 EXPORTS = (
     "structkv_last_error", "structkv_version", "structkv_workspace_bytes", "structkv_score_layer",
@@ -32,6 +33,8 @@ EXPORTS = (
     "structkv_layer_finish",
     "structkv_truncate_hidden", "structkv_block_scores",
     "structkv_pivot_workspace_bytes", "structkv_pivot_metrics", "structkv_score_layer_pivot", "structkv_transition_scores",
+    "structkv_cache_workspace_bytes", "structkv_cache_append", "structkv_cache_attend", "structkv_cache_accept",
+    "structkv_cache_evict",
     "structkv_debug_probs", "structkv_debug_score_steps",
 )
 
@@ -40,6 +43,14 @@ class structkv_shape(ctypes.Structure):
     _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("window", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class structkv_cache(ctypes.Structure):
+    """A layer's cache in use; make_cache fills it in from tensors (and keeps those alive)."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride_head", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("planes", ctypes.c_int32),
+                ("mass", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("cu_slots", ctypes.c_void_p),
+                ("batch", ctypes.c_int32)]
 
 
 class StructKVError(RuntimeError):
@@ -105,6 +116,17 @@ _lib.structkv_transition_scores.argtypes = [_vp, _vp, _vp, _i32, ctypes.c_double
                                             _vp, _vp]
 _lib.structkv_debug_probs.restype = _i32
 _lib.structkv_debug_probs.argtypes = [_sp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _sz, _vp, _i32]
+_cp = ctypes.POINTER(structkv_cache)
+_lib.structkv_cache_workspace_bytes.restype = _sz
+_lib.structkv_cache_workspace_bytes.argtypes = [_cp, _i32, _i64]
+_lib.structkv_cache_append.restype = _i32
+_lib.structkv_cache_append.argtypes = [_cp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _vp]
+_lib.structkv_cache_attend.restype = _i32
+_lib.structkv_cache_attend.argtypes = [_cp, _i32, _f32, _f32, _vp, _vp, _i64, _i64, _vp, _vp, _f32, _vp, _vp, _vp, _sz, _vp]
+_lib.structkv_cache_accept.restype = _i32
+_lib.structkv_cache_accept.argtypes = [_cp, _i32, _f32, _f32, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp]
+_lib.structkv_cache_evict.restype = _i32
+_lib.structkv_cache_evict.argtypes = [_cp, _vp, _vp, _i32, _vp, _vp, _sz, _vp]
 
 
 def make_shape(n_q_heads: int, n_kv_heads: int, head_dim: int, window: int, dtype: int,
@@ -363,3 +385,140 @@ def structkv_debug_probs(shape: structkv_shape, q_win: torch.Tensor, k: torch.Te
                                      _ptr(probs_out), _ptr(workspace),
                                      workspace.numel() * workspace.element_size(), _stream(stream),
                                      int(bool(force_simt))))
+
+
+# ---- a layer's cache in use ----------------------------------------------------------------------------------------------------
+
+def _require(ok: bool, message: str) -> None:
+    if not ok:
+        raise StructKVError(STRUCTKV_ERR_INVALID_ARG, message)
+
+
+def _vector(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, device, name: str) -> None:
+    if t is not None and (t.dtype != dtype or t.numel() != numel or t.device != device or not t.is_contiguous()):
+        raise StructKVError(STRUCTKV_ERR_INVALID_ARG, "%s must be a contiguous %s tensor of %d elements on %s" % (name, dtype, numel, device))
+
+
+def make_cache(k: torch.Tensor, v: torch.Tensor, cu_slots: Sequence[int], lens: torch.Tensor, mass: Optional[torch.Tensor] = None,
+               pos: Optional[torch.Tensor] = None) -> structkv_cache:
+    """k, v: [G, slots, d] views sharing strides, d contiguous; lens: int32 [batch]; mass fp32, pos int32: [planes, slots] (or [slots]),
+    planes = 1 or G.  The tensors are kept alive by the result; `lens` is read by the calls, whose lens_out is another tensor."""
+    _require(k.dim() == 3 and v.dim() == 3 and v.shape == k.shape and v.stride() == k.stride() and v.dtype == k.dtype,
+             "k and v must be [G, slots, d] views of one dtype that share shape and strides")
+    _require(k.dtype in (torch.float32, torch.bfloat16), "k and v must be float32 or bfloat16")
+    G, slots, d = k.shape
+    _require(G >= 1 and d >= 1 and (k.stride(2) == 1 or d == 1), "k and v need a KV head, and contiguous components")
+    batch = len(cu_slots) - 1
+    _require(batch >= 0 and cu_slots[batch] <= slots, "cu_slots needs batch + 1 entries, at most %d" % slots)
+    total = cu_slots[batch]
+    planes = 1
+    for t, name in ((mass, "mass"), (pos, "pos")):
+        if t is not None:
+            _require(t.dim() in (1, 2), "%s must be [planes, slots] or [slots]" % name)
+            planes = t.shape[0] if t.dim() == 2 else 1
+            _require(planes in (1, G), "%s must have one plane, or one per KV head" % name)
+    _vector(mass, torch.float32, planes * total, k.device, "mass")
+    _vector(pos, torch.int32, planes * total, k.device, "pos")
+    _vector(lens, torch.int32, batch, k.device, "lens")
+    _require(v.device == k.device and k.device.type == "cuda", "the cache must be on one GPU")
+    host = _host_i64(cu_slots)
+    code = STRUCTKV_DTYPE_BF16 if k.dtype == torch.bfloat16 else STRUCTKV_DTYPE_F32
+    c = structkv_cache(_ptr(k), _ptr(v), k.stride(0), k.stride(1), G, d, code, planes, _ptr(mass), _ptr(pos), _ptr(lens),
+                       ctypes.addressof(host), batch)
+    c.tensors = (k, v, lens, mass, pos, host)
+    c.tensor_dtype, c.device, c.slots = k.dtype, k.device, total
+    return c
+
+
+def _cache_call(fn, cache: structkv_cache, stream, *args) -> None:
+    """The call on the cache's GPU: on `stream`, or on the current one of that GPU."""
+    index = cache.device.index
+    _require(getattr(stream, "device", cache.device) == cache.device, "the stream belongs to another device than the cache")
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            _check(fn(ctypes.byref(cache), *args, _stream(stream)))
+    else:
+        _check(fn(ctypes.byref(cache), *args, _stream(stream)))
+
+
+def _query_strides(cache: structkv_cache, n_q_heads: int, q: torch.Tensor, new: int):
+    _require(q.dim() == 3 and q.shape[0] == new and q.shape[1] == n_q_heads and q.shape[2] == cache.head_dim and
+             q.dtype == cache.tensor_dtype and q.device == cache.device and (q.stride(2) == 1 or cache.head_dim == 1),
+             "q must be [new tokens, n_q_heads, head_dim], of the cache's dtype and device, with contiguous components")
+    return q.stride(0), q.stride(1)
+
+
+def _workspace(cache: structkv_cache, workspace: torch.Tensor) -> int:
+    _require(workspace.device == cache.device and workspace.is_contiguous(), "workspace must be contiguous and on the cache's device")
+    return workspace.numel() * workspace.element_size()
+
+
+def structkv_cache_workspace_bytes(cache: structkv_cache, n_q_heads: int, new_tokens: int) -> int:
+    return int(_lib.structkv_cache_workspace_bytes(ctypes.byref(cache), n_q_heads, new_tokens))
+
+
+def structkv_cache_append(cache: structkv_cache, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: Sequence[int],
+                          lens_out: torch.Tensor, pos_new: Optional[torch.Tensor] = None, mass_new: Optional[torch.Tensor] = None,
+                          stream=None) -> None:
+    """k_new, v_new: [G, new, d] views sharing strides; pos_new int32, mass_new fp32: [new] for all planes, or [planes, new]."""
+    _require(len(cu_new) == cache.batch + 1, "cu_new needs batch + 1 entries")
+    new = cu_new[cache.batch]
+    _require(k_new.dim() == 3 and k_new.shape[0] == cache.n_kv_heads and k_new.shape[1] >= new and k_new.shape[2] == cache.head_dim and
+             k_new.dtype == cache.tensor_dtype and k_new.device == cache.device and (k_new.stride(2) == 1 or cache.head_dim == 1) and
+             v_new.shape == k_new.shape and v_new.stride() == k_new.stride() and v_new.dtype == k_new.dtype and v_new.device == k_new.device,
+             "k_new and v_new must be [G, new tokens, head_dim] views sharing strides, of the cache's dtype and device")
+    plane = 0
+    for t, dtype, name in ((pos_new, torch.int32, "pos_new"), (mass_new, torch.float32, "mass_new")):
+        if t is not None:
+            _require(t.shape in ((new,), (cache.planes, new)), "%s must be [new tokens] or [planes, new tokens]" % name)
+            _vector(t, dtype, t.numel(), cache.device, name)
+            plane = new if t.dim() == 2 else 0
+    _require(pos_new is None or mass_new is None or pos_new.dim() == mass_new.dim(), "pos_new and mass_new must have the same shape")
+    _vector(lens_out, torch.int32, cache.batch, cache.device, "lens_out")
+    _cache_call(_lib.structkv_cache_append, cache, stream, _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _host_i64(cu_new),
+                _ptr(pos_new), _ptr(mass_new), plane, _ptr(lens_out))
+
+
+def structkv_cache_attend(cache: structkv_cache, n_q_heads: int, q: torch.Tensor, cu_new: Sequence[int], out: torch.Tensor,
+                          lse_out: torch.Tensor, workspace: torch.Tensor, tree_mask: Optional[torch.Tensor] = None, scale: float = 0.0,
+                          softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, lam: float = 0.0, stream=None) -> None:
+    """q: [new, H_q, d] view with d contiguous; out [new, H_q, d] and lse_out fp32 [new, H_q] contiguous; tree_mask: int64 [new], whose
+    64 bits are the fresh tokens that a token sees; slopes: fp32 [H_q]."""
+    _require(len(cu_new) == cache.batch + 1, "cu_new needs batch + 1 entries")
+    new = cu_new[cache.batch]
+    st, sh = _query_strides(cache, n_q_heads, q, new)
+    _vector(out, cache.tensor_dtype, new * n_q_heads * cache.head_dim, cache.device, "out")
+    _vector(lse_out, torch.float32, new * n_q_heads, cache.device, "lse_out")
+    _vector(tree_mask, torch.int64, new, cache.device, "tree_mask")
+    _vector(slopes, torch.float32, n_q_heads, cache.device, "slopes")
+    _cache_call(_lib.structkv_cache_attend, cache, stream, n_q_heads, scale, softcap, _ptr(slopes), _ptr(q), st, sh, _host_i64(cu_new),
+                _ptr(tree_mask), lam, _ptr(out), _ptr(lse_out), _ptr(workspace), _workspace(cache, workspace))
+
+
+def structkv_cache_accept(cache: structkv_cache, n_q_heads: int, q: Optional[torch.Tensor], lse: Optional[torch.Tensor],
+                          cu_new: Sequence[int], lens_out: torch.Tensor, path: Optional[torch.Tensor] = None,
+                          n_accept: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None, scale: float = 0.0,
+                          softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, lam: float = 0.0, stream=None) -> None:
+    """q, lse, tree_mask, scale, softcap, slopes as in the attend call (q and lse may be None with lam = 0); path: int32 [new], the accepted
+    tokens first in each sequence's part; n_accept: int32 [batch]."""
+    _require(len(cu_new) == cache.batch + 1, "cu_new needs batch + 1 entries")
+    new = cu_new[cache.batch]
+    st, sh = _query_strides(cache, n_q_heads, q, new) if q is not None else (0, 0)
+    _vector(lse, torch.float32, new * n_q_heads, cache.device, "lse")
+    _vector(tree_mask, torch.int64, new, cache.device, "tree_mask")
+    _vector(slopes, torch.float32, n_q_heads, cache.device, "slopes")
+    _vector(path, torch.int32, new, cache.device, "path")
+    _vector(n_accept, torch.int32, cache.batch, cache.device, "n_accept")
+    _vector(lens_out, torch.int32, cache.batch, cache.device, "lens_out")
+    _cache_call(_lib.structkv_cache_accept, cache, stream, n_q_heads, scale, softcap, _ptr(slopes), _ptr(q), st, sh, _ptr(lse),
+                _host_i64(cu_new), _ptr(tree_mask), _ptr(path), _ptr(n_accept), lam, _ptr(lens_out))
+
+
+def structkv_cache_evict(cache: structkv_cache, scores: Optional[torch.Tensor], budget: Sequence[int], keep_tail: int,
+                         lens_out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """scores: fp32 [planes, slots], or None for the cache's mass."""
+    _require(len(budget) == cache.batch, "budget needs batch entries")
+    _vector(scores, torch.float32, cache.planes * cache.slots, cache.device, "scores")
+    _vector(lens_out, torch.int32, cache.batch, cache.device, "lens_out")
+    _cache_call(_lib.structkv_cache_evict, cache, stream, _ptr(scores), _host_i64(budget), keep_tail, _ptr(lens_out), _ptr(workspace),
+                _workspace(cache, workspace))

@@ -1,0 +1,313 @@
+// C-ABI entry points of the operators on a cache in use: argument checks, the cut of an attend call, workspace, launches.
+// As in api.cpp no device memory is allocated and nothing synchronises.
+#include "cache.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+namespace skv {
+namespace {
+
+constexpr int kMaxHeads = 4096;
+
+structkv_status check_cache(const structkv_cache* c, CacheTable* t, CacheView* v) {
+  if (!c) return fail(STRUCTKV_ERR_INVALID_ARG, "cache is NULL");
+  if (c->n_kv_heads < 1 || c->head_dim < 1) return fail(STRUCTKV_ERR_INVALID_ARG, "n_kv_heads and head_dim must be >= 1");
+  if (c->n_kv_heads > kMaxHeads) return fail(STRUCTKV_ERR_UNSUPPORTED, "n_kv_heads %d > %d", c->n_kv_heads, kMaxHeads);
+  if (c->head_dim > 256) return fail(STRUCTKV_ERR_UNSUPPORTED, "head_dim %d > 256", c->head_dim);
+  if (c->dtype != STRUCTKV_DTYPE_F32 && c->dtype != STRUCTKV_DTYPE_BF16)
+    return fail(STRUCTKV_ERR_UNSUPPORTED, "dtype %d is neither f32 (0) nor bf16 (1)", c->dtype);
+  if (c->planes != 1 && c->planes != c->n_kv_heads)
+    return fail(STRUCTKV_ERR_INVALID_ARG, "planes must be 1 or n_kv_heads (%d), got %d", c->n_kv_heads, c->planes);
+  if (c->batch < 0) return fail(STRUCTKV_ERR_INVALID_ARG, "batch must be >= 0, got %d", c->batch);
+  if (c->batch > kMaxBatch) return fail(STRUCTKV_ERR_UNSUPPORTED, "batch %d exceeds STRUCTKV_MAX_BATCH (%d)", c->batch, kMaxBatch);
+  if (!c->cu_slots) return fail(STRUCTKV_ERR_INVALID_ARG, "cu_slots is NULL");
+  if (c->cu_slots[0] != 0) return fail(STRUCTKV_ERR_INVALID_ARG, "cu_slots[0] must be 0");
+  memset(t, 0, sizeof(*t));
+  t->batch = c->batch;
+  for (int b = 0; b < c->batch; ++b) {
+    if (c->cu_slots[b + 1] < c->cu_slots[b]) return fail(STRUCTKV_ERR_INVALID_ARG, "cu_slots decreases at %d", b);
+    if (c->cu_slots[b + 1] - c->cu_slots[b] >= ((int64_t)1 << 31) - 1024)
+      return fail(STRUCTKV_ERR_UNSUPPORTED, "sequence %d has a capacity of 2^31 slots or more", b);
+    t->cu[b + 1] = c->cu_slots[b + 1];
+  }
+  const int64_t slots = t->cu[c->batch];
+  if (slots > ((int64_t)1 << 40)) return fail(STRUCTKV_ERR_UNSUPPORTED, "more than 2^40 slots");
+  if (c->stride_slot < c->head_dim) return fail(STRUCTKV_ERR_INVALID_ARG, "stride_slot (%lld) < head_dim", (long long)c->stride_slot);
+  if (c->n_kv_heads > 1 && c->stride_head < c->head_dim)
+    return fail(STRUCTKV_ERR_INVALID_ARG, "stride_head (%lld) < head_dim", (long long)c->stride_head);
+  if (c->n_kv_heads > 1 && slots > 1 && c->stride_head < (slots - 1) * c->stride_slot + c->head_dim &&
+      c->stride_slot < (c->n_kv_heads - 1) * c->stride_head + c->head_dim)
+    return fail(STRUCTKV_ERR_INVALID_ARG, "rows of the cache overlap: neither the heads nor the slots lie apart");
+  if (c->batch > 0 && (!c->lens || ((uintptr_t)c->lens & 3))) return fail(STRUCTKV_ERR_INVALID_ARG, "lens is NULL or not 4-byte aligned");
+  if (slots > 0 && (!c->k || !c->v)) return fail(STRUCTKV_ERR_INVALID_ARG, "k or v is NULL");
+  const uintptr_t esz = c->dtype == STRUCTKV_DTYPE_BF16 ? 2 : 4;
+  if (((uintptr_t)c->k | (uintptr_t)c->v) & (esz - 1)) return fail(STRUCTKV_ERR_INVALID_ARG, "k or v is not aligned to its elements");
+  if (((uintptr_t)c->mass | (uintptr_t)c->pos) & 3) return fail(STRUCTKV_ERR_INVALID_ARG, "mass or pos is not 4-byte aligned");
+  *v = CacheView{c->k, c->v, c->n_kv_heads > 1 ? c->stride_head : 0, c->stride_slot, slots, c->mass, c->pos, c->lens,
+                 c->n_kv_heads, c->head_dim, c->planes};
+  return STRUCTKV_OK;
+}
+
+int elem_bytes(const structkv_cache* c) { return c->dtype == STRUCTKV_DTYPE_BF16 ? 2 : 4; }
+
+structkv_status check_new(const structkv_cache* c, const int64_t* cu_new, int64_t most, CacheTable* t) {
+  if (!cu_new) return fail(STRUCTKV_ERR_INVALID_ARG, "cu_new is NULL");
+  if (cu_new[0] != 0) return fail(STRUCTKV_ERR_INVALID_ARG, "cu_new[0] must be 0");
+  for (int b = 0; b < c->batch; ++b) {
+    const int64_t n = cu_new[b + 1] - cu_new[b];
+    if (n < 0) return fail(STRUCTKV_ERR_INVALID_ARG, "cu_new decreases at %d", b);
+    if (most && n > most)
+      return fail(STRUCTKV_ERR_UNSUPPORTED, "sequence %d: %lld fresh tokens, at most STRUCTKV_MAX_DRAFTS (%lld) are taken", b,
+                  (long long)n, (long long)most);
+    if (cu_new[b + 1] >= ((int64_t)1 << 31)) return fail(STRUCTKV_ERR_UNSUPPORTED, "2^31 new tokens or more");
+    t->cu_new[b + 1] = (int32_t)cu_new[b + 1];
+  }
+  return STRUCTKV_OK;
+}
+
+structkv_status check_lens_out(const structkv_cache* c, const int32_t* lens_out) {
+  if (!lens_out || ((uintptr_t)lens_out & 3)) return fail(STRUCTKV_ERR_INVALID_ARG, "lens_out is NULL or not 4-byte aligned");
+  const uintptr_t a = (uintptr_t)c->lens, b = (uintptr_t)lens_out, n = sizeof(int32_t) * (uintptr_t)c->batch;
+  if (a < b + n && b < a + n) return fail(STRUCTKV_ERR_INVALID_ARG, "lens_out must not be cache->lens: it is written while those are read");
+  return STRUCTKV_OK;
+}
+
+structkv_status check_heads(const structkv_cache* c, int32_t H) {
+  if (H < 1 || H % c->n_kv_heads)
+    return fail(STRUCTKV_ERR_INVALID_ARG, "n_kv_heads (%d) must divide n_q_heads (%d)", c->n_kv_heads, H);
+  if (H > kMaxHeads) return fail(STRUCTKV_ERR_UNSUPPORTED, "n_q_heads %d > %d", H, kMaxHeads);
+  return STRUCTKV_OK;
+}
+
+// what attend and accept share: heads, form of the scores, queries
+structkv_status check_scores(const structkv_cache* c, int32_t H, float scale, float softcap, const float* slopes, const void* q,
+                             int64_t qst, int64_t qsh, const uint64_t* tree, float lambda, ScoreForm* f) {
+  structkv_status st = check_heads(c, H);
+  if (st != STRUCTKV_OK) return st;
+  if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(STRUCTKV_ERR_INVALID_ARG, "scale must be finite and >= 0 (0 = 1/sqrt(head_dim))");
+  if (!(softcap >= 0.f) || !std::isfinite(softcap)) return fail(STRUCTKV_ERR_INVALID_ARG, "softcap must be finite and >= 0 (0 = none)");
+  if (!(lambda >= 0.f && lambda <= 1.f)) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda must be in [0,1]");
+  if (lambda > 0.f && !c->mass) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda > 0 needs the cache's mass");
+  if (slopes && !c->pos) return fail(STRUCTKV_ERR_INVALID_ARG, "slopes need the cache's pos");
+  if (((uintptr_t)slopes & 3) || ((uintptr_t)tree & 7)) return fail(STRUCTKV_ERR_INVALID_ARG, "slopes or tree_mask is misaligned");
+  if ((uintptr_t)q & (uintptr_t)(elem_bytes(c) - 1)) return fail(STRUCTKV_ERR_INVALID_ARG, "q is not aligned to its elements");
+  if (qst < 0 || qsh < 0) return fail(STRUCTKV_ERR_INVALID_ARG, "negative stride of q");
+  const float s = scale > 0.f ? scale : 1.0f / std::sqrt((float)c->head_dim);
+  *f = ScoreForm{s, (float)((double)s * 1.4426950408889634), softcap, softcap > 0.f ? 1.f / softcap : 0.f, slopes, tree};
+  return STRUCTKV_OK;
+}
+
+int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+// Chunks: as many workgroups as fill the chip once or twice, but at least kLeastChunk slots each.
+constexpr int64_t kAttendBlocks = 512, kLeastChunk = 128;
+
+structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mfma, CacheTable* t, AttendPlan* p) {
+  const int gs = H / c->n_kv_heads;
+  memset(p, 0, sizeof(*p));
+  p->mfma = mfma;
+  p->gather = gather;
+  p->rb = 1;
+  p->min_chunk = kAttendWaves * 16;
+  const int rows_wg = 16 * p->rb;
+  double work = 0;   // slots that the workgroups read in all
+  for (int b = 0; b < c->batch; ++b)
+    work += (double)ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, rows_wg) * c->n_kv_heads * (double)(t->cu[b + 1] - t->cu[b]);
+  const int64_t each = std::max<int64_t>(kLeastChunk, (int64_t)std::ceil(work / kAttendBlocks));
+  int64_t units = 0, part = 0;
+  p->join = gather;
+  for (int b = 0; b < c->batch; ++b) {
+    const int64_t fresh = t->cu_new[b + 1] - t->cu_new[b], cap = t->cu[b + 1] - t->cu[b];
+    const int64_t nc = std::max<int64_t>(1, ceil_div(cap, each));
+    units += nc * ceil_div(fresh * gs, rows_wg);
+    part += fresh * H * nc;
+    if (units * c->n_kv_heads >= ((int64_t)1 << 31) || part >= ((int64_t)1 << 31))
+      return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
+    t->units[b + 1] = (int32_t)units;
+    t->part[b + 1] = (int32_t)part;
+    if (fresh > 0 && nc > 1) p->join = 1;
+  }
+  p->blocks = units * c->n_kv_heads;
+  const size_t parts = p->join ? (size_t)part : 0;
+  size_t off = 0;
+  p->off_ml = off; off += align_up(parts * 2 * sizeof(float), 256);
+  p->off_o = off;  off += align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256);
+  p->off_x = off;  off += gather ? align_up((size_t)H * (size_t)t->cu[c->batch] * sizeof(float), 256) : 0;
+  p->total_bytes = off;
+  return STRUCTKV_OK;
+}
+
+// ... at most, however the tokens spread: a sequence's chunks are at most its share of kAttendBlocks / its row blocks and KV heads, and one
+// more; its rows per row block and KV head at most rows_wg
+size_t most_attend_bytes(const structkv_cache* c, int H, int64_t new_tokens, int64_t slots) {
+  const size_t rows_wg = 64;
+  const size_t parts = rows_wg * (size_t)kAttendBlocks + (size_t)new_tokens * H;
+  return align_up(parts * 2 * sizeof(float), 256) + align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256) +
+         (c->mass ? align_up((size_t)H * (size_t)slots * sizeof(float), 256) : 0);
+}
+
+struct EvictSpace {
+  size_t off_count, off_holes, off_moved, total_bytes;
+};
+EvictSpace evict_space(const structkv_cache* c, int64_t slots) {
+  EvictSpace e;
+  size_t off = 0;
+  e.off_count = off; off += align_up(sizeof(int32_t) * (size_t)c->planes * c->batch, 256);
+  e.off_holes = off; off += align_up(sizeof(int32_t) * (size_t)c->planes * (size_t)slots, 256);
+  e.off_moved = off; off += align_up(sizeof(int32_t) * (size_t)c->planes * (size_t)slots, 256);
+  e.total_bytes = off;
+  return e;
+}
+
+structkv_status check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (!ws || ((uintptr_t)ws & 255)) return fail(STRUCTKV_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
+  if (bytes < need) return fail(STRUCTKV_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", bytes, need);
+  return STRUCTKV_OK;
+}
+
+}  // namespace
+}  // namespace skv
+
+using namespace skv;
+
+extern "C" {
+
+size_t structkv_cache_workspace_bytes(const structkv_cache* cache, int32_t n_q_heads, int64_t new_tokens) {
+  CacheTable t;
+  CacheView v;
+  clear_error();
+  if (check_cache(cache, &t, &v) != STRUCTKV_OK || check_heads(cache, n_q_heads) != STRUCTKV_OK) return 0;
+  if (new_tokens < 0 || new_tokens > (int64_t)STRUCTKV_MAX_DRAFTS * kMaxBatch) {
+    fail(STRUCTKV_ERR_INVALID_ARG, "new_tokens (%lld) outside [0, STRUCTKV_MAX_DRAFTS x STRUCTKV_MAX_BATCH]", (long long)new_tokens);
+    return 0;
+  }
+  return std::max<size_t>(256, std::max(most_attend_bytes(cache, n_q_heads, new_tokens, v.slots), evict_space(cache, v.slots).total_bytes));
+}
+
+structkv_status structkv_cache_append(const structkv_cache* cache, const void* k_new, const void* v_new,
+                                      int64_t new_stride_head, int64_t new_stride_tok, const int64_t* cu_new,
+                                      const int32_t* pos_new, const float* mass_new, int64_t new_stride_plane,
+                                      int32_t* lens_out, void* stream) {
+  clear_error();
+  CacheTable t;
+  CacheView v;
+  structkv_status st = check_cache(cache, &t, &v);
+  if (st == STRUCTKV_OK) st = check_new(cache, cu_new, 0, &t);
+  if (st != STRUCTKV_OK || cache->batch == 0) return st;
+  st = check_lens_out(cache, lens_out);
+  if (st != STRUCTKV_OK) return st;
+  const int64_t total = t.cu_new[cache->batch];
+  const int e = elem_bytes(cache);
+  if (total > 0) {
+    if (!k_new || !v_new) return fail(STRUCTKV_ERR_INVALID_ARG, "k_new or v_new is NULL");
+    if (((uintptr_t)k_new | (uintptr_t)v_new) & (uintptr_t)(e - 1))
+      return fail(STRUCTKV_ERR_INVALID_ARG, "k_new or v_new is not aligned to its elements");
+    if (new_stride_head < 0 || new_stride_tok < 0 || new_stride_plane < 0) return fail(STRUCTKV_ERR_INVALID_ARG, "negative stride");
+    if ((pos_new == nullptr) != (cache->pos == nullptr))
+      return fail(STRUCTKV_ERR_INVALID_ARG, "pos_new must be given where the cache keeps positions, and only there");
+    if (mass_new && !cache->mass) return fail(STRUCTKV_ERR_INVALID_ARG, "mass_new given, but the cache keeps no mass");
+    if (((uintptr_t)pos_new | (uintptr_t)mass_new) & 3) return fail(STRUCTKV_ERR_INVALID_ARG, "pos_new or mass_new is not 4-byte aligned");
+    if (total * cache->head_dim * (int64_t)e / 2 >= ((int64_t)1 << 31) - 4096 || total * cache->planes >= ((int64_t)1 << 31))
+      return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows for one launch (rows*head_dim*element bytes/2 must stay below 2^31)");
+  }
+  SKV_HIP_CHECK(launch_cache_append(t, v, k_new, v_new, new_stride_head, new_stride_tok, pos_new, mass_new, new_stride_plane, e,
+                                    lens_out, (hipStream_t)stream));
+  return STRUCTKV_OK;
+}
+
+structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_heads, float scale, float softcap,
+                                      const float* slopes, const void* q, int64_t q_stride_tok, int64_t q_stride_head,
+                                      const int64_t* cu_new, const uint64_t* tree_mask, float lambda, void* out,
+                                      float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  CacheTable t;
+  CacheView v;
+  ScoreForm f;
+  structkv_status st = check_cache(cache, &t, &v);
+  if (st == STRUCTKV_OK) st = check_new(cache, cu_new, STRUCTKV_MAX_DRAFTS, &t);
+  if (st == STRUCTKV_OK) st = check_scores(cache, n_q_heads, scale, softcap, slopes, q, q_stride_tok, q_stride_head, tree_mask, lambda, &f);
+  if (st != STRUCTKV_OK || cache->batch == 0 || t.cu_new[cache->batch] == 0) return st;
+  if (!q || !out || !lse_out) return fail(STRUCTKV_ERR_INVALID_ARG, "q, out or lse_out is NULL");
+  if (((uintptr_t)out & (uintptr_t)(elem_bytes(cache) - 1)) || ((uintptr_t)lse_out & 3))
+    return fail(STRUCTKV_ERR_INVALID_ARG, "out or lse_out is not aligned to its elements");
+  if (lambda > 0.f)
+    for (int b = 0; b < cache->batch; ++b)
+      if (t.cu_new[b + 1] - t.cu_new[b] > 1)
+        return fail(STRUCTKV_ERR_INVALID_ARG, "sequence %d: lambda > 0 is for single tokens; drafts gather their weights in structkv_cache_accept", b);
+  AttendPlan p;
+  const bool bf16 = cache->dtype == STRUCTKV_DTYPE_BF16;
+  st = plan_attend(cache, n_q_heads, lambda > 0.f, false, &t, &p);
+  if (st == STRUCTKV_OK) st = check_workspace(workspace, workspace_bytes, p.total_bytes);
+  if (st != STRUCTKV_OK) return st;
+  uint8_t* w8 = (uint8_t*)workspace;
+  const AttendWork w = {q, q_stride_tok, q_stride_head, out, lse_out, (float*)(w8 + p.off_ml), (float*)(w8 + p.off_o),
+                        p.gather ? (float*)(w8 + p.off_x) : nullptr, n_q_heads, n_q_heads / cache->n_kv_heads, p.min_chunk, lambda,
+                        (int64_t)t.cu_new[cache->batch] * n_q_heads};
+  SKV_HIP_CHECK(launch_cache_attend_f32(t, v, f, p, w, bf16, (hipStream_t)stream));
+  if (p.join) SKV_HIP_CHECK(launch_cache_combine(t, v, p, w, bf16, (hipStream_t)stream));
+  return STRUCTKV_OK;
+}
+
+structkv_status structkv_cache_accept(const structkv_cache* cache, int32_t n_q_heads, float scale, float softcap,
+                                      const float* slopes, const void* q, int64_t q_stride_tok, int64_t q_stride_head,
+                                      const float* lse, const int64_t* cu_new, const uint64_t* tree_mask,
+                                      const int32_t* path, const int32_t* n_accept, float lambda, int32_t* lens_out,
+                                      void* stream) {
+  clear_error();
+  CacheTable t;
+  CacheView v;
+  ScoreForm f;
+  structkv_status st = check_cache(cache, &t, &v);
+  if (st == STRUCTKV_OK) st = check_new(cache, cu_new, STRUCTKV_MAX_DRAFTS, &t);
+  if (st == STRUCTKV_OK) st = check_scores(cache, n_q_heads, scale, softcap, slopes, q, q_stride_tok, q_stride_head, tree_mask, lambda, &f);
+  if (st != STRUCTKV_OK || cache->batch == 0) return st;
+  st = check_lens_out(cache, lens_out);
+  if (st != STRUCTKV_OK) return st;
+  if (((uintptr_t)lse | (uintptr_t)path | (uintptr_t)n_accept) & 3) return fail(STRUCTKV_ERR_INVALID_ARG, "lse, path or n_accept is not 4-byte aligned");
+  const bool weigh = lambda > 0.f && t.cu_new[cache->batch] > 0;
+  if (weigh && (!q || !lse)) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda > 0 needs q and lse");
+  if (weigh) {
+    const AttendWork w = {q, q_stride_tok, q_stride_head, nullptr, const_cast<float*>(lse), nullptr, nullptr, nullptr, n_q_heads,
+                          n_q_heads / cache->n_kv_heads, 0, lambda, 0};
+    SKV_HIP_CHECK(launch_cache_weights(t, v, f, w, path, n_accept, STRUCTKV_MAX_DRAFTS, cache->dtype == STRUCTKV_DTYPE_BF16, (hipStream_t)stream));
+  }
+  SKV_HIP_CHECK(launch_cache_accept(t, v, path, n_accept, elem_bytes(cache), lens_out, (hipStream_t)stream));
+  return STRUCTKV_OK;
+}
+
+structkv_status structkv_cache_evict(const structkv_cache* cache, const float* scores, const int64_t* budget,
+                                     int32_t keep_tail, int32_t* lens_out, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  clear_error();
+  CacheTable t;
+  CacheView v;
+  structkv_status st = check_cache(cache, &t, &v);
+  if (st != STRUCTKV_OK || cache->batch == 0) return st;
+  st = check_lens_out(cache, lens_out);
+  if (st != STRUCTKV_OK) return st;
+  if (!budget) return fail(STRUCTKV_ERR_INVALID_ARG, "budget is NULL");
+  if (keep_tail < 0) return fail(STRUCTKV_ERR_INVALID_ARG, "keep_tail < 0");
+  if (keep_tail > 0 && !cache->pos) return fail(STRUCTKV_ERR_INVALID_ARG, "keep_tail > 0 needs the cache's pos");
+  if (!scores) scores = cache->mass;
+  if (v.slots > 0 && (!scores || ((uintptr_t)scores & 3)))
+    return fail(STRUCTKV_ERR_INVALID_ARG, "scores is NULL (and the cache keeps no mass) or not 4-byte aligned");
+  const int64_t units = (int64_t)cache->head_dim * elem_bytes(cache) / 2;
+  for (int b = 0; b < cache->batch; ++b) {
+    if (budget[b] < 0) return fail(STRUCTKV_ERR_INVALID_ARG, "budget[%d] < 0", b);
+    const int64_t cap = t.cu[b + 1] - t.cu[b];
+    t.units[b] = (int32_t)std::min(budget[b], cap);
+    if (std::min(cap - t.units[b], (int64_t)t.units[b]) * units >= ((int64_t)1 << 31) - 4096)
+      return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows may move for one launch (rows*head_dim*element bytes/2 must stay below 2^31)");
+  }
+  const EvictSpace e = evict_space(cache, v.slots);
+  st = check_workspace(workspace, workspace_bytes, e.total_bytes);
+  if (st != STRUCTKV_OK) return st;
+  uint8_t* w8 = (uint8_t*)workspace;
+  const EvictWork w = {scores, keep_tail, lens_out, (int32_t*)(w8 + e.off_count), (int32_t*)(w8 + e.off_holes), (int32_t*)(w8 + e.off_moved)};
+  SKV_HIP_CHECK(launch_cache_evict(t, v, w, elem_bytes(cache), (hipStream_t)stream));
+  return STRUCTKV_OK;
+}
+
+}  // extern "C"

@@ -298,3 +298,61 @@ hipError_t launch_gather(const void*, const void*, int64_t, int64_t, void*, void
                          const SeqTable&, const int32_t*, hipStream_t) { ++g_launches; return hipSuccess; }
 
 }  // namespace skv
+
+// ---- the operators on a cache in use: their entry points, compiled here, and their launchers ------------------------------------
+#include "../../paper_2604_06746_amd/csrc/cache_api.cpp"
+
+namespace skv {
+
+static AttendPlan g_last_attend;
+static int32_t g_last_chunks;   // of the latest attend call: workgroups per KV head
+// rows per workgroup, workgroups, whether the chunks are joined, whether by the bf16 kernels
+extern "C" void structkv_stub_last_attend(int64_t* out) {
+  out[0] = 16 * g_last_attend.rb; out[1] = g_last_attend.blocks; out[2] = g_last_attend.join; out[3] = g_last_attend.mfma;
+  out[4] = (int64_t)g_last_attend.total_bytes; out[5] = g_last_chunks;
+}
+// the bookkeeping that the attend kernels go by: whole row blocks times chunks for every sequence, partial results side by side
+static bool attend_fits(const CacheTable& t, const AttendPlan& p, const AttendWork& w, int G) {
+  ++g_launches;
+  g_last_attend = p;
+  g_last_chunks = t.units[t.batch];
+  bool ok = p.rb >= 1 && p.rb <= 4 && p.min_chunk >= 16 * kAttendWaves && p.min_chunk % 32 == 0 && t.units[0] == 0 && t.part[0] == 0 &&
+            p.blocks == (int64_t)t.units[t.batch] * G && w.rows == (int64_t)t.cu_new[t.batch] * w.H;
+  for (int b = 0; ok && b < t.batch; ++b) {
+    const int fresh = t.cu_new[b + 1] - t.cu_new[b], blocks = (fresh * w.gs + 16 * p.rb - 1) / (16 * p.rb), units = t.units[b + 1] - t.units[b];
+    ok = fresh == 0 ? units == 0 && t.part[b + 1] == t.part[b] : units > 0 && units % blocks == 0;
+    if (ok && fresh) {
+      const int64_t nc = units / blocks, cap = t.cu[b + 1] - t.cu[b];
+      ok = t.part[b + 1] - t.part[b] == nc * fresh * w.H && (nc == 1 || p.join) && (!p.gather || p.join);
+      for (int64_t n : {cap, cap / 3, (int64_t)1}) {   // whatever the length, the chunks cover it
+        const int len = chunk_slots((int)n, (int)nc, p.min_chunk);
+        ok = ok && (int64_t)len * nc >= n && len % 32 == 0 && len >= p.min_chunk;
+      }
+    }
+  }
+  return ok;
+}
+hipError_t launch_cache_append(const CacheTable&, const CacheView&, const void*, const void*, int64_t, int64_t, const int32_t*,
+                               const float*, int64_t, int, int32_t*, hipStream_t) { ++g_launches; return hipSuccess; }
+hipError_t launch_cache_attend_f32(const CacheTable& t, const CacheView& c, const ScoreForm&, const AttendPlan& p, const AttendWork& w,
+                                   bool, hipStream_t) {
+  return attend_fits(t, p, w, c.G) && !p.mfma ? hipSuccess : hipErrorInvalidValue;
+}
+hipError_t launch_cache_combine(const CacheTable&, const CacheView&, const AttendPlan& p, const AttendWork&, bool, hipStream_t) {
+  ++g_launches;
+  return p.join ? hipSuccess : hipErrorInvalidValue;
+}
+hipError_t launch_cache_weights(const CacheTable&, const CacheView&, const ScoreForm&, const AttendWork&, const int32_t*, const int32_t*, int,
+                                bool, hipStream_t) { ++g_launches; return hipSuccess; }
+hipError_t launch_cache_accept(const CacheTable&, const CacheView&, const int32_t*, const int32_t*, int, int32_t*, hipStream_t) {
+  ++g_launches;
+  return hipSuccess;
+}
+hipError_t launch_cache_evict(const CacheTable& t, const CacheView&, const EvictWork& w, int, hipStream_t) {
+  ++g_launches;
+  bool ok = w.count && w.holes && w.moved && w.lens_out;
+  for (int b = 0; ok && b < t.batch; ++b) ok = t.units[b] >= 0 && t.units[b] <= t.cu[b + 1] - t.cu[b];
+  return ok ? hipSuccess : hipErrorInvalidValue;
+}
+
+}  // namespace skv
