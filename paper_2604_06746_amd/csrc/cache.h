@@ -64,6 +64,7 @@ struct AttendWork {
   int H, gs, min_chunk;
   float lambda;
   int64_t rows;           // new tokens x H
+  int64_t xs;             // scores: head h, slot s of sequence b at h xs + cu[b] + 4 b + s; 256 words behind the last head are nobody's
 };
 
 // Slots of a chunk when n of them are cut into at most nc: whole tiles for every wave.
@@ -77,6 +78,9 @@ hipError_t launch_cache_append(const CacheTable& t, const CacheView& c, const vo
                                int32_t* lens_out, hipStream_t st);
 hipError_t launch_cache_attend_f32(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p,
                                    const AttendWork& w, bool bf16, hipStream_t st);
+// a plan with mfma set
+hipError_t launch_cache_attend_bf16(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p,
+                                    const AttendWork& w, hipStream_t st);
 hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const AttendPlan& p, const AttendWork& w, bool bf16,
                                 hipStream_t st);
 hipError_t launch_cache_weights(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendWork& w,

@@ -101,6 +101,15 @@ structkv_status check_scores(const structkv_cache* c, int32_t H, float scale, fl
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
+size_t score_bytes(int H, int64_t slots, int batch) { return align_up(((size_t)H * (size_t)(slots + 4 * batch) + 256) * sizeof(float), 256); }
+
+// what the bf16 matrix kernels take: whole 16-byte pieces, and a tile's rows within 32 bits
+bool mfma_fits(const structkv_cache* c, const void* q, int64_t qst, int64_t qsh) {
+  const int64_t strides = (c->n_kv_heads > 1 ? c->stride_head : 0) | c->stride_slot | qst | qsh;
+  return c->dtype == STRUCTKV_DTYPE_BF16 && (c->head_dim == 64 || c->head_dim == 128) && strides % 8 == 0 &&
+         (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)q) & 15) == 0 && c->stride_slot < ((int64_t)1 << 25);
+}
+
 // Chunks: as many workgroups as fill the chip once or twice, but at least kLeastChunk slots each.
 constexpr int64_t kAttendBlocks = 512, kLeastChunk = 128;
 
@@ -109,8 +118,10 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   memset(p, 0, sizeof(*p));
   p->mfma = mfma;
   p->gather = gather;
-  p->rb = 1;
-  p->min_chunk = kAttendWaves * 16;
+  int64_t most_rows = 0;
+  for (int b = 0; b < c->batch; ++b) most_rows = std::max<int64_t>(most_rows, (int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs);
+  p->rb = !mfma || gather || most_rows <= 16 ? 1 : 2;
+  p->min_chunk = kAttendWaves * (mfma ? 32 : 16);
   const int rows_wg = 16 * p->rb;
   double work = 0;   // slots that the workgroups read in all
   for (int b = 0; b < c->batch; ++b)
@@ -134,7 +145,7 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   size_t off = 0;
   p->off_ml = off; off += align_up(parts * 2 * sizeof(float), 256);
   p->off_o = off;  off += align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256);
-  p->off_x = off;  off += gather ? align_up((size_t)H * (size_t)t->cu[c->batch] * sizeof(float), 256) : 0;
+  p->off_x = off;  off += gather ? score_bytes(H, t->cu[c->batch], c->batch) : 0;
   p->total_bytes = off;
   return STRUCTKV_OK;
 }
@@ -145,7 +156,7 @@ size_t most_attend_bytes(const structkv_cache* c, int H, int64_t new_tokens, int
   const size_t rows_wg = 64;
   const size_t parts = rows_wg * (size_t)kAttendBlocks + (size_t)new_tokens * H;
   return align_up(parts * 2 * sizeof(float), 256) + align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256) +
-         (c->mass ? align_up((size_t)H * (size_t)slots * sizeof(float), 256) : 0);
+         (c->mass ? score_bytes(H, slots, c->batch) : 0);
 }
 
 struct EvictSpace {
@@ -238,14 +249,15 @@ structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_h
         return fail(STRUCTKV_ERR_INVALID_ARG, "sequence %d: lambda > 0 is for single tokens; drafts gather their weights in structkv_cache_accept", b);
   AttendPlan p;
   const bool bf16 = cache->dtype == STRUCTKV_DTYPE_BF16;
-  st = plan_attend(cache, n_q_heads, lambda > 0.f, false, &t, &p);
+  st = plan_attend(cache, n_q_heads, lambda > 0.f, mfma_fits(cache, q, q_stride_tok, q_stride_head), &t, &p);
   if (st == STRUCTKV_OK) st = check_workspace(workspace, workspace_bytes, p.total_bytes);
   if (st != STRUCTKV_OK) return st;
   uint8_t* w8 = (uint8_t*)workspace;
   const AttendWork w = {q, q_stride_tok, q_stride_head, out, lse_out, (float*)(w8 + p.off_ml), (float*)(w8 + p.off_o),
                         p.gather ? (float*)(w8 + p.off_x) : nullptr, n_q_heads, n_q_heads / cache->n_kv_heads, p.min_chunk, lambda,
-                        (int64_t)t.cu_new[cache->batch] * n_q_heads};
-  SKV_HIP_CHECK(launch_cache_attend_f32(t, v, f, p, w, bf16, (hipStream_t)stream));
+                        (int64_t)t.cu_new[cache->batch] * n_q_heads, v.slots + 4 * cache->batch};
+  if (p.mfma) SKV_HIP_CHECK(launch_cache_attend_bf16(t, v, f, p, w, (hipStream_t)stream));
+  else SKV_HIP_CHECK(launch_cache_attend_f32(t, v, f, p, w, bf16, (hipStream_t)stream));
   if (p.join) SKV_HIP_CHECK(launch_cache_combine(t, v, p, w, bf16, (hipStream_t)stream));
   return STRUCTKV_OK;
 }
@@ -270,7 +282,7 @@ structkv_status structkv_cache_accept(const structkv_cache* cache, int32_t n_q_h
   if (weigh && (!q || !lse)) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda > 0 needs q and lse");
   if (weigh) {
     const AttendWork w = {q, q_stride_tok, q_stride_head, nullptr, const_cast<float*>(lse), nullptr, nullptr, nullptr, n_q_heads,
-                          n_q_heads / cache->n_kv_heads, 0, lambda, 0};
+                          n_q_heads / cache->n_kv_heads, 0, lambda, 0, 0};
     SKV_HIP_CHECK(launch_cache_weights(t, v, f, w, path, n_accept, STRUCTKV_MAX_DRAFTS, cache->dtype == STRUCTKV_DTYPE_BF16, (hipStream_t)stream));
   }
   SKV_HIP_CHECK(launch_cache_accept(t, v, path, n_accept, elem_bytes(cache), lens_out, (hipStream_t)stream));

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
       const bool seen = s < s1 && sees(mask, min(s, n - 1), h.base);
       x[i] = more ? full_score(f, acc[i], slope, pos ? at - pos[min(s, n - 1)] : 0) : acc[i] * f.c2;
       if (!seen) x[i] = -INFINITY;
-      if (w.x && s < s1 && row0 + l16 < rows) w.x[(int64_t)head * c.slots + h.lo + s] = x[i];
+      if (w.x && s < s1 && row0 + l16 < rows) w.x[head * w.xs + h.lo + 4 * p.b + s] = x[i];
     }
     float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
     top = fmaxf(top, __shfl_xor(top, 16));
@@ -323,9 +323,9 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
   __syncthreads();
   const int s = (int)u * 256 + threadIdx.x;
   if (s >= h.n) return;
-  const float* x = w.x + (int64_t)plane * heads * c.slots + h.lo + s;
+  const float* x = w.x + plane * heads * w.xs + h.lo + 4 * b + s;
   float sum = 0.f;
-  for (int i = 0; i < heads; ++i) sum += __builtin_amdgcn_exp2f(x[i * c.slots] - sh_lse[i]);
+  for (int i = 0; i < heads; ++i) sum += __builtin_amdgcn_exp2f(x[i * w.xs] - sh_lse[i]);
   float* mass = c.mass + plane * c.slots + h.lo + s;
   *mass = fmaf(w.lambda, *mass, sum);
 }

@@ -338,6 +338,12 @@ hipError_t launch_cache_attend_f32(const CacheTable& t, const CacheView& c, cons
                                    bool, hipStream_t) {
   return attend_fits(t, p, w, c.G) && !p.mfma ? hipSuccess : hipErrorInvalidValue;
 }
+hipError_t launch_cache_attend_bf16(const CacheTable& t, const CacheView& c, const ScoreForm&, const AttendPlan& p, const AttendWork& w,
+                                    hipStream_t) {
+  const bool ok = p.mfma && (c.d == 64 || c.d == 128) && (p.rb == 1 || p.rb == 2 || p.rb == 4) && p.min_chunk >= 32 * kAttendWaves &&
+                  (!p.gather || p.rb == 1) && (c.sh | c.ss | w.qst | w.qsh) % 8 == 0 && c.ss < (1 << 25);
+  return attend_fits(t, p, w, c.G) && ok ? hipSuccess : hipErrorInvalidValue;
+}
 hipError_t launch_cache_combine(const CacheTable&, const CacheView&, const AttendPlan& p, const AttendWork&, bool, hipStream_t) {
   ++g_launches;
   return p.join ? hipSuccess : hipErrorInvalidValue;
