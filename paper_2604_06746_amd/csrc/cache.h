@@ -52,6 +52,7 @@ struct AttendPlan {
   int gather;             // the weights are gathered: the first launch leaves the scores in the workspace
   int join;               // a second launch joins the chunks (and gathers); else the first one writes out and lse
   int64_t blocks;         // workgroups of the first launch
+  int64_t most_chunks;    // of a sequence
   size_t off_ml, off_o, off_x, total_bytes;   // workspace: (M, Z) and sums of the chunks, scores [H][slots]
 };
 
@@ -83,8 +84,11 @@ hipError_t launch_cache_attend_bf16(const CacheTable& t, const CacheView& c, con
                                     const AttendWork& w, hipStream_t st);
 hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const AttendPlan& p, const AttendWork& w, bool bf16,
                                 hipStream_t st);
-hipError_t launch_cache_weights(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendWork& w,
-                                const int32_t* path, const int32_t* n_accept, int most_new, bool bf16, hipStream_t st);
+hipError_t launch_cache_weights_f32(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendWork& w,
+                                    const int32_t* path, const int32_t* n_accept, bool bf16, hipStream_t st);
+// caches and queries that the bf16 matrix kernels take
+hipError_t launch_cache_weights_bf16(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendWork& w,
+                                     const int32_t* path, const int32_t* n_accept, hipStream_t st);
 hipError_t launch_cache_accept(const CacheTable& t, const CacheView& c, const int32_t* path, const int32_t* n_accept,
                                int elem_bytes, int32_t* lens_out, hipStream_t st);
 // lists: [batch][planes] counts, then per plane and sequence the holes and the slots that fill them (evict_list_words)

@@ -127,18 +127,20 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   for (int b = 0; b < c->batch; ++b)
     work += (double)ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, rows_wg) * c->n_kv_heads * (double)(t->cu[b + 1] - t->cu[b]);
   const int64_t each = std::max<int64_t>(kLeastChunk, (int64_t)std::ceil(work / kAttendBlocks));
-  int64_t units = 0, part = 0;
+  int64_t units = 0, part = 0, stretches = 0;   // (of 256 slots, whose weights a workgroup of the join gathers)
   p->join = gather;
   for (int b = 0; b < c->batch; ++b) {
     const int64_t fresh = t->cu_new[b + 1] - t->cu_new[b], cap = t->cu[b + 1] - t->cu[b];
     const int64_t nc = std::max<int64_t>(1, ceil_div(cap, each));
     units += nc * ceil_div(fresh * gs, rows_wg);
     part += fresh * H * nc;
-    if (units * c->n_kv_heads >= ((int64_t)1 << 31) || part >= ((int64_t)1 << 31))
+    stretches += gather ? ceil_div(cap, 256) * c->planes : 0;
+    if (units * c->n_kv_heads >= ((int64_t)1 << 31) || part + stretches >= ((int64_t)1 << 31))
       return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
     t->units[b + 1] = (int32_t)units;
     t->part[b + 1] = (int32_t)part;
     if (fresh > 0 && nc > 1) p->join = 1;
+    if (fresh > 0) p->most_chunks = std::max(p->most_chunks, nc);
   }
   p->blocks = units * c->n_kv_heads;
   const size_t parts = p->join ? (size_t)part : 0;
@@ -283,7 +285,8 @@ structkv_status structkv_cache_accept(const structkv_cache* cache, int32_t n_q_h
   if (weigh) {
     const AttendWork w = {q, q_stride_tok, q_stride_head, nullptr, const_cast<float*>(lse), nullptr, nullptr, nullptr, n_q_heads,
                           n_q_heads / cache->n_kv_heads, 0, lambda, 0, 0};
-    SKV_HIP_CHECK(launch_cache_weights(t, v, f, w, path, n_accept, STRUCTKV_MAX_DRAFTS, cache->dtype == STRUCTKV_DTYPE_BF16, (hipStream_t)stream));
+    if (mfma_fits(cache, q, q_stride_tok, q_stride_head)) SKV_HIP_CHECK(launch_cache_weights_bf16(t, v, f, w, path, n_accept, (hipStream_t)stream));
+    else SKV_HIP_CHECK(launch_cache_weights_f32(t, v, f, w, path, n_accept, cache->dtype == STRUCTKV_DTYPE_BF16, (hipStream_t)stream));
   }
   SKV_HIP_CHECK(launch_cache_accept(t, v, path, n_accept, elem_bytes(cache), lens_out, (hipStream_t)stream));
   return STRUCTKV_OK;

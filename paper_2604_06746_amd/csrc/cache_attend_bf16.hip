@@ -12,31 +12,10 @@
 // components) fill each other's waits with about 100 KB on their way.
 // The rows' references M follow lazily: they are raised only when a score lies more than 2^8 above one of them, so that the usual tile has
 // no exchange between lanes and no rescaling.
-#include "cache.h"
+#include "cache_bf16.h"
 
 namespace skv {
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) float floatx2;
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
-typedef const __attribute__((address_space(1))) void* gbl_ptr_t;
-
-// s_waitcnt with only the vector-memory counter constrained (gfx9 encoding: vmcnt in bits 3:0 and 15:14); no access moves across
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  static_assert(N < 64, "the counter's range");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
-  asm volatile("" ::: "memory");
-}
-// ... with only the LDS counter constrained, to zero
-__device__ __forceinline__ void wait_lds() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4) | (0 << 8));
-  asm volatile("" ::: "memory");
-}
 
 // What the matrix instruction wants of V for four blocks of 16 components: ds_read_b64_tr_b16 reads, by 16 lanes, 8 bytes each, four rows of
 // 16 numbers and hands lane i column i of them.  The wait is part of the statement: nothing uses or moves a register before it is there.
@@ -61,9 +40,6 @@ __device__ __forceinline__ void read_columns(bf16x8 (&v)[4], uint32_t a0, uint32
 }
 typedef floatx4 __attribute__((aligned(4))) floatx4_at_4;
 
-enum { kPlain = 0, kCapped = 1, kBiased = 2 };   // how scores are formed: scaled; capped; in full
-// Up to this cap its quick form is taken, whose error of cap x 2^-22 is a weight's relative one: 2^-14 here, a 64th of a bf16 rounding.
-constexpr float kLargestQuickCap = 256.f;
 constexpr float kSlack = 8.f;                    // how far above its reference a score may lie, log2
 
 template <class TAB, int D, int RB, int MODE, bool SAVE>
@@ -79,21 +55,36 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const AttendPlace p = attend_place(tab, c.G, w.gs, 16 * RB);
   const Held h = held(tab, c.lens, p.b);
+  // the queries first: the length has no part in their addresses
+  const int new0 = tab.cu_new[p.b], rows = h.fresh * w.gs, row0 = p.rc * 16 * RB;
+  bf16x8 qf[RB][KS];
+  uint64_t mask[RB];
+  float slope[RB];
+  int at[RB];
+  float* save = nullptr;   // where this lane's scores go
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = min(row0 + rb * 16 + l16, rows - 1), t = row / w.gs, head = p.g * w.gs + row - t * w.gs;
+    const int64_t r = new0 + t;
+    const uint16_t* qrow = (const uint16_t*)w.q + r * w.qst + (int64_t)head * w.qsh;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qrow + ks * 32 + 8 * q4);
+    mask[rb] = row_mask(f, r, t);
+    slope[rb] = MODE == kBiased && f.slopes ? f.slopes[head] : 0.f;
+    if (SAVE) save = w.x + head * w.xs + h.lo + 4 * p.b;
+  }
   const int n = h.base < 0 ? 0 : h.n;
   const int len = chunk_slots(n, p.nc, w.min_chunk);
   const int s0 = (int)min((int64_t)n, (int64_t)p.chunk * len), s1 = min(n, s0 + len);
   if (s0 >= s1 && (p.nc > 1 || w.x)) return;   // (the join reads no more chunks than have slots)
-  const int new0 = tab.cu_new[p.b], rows = h.fresh * w.gs, row0 = p.rc * 16 * RB;
 
   const uint16_t* kg = (const uint16_t*)c.k + (int64_t)p.g * c.sh + h.lo * c.ss;
   const uint16_t* vg = (const uint16_t*)c.v + (int64_t)p.g * c.sh + h.lo * c.ss;
   const int32_t* pos = MODE == kBiased && f.slopes ? c.pos + (c.planes > 1 ? p.g * c.slots : 0) + h.lo : nullptr;
   uint8_t* kt = lds + wave * SLOT;
   uint8_t* vt = kt + TILE;
-  // Tile in LDS: piece (slot, seg) at unit slot * SEGS + (seg ^ its swizzle), so that 16 lanes with a slot each and one seg (K), and 32
-  // lanes with four pieces of 8 bytes of eight slots (V) use every bank once.
-  auto swz_k = [](int s) { return SEGS == 16 ? (s & 15) : ((s >> 1) & 7); };
-  auto swz_v = [](int s) { return SEGS == 16 ? (s & 7) << 1 : ((s >> 1) & 3) << 1; };
+  auto swz_k = [](int s) { return swizzle_k<SEGS>(s); };
+  auto swz_v = [](int s) { return swizzle_v<SEGS>(s); };
   uint32_t koff[NI], voff[NI];   // of the pieces this lane fetches, from the tile's first row
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
@@ -123,27 +114,12 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   };
   auto fetch_v = [&](int j0) __attribute__((always_inline)) { fetch(vg, voff, swz_v, j0, vt); };
 
-  // this wave's tiles: wave, wave + 4, ...; the first one is requested ahead of the queries
+  // this wave's tiles: wave, wave + 4, ...
   const int tiles = s1 > s0 ? (s1 - s0 + 31) / 32 : 0, mine = tiles > wave ? (tiles - wave + kAttendWaves - 1) / kAttendWaves : 0;
   if (mine > 0) { fetch_k(s0 + 32 * wave); fetch_v(s0 + 32 * wave); }
 
-  bf16x8 qf[RB][KS];
-  uint64_t mask[RB];
-  float slope[RB];
-  int at[RB];
-  float* save = nullptr;   // where this lane's scores go
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int row = min(row0 + rb * 16 + l16, rows - 1), t = row / w.gs, head = p.g * w.gs + row - t * w.gs;
-    const int64_t r = new0 + t;
-    const uint16_t* qrow = (const uint16_t*)w.q + r * w.qst + (int64_t)head * w.qsh;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qrow + ks * 32 + 8 * q4);
-    mask[rb] = row_mask(f, r, t);
-    slope[rb] = MODE == kBiased && pos ? f.slopes[head] : 0.f;
-    at[rb] = MODE == kBiased && pos && n > 0 ? pos[h.base + t] : 0;
-    if (SAVE) save = w.x + head * w.xs + h.lo + 4 * p.b;
-  }
+  for (int rb = 0; rb < RB; ++rb) at[rb] = MODE == kBiased && pos && n > 0 ? pos[h.base + min(row0 + rb * 16 + l16, rows - 1) / w.gs] : 0;
   // (kept in registers from here on; pinned once all of them are on their way)
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
@@ -160,7 +136,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   }
   // from here on rows differ in what they see: the first fresh slot, or the end
   const int edge = min(s1, f.tree || h.fresh > 1 ? max(h.base, 0) : n);
-  const float cap2 = f.softcap * 1.4426950408889634f, cap_in = f.scale * f.inv_cap * 2.885390082f;
+  const QuickCap cap(f);
 
   for (int i = 0; i < mine; ++i) {
     const int j0 = s0 + 32 * (wave + kAttendWaves * i), next = j0 + 32 * kAttendWaves;
@@ -181,14 +157,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
         for (int rb = 0; rb < RB; ++rb) x[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rb][ks], x[kb][rb], 0, 0, 0);
       }
     // scores in the log2 domain, but for their scale where there is nothing else to them
-    if (MODE == kCapped) {   // c tanh(y / c) = c - 2 c / (1 + e^(2 y / c)): off by c 2^-22 at most
+    if (MODE == kCapped) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            x[kb][rb][e] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[kb][rb][e] * cap_in)), cap2);
+            x[kb][rb][e] = cap(x[kb][rb][e]);
     } else if (MODE == kBiased) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
@@ -309,11 +285,7 @@ hipError_t attend(const CacheTable& t, const CacheView& c, const ScoreForm& f, c
     auto go = [&](auto mode, auto save) {
       cache_attend_bf16_kernel<TAB, D, RB, decltype(mode)::value, decltype(save)::value><<<grid, block, 0, st>>>(tab, c, f, w);
     };
-    auto by_mode = [&](auto save) {
-      if (f.slopes || f.softcap > kLargestQuickCap) go(std::integral_constant<int, kBiased>{}, save);
-      else if (f.softcap > 0.f) go(std::integral_constant<int, kCapped>{}, save);
-      else go(std::integral_constant<int, kPlain>{}, save);
-    };
+    auto by_mode = [&](auto save) { with_mode(f, [&](auto mode) { go(mode, save); }); };
     if constexpr (RB == 1) {
       if (w.x) { by_mode(std::true_type{}); return; }
     }

@@ -252,108 +252,15 @@ hipError_t weights(const CacheTable& t, const CacheView& c, const ScoreForm& f, 
   });
 }
 
-// ---- the chunks of a row joined, and the single tokens' weights ----------------------------------------------------------------
-// Chunk i of a row has (M_i, Z_i, O_i); with M = max M_i: Z = sum 2^(M_i - M) Z_i, out = sum 2^(M_i - M) O_i / Z.  A workgroup per row, its
-// threads on 256 / (DP / 4) shares of the chunks.  The workgroups behind the rows' add the weights: 2^(x - lse) from the scores that the
-// first launch left, so that the cache is read once.
-template <class TAB, class T, int DP>
-__global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c, AttendWork w, int rows_wg) {
-  short_kernel_priority();
-  constexpr int LANES = DP / 4, PARTS = 256 / LANES;
-  __shared__ float sh_o[256][4];
-  __shared__ float sh_z[PARTS];
-  extern __shared__ float sh_lse[];   // heads of a plane
-  if ((int64_t)blockIdx.x < w.rows) {
-    const int64_t at = blockIdx.x;
-    const int r = (int)(at / w.H);
-    int b = 0;
-    while (b + 1 < tab.batch && r >= tab.cu_new[b + 1]) ++b;
-    const Held h = held(tab, c.lens, b);
-    const int n = h.base < 0 ? 0 : h.n, rcs = (h.fresh * w.gs + rows_wg - 1) / rows_wg, nc = (tab.units[b + 1] - tab.units[b]) / rcs;
-    if (nc == 1 && !w.x) return;   // (the first launch has written it)
-    const int len = chunk_slots(n, nc, w.min_chunk), live = (n + len - 1) / len;
-    const int64_t part0 = tab.part[b] + (at - (int64_t)tab.cu_new[b] * w.H) * nc;
-    const float* ml = w.ml + part0 * 2;
-    float top = kNothingSeen;
-    for (int i = 0; i < live; ++i) top = fmaxf(top, ml[2 * i]);
-    const int part = threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    float z = 0.f;
-    for (int i = part; i < live; i += PARTS) {
-      const float s = __builtin_amdgcn_exp2f(ml[2 * i] - top);
-      z = fmaf(s, ml[2 * i + 1], z);
-      if (col < c.d) o += *reinterpret_cast<const floatx4*>(w.o + (part0 + i) * DP + col) * s;
-    }
-    *reinterpret_cast<floatx4*>(sh_o[threadIdx.x]) = o;
-    if (col == 0) sh_z[part] = z;
-    __syncthreads();
-    if (part == 0 && col < c.d) {
-      z = 0.f;
-      o = floatx4{0.f, 0.f, 0.f, 0.f};
-      for (int i = 0; i < PARTS; ++i) { z += sh_z[i]; o += *reinterpret_cast<const floatx4*>(sh_o[i * LANES + threadIdx.x]); }
-      const float inv = z > 0.f ? 1.f / z : 0.f;
-      for (int i = 0; i < 4 && col + i < c.d; ++i) put_out<T>((T*)w.out + at * c.d + col + i, o[i] * inv);
-      if (col == 0) w.lse[at] = z > 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
-    }
-    return;
-  }
-  // weights: 256 slots of a plane
-  int64_t u = (int64_t)blockIdx.x - w.rows;
-  const int plane = (int)(u % c.planes);
-  u /= c.planes;
-  int b = 0;
-  for (; b < tab.batch; ++b) {
-    const int64_t blocks = (tab.cu[b + 1] - tab.cu[b] + 255) / 256;
-    if (u < blocks) break;
-    u -= blocks;
-  }
-  if (b >= tab.batch) return;
-  const Held h = held(tab, c.lens, b);
-  if (h.fresh != 1 || h.base < 0 || u * 256 >= h.n) return;
-  const int nc = (tab.units[b + 1] - tab.units[b]) / ((w.gs + rows_wg - 1) / rows_wg);
-  const int len = chunk_slots(h.n, nc, w.min_chunk), live = (h.n + len - 1) / len;
-  const int heads = w.H / c.planes;
-  for (int i = threadIdx.x; i < heads; i += 256) {
-    const float* ml = w.ml + (tab.part[b] + (int64_t)(plane * heads + i) * nc) * 2;
-    float top = kNothingSeen, z = 0.f;
-    for (int k = 0; k < live; ++k) top = fmaxf(top, ml[2 * k]);
-    for (int k = 0; k < live; ++k) z = fmaf(__builtin_amdgcn_exp2f(ml[2 * k] - top), ml[2 * k + 1], z);
-    sh_lse[i] = z > 0.f ? top + __builtin_amdgcn_logf(z) : INFINITY;
-  }
-  __syncthreads();
-  const int s = (int)u * 256 + threadIdx.x;
-  if (s >= h.n) return;
-  const float* x = w.x + plane * heads * w.xs + h.lo + 4 * b + s;
-  float sum = 0.f;
-  for (int i = 0; i < heads; ++i) sum += __builtin_amdgcn_exp2f(x[i * w.xs] - sh_lse[i]);
-  float* mass = c.mass + plane * c.slots + h.lo + s;
-  *mass = fmaf(w.lambda, *mass, sum);
-}
-
 }  // namespace
 
 hipError_t launch_cache_attend_f32(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p,
                                    const AttendWork& w, bool bf16, hipStream_t st) {
   return bf16 ? attend<uint16_t>(t, c, f, p, w, st) : attend<float>(t, c, f, p, w, st);
 }
-hipError_t launch_cache_weights(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendWork& w,
-                                const int32_t* path, const int32_t* n_accept, int, bool bf16, hipStream_t st) {
+hipError_t launch_cache_weights_f32(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendWork& w,
+                                    const int32_t* path, const int32_t* n_accept, bool bf16, hipStream_t st) {
   return bf16 ? weights<uint16_t>(t, c, f, w, path, n_accept, st) : weights<float>(t, c, f, w, path, n_accept, st);
-}
-hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const AttendPlan& p, const AttendWork& w, bool bf16,
-                                hipStream_t st) {
-  int64_t blocks = w.rows;
-  if (p.gather)
-    for (int b = 0; b < t.batch; ++b) blocks += ceil_div(t.cu[b + 1] - t.cu[b], 256) * c.planes;
-  const size_t lds = p.gather ? sizeof(float) * (w.H / c.planes) : 0;
-  with_cache_table(t, [&](const auto& tab) {
-    with_dim(c.d, [&](auto dp) {
-      using TAB = std::decay_t<decltype(tab)>;
-      if (bf16) cache_combine_kernel<TAB, uint16_t, decltype(dp)::value><<<dim3((unsigned)blocks), 256, lds, st>>>(tab, c, w, 16 * p.rb);
-      else cache_combine_kernel<TAB, float, decltype(dp)::value><<<dim3((unsigned)blocks), 256, lds, st>>>(tab, c, w, 16 * p.rb);
-    });
-  });
-  return hipGetLastError();
 }
 
 }  // namespace skv

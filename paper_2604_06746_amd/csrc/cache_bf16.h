@@ -1,0 +1,52 @@
+// What the bf16 matrix kernels on a cache share.
+#pragma once
+#include "cache.h"
+
+namespace skv {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float floatx2;
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef const __attribute__((address_space(1))) void* gbl_ptr_t;
+
+// s_waitcnt with only the vector-memory counter constrained (gfx9 encoding: vmcnt in bits 3:0 and 15:14); no access moves across
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "the counter's range");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+  asm volatile("" ::: "memory");
+}
+// ... with only the LDS counter constrained, to zero
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4) | (0 << 8));
+  asm volatile("" ::: "memory");
+}
+
+enum { kPlain = 0, kCapped = 1, kBiased = 2 };   // how scores are formed: scaled; capped; in full
+// Up to this cap its quick form is taken, whose error of cap x 2^-22 is a weight's relative one: 2^-14 here, a 64th of a bf16 rounding.
+constexpr float kLargestQuickCap = 256.f;
+// in the log2 domain, c tanh(y / c) = c - 2 c / (1 + e^(2 y / c))
+struct QuickCap {
+  float cap2, in;
+  __device__ __forceinline__ explicit QuickCap(const ScoreForm& f) : cap2(f.softcap * 1.4426950408889634f), in(f.scale * f.inv_cap * 2.885390082f) {}
+  __device__ __forceinline__ float operator()(float s) const {
+    return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * in)), cap2);
+  }
+};
+// the mode that a call's scores need
+template <class F>
+void with_mode(const ScoreForm& f, F go) {
+  if (f.slopes || f.softcap > kLargestQuickCap) go(std::integral_constant<int, kBiased>{});
+  else if (f.softcap > 0.f) go(std::integral_constant<int, kCapped>{});
+  else go(std::integral_constant<int, kPlain>{});
+}
+
+// A tile of 32 rows on its way to LDS, 16-byte pieces: piece (row, seg) at unit row * SEGS + (seg ^ swizzle(row)).  The swizzles let 16 lanes
+// with a row each and one seg (K), and 32 lanes with 8-byte pieces of eight rows (V) use every bank once.
+template <int SEGS> __device__ __forceinline__ constexpr int swizzle_k(int s) { return SEGS == 16 ? (s & 15) : ((s >> 1) & 7); }
+template <int SEGS> __device__ __forceinline__ constexpr int swizzle_v(int s) { return SEGS == 16 ? (s & 7) << 1 : ((s >> 1) & 3) << 1; }
+
+}  // namespace skv

@@ -1,0 +1,237 @@
+// The chunks of an attend call joined, and the single tokens' weights gathered.
+//
+// Chunk i of a row left (M_i, Z_i, O_i); with M = max M_i: Z = sum 2^(M_i - M) Z_i, out = sum 2^(M_i - M) O_i / Z, lse = ln 2 (M + log2 Z).
+// A workgroup per row.  The workgroups behind the rows' add the weights of a stretch of slots of one plane, 2^(x - lse) from the scores that
+// the first launch left, so that the cache is read once.  Few bytes, so what counts is the chain of loads: length; then the chunks' M and Z
+// beside the sums or the scores themselves, all at once; nothing is loaded after the norms are known.
+#include "cache.h"
+
+namespace skv {
+namespace {
+
+// over the 64 lanes, by moves inside the rows of 16 and then between them (six vector instructions; by shuffles six trips through the LDS
+// crossbar, which made a plane of 32 heads' norms take 5 us)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float x, float without) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(without), __float_as_int(x), CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ float last_lane(float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); }
+__device__ __forceinline__ float wave_top(float x) {
+  x = fmaxf(x, moved<0x111, 0xF>(x, -INFINITY));
+  x = fmaxf(x, moved<0x112, 0xF>(x, -INFINITY));
+  x = fmaxf(x, moved<0x114, 0xF>(x, -INFINITY));
+  x = fmaxf(x, moved<0x118, 0xF>(x, -INFINITY));
+  x = fmaxf(x, moved<0x142, 0xA>(x, -INFINITY));
+  x = fmaxf(x, moved<0x143, 0xC>(x, -INFINITY));
+  return last_lane(x);
+}
+__device__ __forceinline__ float wave_total(float x) {
+  x += moved<0x111, 0xF>(x, 0.f);
+  x += moved<0x112, 0xF>(x, 0.f);
+  x += moved<0x114, 0xF>(x, 0.f);
+  x += moved<0x118, 0xF>(x, 0.f);
+  x += moved<0x142, 0xA>(x, 0.f);
+  x += moved<0x143, 0xC>(x, 0.f);
+  return last_lane(x);
+}
+typedef float __attribute__((ext_vector_type(2))) floatx2;
+
+constexpr int kAhead = 8;   // loads of a thread that are on their way at once
+
+// What joining a row needs to know; n: its slots.
+struct Row {
+  int b, live;
+  int64_t part0;
+  bool written;   // by the first launch
+};
+template <class TAB>
+__device__ __forceinline__ Row row_of(const TAB& tab, const CacheView& c, const AttendWork& w, int64_t at, int rows_wg) {
+  const int r = (int)(at / w.H);
+  Row row;
+  int b = 0;
+  while (b + 1 < tab.batch && r >= tab.cu_new[b + 1]) ++b;
+  const Held h = held(tab, c.lens, b);
+  const int n = h.base < 0 ? 0 : h.n, rcs = (h.fresh * w.gs + rows_wg - 1) / rows_wg, nc = (tab.units[b + 1] - tab.units[b]) / rcs;
+  const int len = chunk_slots(n, nc, w.min_chunk);
+  row.b = b;
+  row.live = (n + len - 1) / len;
+  row.part0 = tab.part[b] + (at - (int64_t)tab.cu_new[b] * w.H) * nc;
+  row.written = nc == 1 && !w.x;
+  return row;
+}
+template <class T>
+__device__ __forceinline__ void put_row(const AttendWork& w, int64_t at, int d, int col, floatx4 o, float top, float z) {
+  const float inv = z > 0.f ? 1.f / z : 0.f;
+  for (int e = 0; e < 4 && col + e < d; ++e) put_out<T>((T*)w.out + at * d + col + e, o[e] * inv);
+  if (col == 0) w.lse[at] = z > 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
+}
+
+// FEW: at most kFewChunks chunks a row, a lane group of DP / 4 a row; else a workgroup a row, its lane groups on shares of the chunks
+constexpr int kFewChunks = 8;
+template <class TAB, class T, int DP, bool FEW>
+__global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c, AttendWork w, int rows_wg, int row_blocks, int stretch) {
+  short_kernel_priority();
+  constexpr int LANES = DP / 4, PARTS = 256 / LANES;
+  __shared__ __attribute__((aligned(16))) float sh[256 * 4];
+  __shared__ float zs[4];
+  extern __shared__ float norms[];   // of a plane's heads
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
+  if ((int)blockIdx.x < row_blocks) {
+    const int64_t at = FEW ? (int64_t)blockIdx.x * PARTS + part : blockIdx.x;
+    if (at >= w.rows) return;
+    const Row row = row_of(tab, c, w, at, rows_wg);
+    if (row.written) return;
+    const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + row.part0;
+    const float* po = w.o + row.part0 * DP + col;
+    const bool mine = col < c.d;
+    constexpr int STEP = FEW ? 1 : PARTS;
+    const int i0 = FEW ? 0 : part;
+    floatx4 first[kAhead];
+    floatx2 stat[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + k * STEP;
+      stat[k] = i < row.live ? ml[i] : floatx2{kNothingSeen, 0.f};
+      first[k] = mine && i < row.live ? *reinterpret_cast<const floatx4*>(po + (int64_t)i * DP) : floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    float top = kNothingSeen;
+    if (FEW) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) top = fmaxf(top, stat[k][0]);
+    } else {
+      for (int i = lane; i < row.live; i += 64) top = fmaxf(top, ml[i][0]);
+      top = wave_top(top);
+    }
+    float z = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const float s = __builtin_amdgcn_exp2f(stat[k][0] - top);
+      z = fmaf(s, stat[k][1], z);
+      o += first[k] * s;
+    }
+    if (FEW) {
+      static_assert(kFewChunks == kAhead, "all of a row's chunks at once");
+      if (mine) put_row<T>(w, at, c.d, col, o, top, z);
+      return;
+    }
+    for (int i = part + kAhead * PARTS; i < row.live; i += PARTS) {
+      const float s = __builtin_amdgcn_exp2f(ml[i][0] - top);
+      z = fmaf(s, ml[i][1], z);
+      if (mine) o += *reinterpret_cast<const floatx4*>(po + (int64_t)i * DP) * s;
+    }
+    // the shares: lanes of a wave that have the same components, then the waves
+    for (int m = LANES; m < 64; m <<= 1) {
+      z += __shfl_xor(z, m);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m);
+    }
+    if (lane < LANES) *reinterpret_cast<floatx4*>(sh + (wave * LANES + lane) * 4) = o;
+    if (lane == 0) zs[wave] = z;
+    __syncthreads();
+    if ((int)threadIdx.x < LANES && mine) {
+      z = (zs[0] + zs[1]) + (zs[2] + zs[3]);
+      o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o += *reinterpret_cast<const floatx4*>(sh + (i * LANES + threadIdx.x) * 4);
+      put_row<T>(w, at, c.d, col, o, top, z);
+    }
+    return;
+  }
+  // weights
+  int u = (int)blockIdx.x - row_blocks;
+  const int plane = u % c.planes;
+  u /= c.planes;
+  int b = 0;
+  for (; b < tab.batch; ++b) {
+    const int blocks = (int)((tab.cu[b + 1] - tab.cu[b] + stretch - 1) / stretch);
+    if (u < blocks) break;
+    u -= blocks;
+  }
+  if (b >= tab.batch) return;
+  const Held h = held(tab, c.lens, b);
+  const int s0 = u * stretch;
+  if (h.fresh != 1 || h.base < 0 || s0 >= h.n) return;
+  const int nc = (tab.units[b + 1] - tab.units[b]) / ((w.gs + rows_wg - 1) / rows_wg);
+  const int len = chunk_slots(h.n, nc, w.min_chunk), live = (h.n + len - 1) / len;
+  const int heads = w.H / c.planes;
+  const float* x = w.x + plane * heads * w.xs + h.lo + 4 * b;
+  float* mass = c.mass + plane * c.slots + h.lo;
+  int s = s0 + threadIdx.x;
+  const int s1 = min(s0 + stretch, h.n);
+  float ahead[kAhead], old = s < s1 ? mass[s] : 0.f;
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) ahead[k] = s < s1 && k < heads ? x[k * w.xs + s] : -INFINITY;
+  for (int i0 = wave; i0 < heads; i0 += 4 * kAhead) {   // a lane a chunk, the wave's heads at once
+    floatx2 a[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + 4 * j;
+      const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + tab.part[b] + (int64_t)(plane * heads + i) * nc;
+      a[j] = i < heads && lane < live ? ml[lane] : floatx2{kNothingSeen, 0.f};
+      for (int k = lane + 64; i < heads && k < live; k += 64) {
+        const float top = fmaxf(a[j][0], ml[k][0]);
+        a[j] = floatx2{top, a[j][1] * __builtin_amdgcn_exp2f(a[j][0] - top) + ml[k][1] * __builtin_amdgcn_exp2f(ml[k][0] - top)};
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i0 + 4 * j >= heads) break;
+      const float top = wave_top(a[j][0]), z = wave_total(a[j][1] * __builtin_amdgcn_exp2f(a[j][0] - top));
+      if (lane == 0) norms[i0 + 4 * j] = z > 0.f ? top + __builtin_amdgcn_logf(z) : INFINITY;
+    }
+  }
+  __syncthreads();
+  for (; s < s1; s += 256) {
+    float sum = 0.f;
+    for (int i0 = 0; i0 < heads; i0 += kAhead) {
+      float now[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) now[k] = ahead[k];
+      // the next heads, or the first ones of the next slot
+      const bool same = i0 + kAhead < heads;
+      const int sn = same ? s : s + 256, in = same ? i0 + kAhead : 0;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) ahead[k] = sn < s1 && in + k < heads ? x[(in + k) * w.xs + sn] : -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + k < heads) sum += __builtin_amdgcn_exp2f(now[k] - norms[i0 + k]);
+    }
+    const float was = old;
+    old = s + 256 < s1 ? mass[s + 256] : 0.f;
+    mass[s] = fmaf(w.lambda, was, sum);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const AttendPlan& p, const AttendWork& w, bool bf16,
+                                hipStream_t st) {
+  const auto launch = [&](auto dp, auto few) {
+    constexpr int DP = decltype(dp)::value;
+    constexpr bool FEW = decltype(few)::value;
+    const int64_t row_blocks = FEW ? ceil_div(w.rows, 256 / (DP / 4)) : w.rows;
+    // slots of a workgroup: one a thread, four where that still leaves the chip four workgroups a CU
+    int64_t blocks = row_blocks, fine = 0;
+    int stretch = 256;
+    if (p.gather) {
+      for (int b = 0; b < t.batch; ++b) fine += ceil_div(t.cu[b + 1] - t.cu[b], 256) * c.planes;
+      if (fine >= 4 * 1024) stretch = 1024;
+      for (int b = 0; b < t.batch; ++b) blocks += ceil_div(t.cu[b + 1] - t.cu[b], stretch) * c.planes;
+    }
+    const size_t lds = p.gather ? sizeof(float) * (w.H / c.planes) : 0;
+    with_cache_table(t, [&](const auto& tab) {
+      using TAB = std::decay_t<decltype(tab)>;
+      const dim3 grid((unsigned)blocks);
+      if (bf16) cache_combine_kernel<TAB, uint16_t, DP, FEW><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
+      else cache_combine_kernel<TAB, float, DP, FEW><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
+    });
+    return hipGetLastError();
+  };
+  const auto by_chunks = [&](auto dp) { return p.most_chunks <= kFewChunks ? launch(dp, std::true_type{}) : launch(dp, std::false_type{}); };
+  if (c.d <= 64) return by_chunks(std::integral_constant<int, 64>{});
+  if (c.d <= 128) return by_chunks(std::integral_constant<int, 128>{});
+  return by_chunks(std::integral_constant<int, 256>{});
+}
+
+}  // namespace skv

@@ -348,8 +348,13 @@ hipError_t launch_cache_combine(const CacheTable&, const CacheView&, const Atten
   ++g_launches;
   return p.join ? hipSuccess : hipErrorInvalidValue;
 }
-hipError_t launch_cache_weights(const CacheTable&, const CacheView&, const ScoreForm&, const AttendWork&, const int32_t*, const int32_t*, int,
-                                bool, hipStream_t) { ++g_launches; return hipSuccess; }
+hipError_t launch_cache_weights_f32(const CacheTable&, const CacheView&, const ScoreForm&, const AttendWork&, const int32_t*, const int32_t*,
+                                    bool, hipStream_t) { ++g_launches; return hipSuccess; }
+hipError_t launch_cache_weights_bf16(const CacheTable&, const CacheView& c, const ScoreForm&, const AttendWork& w, const int32_t*,
+                                     const int32_t*, hipStream_t) {
+  ++g_launches;
+  return (c.d == 64 || c.d == 128) && (c.sh | c.ss | w.qst | w.qsh) % 8 == 0 && c.ss < (1 << 25) ? hipSuccess : hipErrorInvalidValue;
+}
 hipError_t launch_cache_accept(const CacheTable&, const CacheView&, const int32_t*, const int32_t*, int, int32_t*, hipStream_t) {
   ++g_launches;
   return hipSuccess;
