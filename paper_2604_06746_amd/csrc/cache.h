@@ -91,13 +91,21 @@ hipError_t launch_cache_weights_bf16(const CacheTable& t, const CacheView& c, co
                                      const int32_t* path, const int32_t* n_accept, hipStream_t st);
 hipError_t launch_cache_accept(const CacheTable& t, const CacheView& c, const int32_t* path, const int32_t* n_accept,
                                int elem_bytes, int32_t* lens_out, hipStream_t st);
-// lists: [batch][planes] counts, then per plane and sequence the holes and the slots that fill them (evict_list_words)
+// Up to this capacity of the longest sequence a workgroup holds a sequence's keys in registers; beyond, the launches take turns at digits of
+// them through records in the workspace: per plane and sequence evict_hist_words() words, per plane and share of a sequence's slots
+// (evict_shares of its capacity) the largest position and four counts.
+constexpr int64_t kEvictShort = 32768;
+int evict_shares(int64_t cap);
+size_t evict_hist_words();
 struct EvictWork {
   const float* scores;
   int keep_tail;
   int32_t* lens_out;
-  int32_t* count;         // [planes][batch]
-  int32_t *holes, *moved; // [planes][slots of the cache]
+  int32_t* count;         // [planes][batch] slots that move
+  int32_t *holes, *moved; // [planes][slots of the cache]: where they go and come from, a sequence's from its first slot's place on
+  uint32_t* hist;         // longer caches: [planes][batch][evict_hist_words()], ...
+  int32_t* tops;          //                [planes][shares], ...
+  uint32_t* counts;       //                [planes][shares][4]
 };
 hipError_t launch_cache_evict(const CacheTable& t, const CacheView& c, const EvictWork& w, int elem_bytes, hipStream_t st);
 

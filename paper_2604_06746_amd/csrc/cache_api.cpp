@@ -162,14 +162,26 @@ size_t most_attend_bytes(const structkv_cache* c, int H, int64_t new_tokens, int
 }
 
 struct EvictSpace {
-  size_t off_count, off_holes, off_moved, total_bytes;
+  size_t off_count, off_holes, off_moved, off_hist, off_tops, off_counts, total_bytes;
 };
-EvictSpace evict_space(const structkv_cache* c, int64_t slots) {
+EvictSpace evict_space(const structkv_cache* c) {
   EvictSpace e;
-  size_t off = 0;
-  e.off_count = off; off += align_up(sizeof(int32_t) * (size_t)c->planes * c->batch, 256);
-  e.off_holes = off; off += align_up(sizeof(int32_t) * (size_t)c->planes * (size_t)slots, 256);
-  e.off_moved = off; off += align_up(sizeof(int32_t) * (size_t)c->planes * (size_t)slots, 256);
+  size_t off = 0, shares = 0;
+  const size_t P = (size_t)c->planes, slots = (size_t)c->cu_slots[c->batch];
+  int64_t longest = 0;
+  for (int b = 0; b < c->batch; ++b) {
+    const int64_t cap = c->cu_slots[b + 1] - c->cu_slots[b];
+    longest = std::max(longest, cap);
+    shares += (size_t)evict_shares(cap);
+  }
+  auto take = [&](size_t words) { const size_t at = off; off += align_up(words * 4, 256); return at; };
+  e.off_count = take(P * c->batch);
+  e.off_holes = take(P * slots);
+  e.off_moved = take(P * slots);
+  const bool digits = longest > kEvictShort;
+  e.off_hist = take(digits ? P * c->batch * evict_hist_words() : 0);
+  e.off_tops = take(digits ? P * shares : 0);
+  e.off_counts = take(digits ? P * shares * 4 : 0);
   e.total_bytes = off;
   return e;
 }
@@ -196,7 +208,7 @@ size_t structkv_cache_workspace_bytes(const structkv_cache* cache, int32_t n_q_h
     fail(STRUCTKV_ERR_INVALID_ARG, "new_tokens (%lld) outside [0, STRUCTKV_MAX_DRAFTS x STRUCTKV_MAX_BATCH]", (long long)new_tokens);
     return 0;
   }
-  return std::max<size_t>(256, std::max(most_attend_bytes(cache, n_q_heads, new_tokens, v.slots), evict_space(cache, v.slots).total_bytes));
+  return std::max<size_t>(256, std::max(most_attend_bytes(cache, n_q_heads, new_tokens, v.slots), evict_space(cache).total_bytes));
 }
 
 structkv_status structkv_cache_append(const structkv_cache* cache, const void* k_new, const void* v_new,
@@ -316,11 +328,12 @@ structkv_status structkv_cache_evict(const structkv_cache* cache, const float* s
     if (std::min(cap - t.units[b], (int64_t)t.units[b]) * units >= ((int64_t)1 << 31) - 4096)
       return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows may move for one launch (rows*head_dim*element bytes/2 must stay below 2^31)");
   }
-  const EvictSpace e = evict_space(cache, v.slots);
+  const EvictSpace e = evict_space(cache);
   st = check_workspace(workspace, workspace_bytes, e.total_bytes);
   if (st != STRUCTKV_OK) return st;
   uint8_t* w8 = (uint8_t*)workspace;
-  const EvictWork w = {scores, keep_tail, lens_out, (int32_t*)(w8 + e.off_count), (int32_t*)(w8 + e.off_holes), (int32_t*)(w8 + e.off_moved)};
+  const EvictWork w = {scores, keep_tail, lens_out, (int32_t*)(w8 + e.off_count), (int32_t*)(w8 + e.off_holes), (int32_t*)(w8 + e.off_moved),
+                       (uint32_t*)(w8 + e.off_hist), (int32_t*)(w8 + e.off_tops), (uint32_t*)(w8 + e.off_counts)};
   SKV_HIP_CHECK(launch_cache_evict(t, v, w, elem_bytes(cache), (hipStream_t)stream));
   return STRUCTKV_OK;
 }

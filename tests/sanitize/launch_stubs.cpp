@@ -359,6 +359,8 @@ hipError_t launch_cache_accept(const CacheTable&, const CacheView&, const int32_
   ++g_launches;
   return hipSuccess;
 }
+int evict_shares(int64_t cap) { return (int)std::max<int64_t>(1, ceil_div(cap, std::max<int64_t>(1024, ceil_div(cap, 1024)))); }
+size_t evict_hist_words() { return 3 * 2048 + 8; }
 hipError_t launch_cache_evict(const CacheTable& t, const CacheView&, const EvictWork& w, int, hipStream_t) {
   ++g_launches;
   bool ok = w.count && w.holes && w.moved && w.lens_out;
