@@ -5,6 +5,7 @@ runs inside the library's HIP kernels.  cu_seqlens / k_per_seq / rows_per_seq ar
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -143,6 +144,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _host_i64(values: Sequence[int]):
     try:
+        if len(values) > 8:   # (65 offsets: 2.0 us against 4.0)
+            return (_i64 * len(values)).from_buffer(array.array("q", values))
         return (_i64 * len(values))(*values)
     except TypeError:   # (numbers of other kinds)
         return (_i64 * len(values))(*[int(v) for v in values])

@@ -11,6 +11,7 @@ struct CacheTab {
   int32_t cu_new[N + 1];  // fresh tokens (append, attend, accept)
   int32_t units[N + 1];   // cumulative workgroups (attend: x KV heads), or the budgets (evict)
   int32_t part[N + 1];    // attend: cumulative partial results (rows x chunks)
+  int32_t reach[N + 1];   // ... and stretches of slots whose weights a workgroup gathers
   int32_t batch;
 };
 using CacheTable = CacheTab<kMaxBatch>;
@@ -19,7 +20,7 @@ template <class F>
 void with_cache_table(const CacheTable& s, F f) {
   if (s.batch > 8) { f(s); return; }
   SmallCacheTable t;
-  for (int i = 0; i <= 8; ++i) { t.cu[i] = s.cu[i]; t.cu_new[i] = s.cu_new[i]; t.units[i] = s.units[i]; t.part[i] = s.part[i]; }
+  for (int i = 0; i <= 8; ++i) { t.cu[i] = s.cu[i]; t.cu_new[i] = s.cu_new[i]; t.units[i] = s.units[i]; t.part[i] = s.part[i]; t.reach[i] = s.reach[i]; }
   t.batch = s.batch;
   f(t);
 }

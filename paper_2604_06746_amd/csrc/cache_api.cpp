@@ -127,14 +127,14 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   for (int b = 0; b < c->batch; ++b)
     work += (double)ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, rows_wg) * c->n_kv_heads * (double)(t->cu[b + 1] - t->cu[b]);
   const int64_t each = std::max<int64_t>(kLeastChunk, (int64_t)std::ceil(work / kAttendBlocks));
-  int64_t units = 0, part = 0, stretches = 0;   // (of 256 slots, whose weights a workgroup of the join gathers)
+  int64_t units = 0, part = 0, stretches = 0;   // (of 64 slots, the fewest whose weights a workgroup of the join gathers)
   p->join = gather;
   for (int b = 0; b < c->batch; ++b) {
     const int64_t fresh = t->cu_new[b + 1] - t->cu_new[b], cap = t->cu[b + 1] - t->cu[b];
     const int64_t nc = std::max<int64_t>(1, ceil_div(cap, each));
     units += nc * ceil_div(fresh * gs, rows_wg);
     part += fresh * H * nc;
-    stretches += gather ? ceil_div(cap, 256) * c->planes : 0;
+    stretches += gather ? ceil_div(cap, 64) * c->planes : 0;
     if (units * c->n_kv_heads >= ((int64_t)1 << 31) || part + stretches >= ((int64_t)1 << 31))
       return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
     t->units[b + 1] = (int32_t)units;

@@ -36,6 +36,7 @@ __device__ __forceinline__ float wave_total(float x) {
 }
 typedef float __attribute__((ext_vector_type(2))) floatx2;
 
+constexpr int kSplitHeads = 16;   // from so many heads of a plane on, the waves share them
 constexpr int kAhead = 8;   // loads of a thread that are on their way at once
 
 // What joining a row needs to know; n: its slots.
@@ -46,7 +47,7 @@ struct Row {
 };
 template <class TAB>
 __device__ __forceinline__ Row row_of(const TAB& tab, const CacheView& c, const AttendWork& w, int64_t at, int rows_wg) {
-  const int r = (int)(at / w.H);
+  const int r = (int)((uint32_t)at / (uint32_t)w.H);   // (rows stay below 2^31)
   Row row;
   int b = 0;
   while (b + 1 < tab.batch && r >= tab.cu_new[b + 1]) ++b;
@@ -139,30 +140,25 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
     return;
   }
   // weights
-  int u = (int)blockIdx.x - row_blocks;
-  const int plane = u % c.planes;
-  u /= c.planes;
+  const int u = ((int)blockIdx.x - row_blocks) / c.planes, plane = ((int)blockIdx.x - row_blocks) % c.planes;
   int b = 0;
-  for (; b < tab.batch; ++b) {
-    const int blocks = (int)((tab.cu[b + 1] - tab.cu[b] + stretch - 1) / stretch);
-    if (u < blocks) break;
-    u -= blocks;
-  }
-  if (b >= tab.batch) return;
+  while (b + 1 < tab.batch && u >= tab.reach[b + 1]) ++b;
   const Held h = held(tab, c.lens, b);
-  const int s0 = u * stretch;
-  if (h.fresh != 1 || h.base < 0 || s0 >= h.n) return;
+  const int s0 = (u - tab.reach[b]) * stretch, s1 = min(s0 + stretch, h.n);
+  if (h.fresh != 1 || h.base < 0 || s0 >= s1) return;
   const int nc = (tab.units[b + 1] - tab.units[b]) / ((w.gs + rows_wg - 1) / rows_wg);
   const int len = chunk_slots(h.n, nc, w.min_chunk), live = (h.n + len - 1) / len;
   const int heads = w.H / c.planes;
   const float* x = w.x + plane * heads * w.xs + h.lo + 4 * b;
   float* mass = c.mass + plane * c.slots + h.lo;
-  int s = s0 + threadIdx.x;
-  const int s1 = min(s0 + stretch, h.n);
-  float ahead[kAhead], old = s < s1 ? mass[s] : 0.f;
+  // many heads: 64 slots at a time, a wave every fourth head of them; few: 256 slots at a time, all heads of a slot in its thread
+  const bool split = heads >= kSplitHeads;
+  const int first_head = split ? wave : 0, step = split ? 4 : 1, slots = split ? 64 : 256;
+  int s = s0 + (split ? lane : (int)threadIdx.x);
+  float ahead[kAhead], old = s < s1 && (!split || wave == 0) ? mass[s] : 0.f;
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) ahead[k] = s < s1 && k < heads ? x[k * w.xs + s] : -INFINITY;
-  for (int i0 = wave; i0 < heads; i0 += 4 * kAhead) {   // a lane a chunk, the wave's heads at once
+  for (int k = 0; k < kAhead; ++k) ahead[k] = s < s1 && first_head + k * step < heads ? x[(first_head + k * step) * w.xs + s] : -INFINITY;
+  for (int i0 = wave; i0 < heads; i0 += 4 * kAhead) {   // norms: a lane a chunk, the wave's heads at once
     floatx2 a[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -182,24 +178,31 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
     }
   }
   __syncthreads();
-  for (; s < s1; s += 256) {
+  for (int t0 = s0; t0 < s1; t0 += slots, s += slots) {
     float sum = 0.f;
-    for (int i0 = 0; i0 < heads; i0 += kAhead) {
+    for (int i0 = first_head; i0 < heads; i0 += kAhead * step) {
       float now[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) now[k] = ahead[k];
       // the next heads, or the first ones of the next slot
-      const bool same = i0 + kAhead < heads;
-      const int sn = same ? s : s + 256, in = same ? i0 + kAhead : 0;
+      const bool same = i0 + kAhead * step < heads;
+      const int sn = same ? s : s + slots, in = same ? i0 + kAhead * step : first_head;
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) ahead[k] = sn < s1 && in + k < heads ? x[(in + k) * w.xs + sn] : -INFINITY;
+      for (int k = 0; k < kAhead; ++k) ahead[k] = sn < s1 && in + k * step < heads ? x[(in + k * step) * w.xs + sn] : -INFINITY;
 #pragma unroll
       for (int k = 0; k < kAhead; ++k)
-        if (i0 + k < heads) sum += __builtin_amdgcn_exp2f(now[k] - norms[i0 + k]);
+        if (i0 + k * step < heads) sum += __builtin_amdgcn_exp2f(now[k] - norms[i0 + k * step]);
+    }
+    if (split) {   // (two halves of sh in turns: a wave is at most one barrier ahead)
+      float* part = sh + ((t0 - s0) / slots & 1) * 256;
+      part[threadIdx.x] = sum;
+      __syncthreads();
+      if (wave != 0) continue;
+      sum = (part[lane] + part[64 + lane]) + (part[128 + lane] + part[192 + lane]);
     }
     const float was = old;
-    old = s + 256 < s1 ? mass[s + 256] : 0.f;
-    mass[s] = fmaf(w.lambda, was, sum);
+    old = s + slots < s1 ? mass[s + slots] : 0.f;
+    if (s < s1) mass[s] = fmaf(w.lambda, was, sum);
   }
 }
 
@@ -211,16 +214,21 @@ hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const A
     constexpr int DP = decltype(dp)::value;
     constexpr bool FEW = decltype(few)::value;
     const int64_t row_blocks = FEW ? ceil_div(w.rows, 256 / (DP / 4)) : w.rows;
-    // slots of a workgroup: one a thread, four where that still leaves the chip four workgroups a CU
-    int64_t blocks = row_blocks, fine = 0;
-    int stretch = 256;
+    // slots of a workgroup: as many as it takes at a time, and more, up to eight times, where four workgroups a CU are left
+    CacheTable u = t;
+    int64_t blocks = row_blocks;
+    int stretch = w.H / c.planes >= kSplitHeads ? 64 : 256;
     if (p.gather) {
-      for (int b = 0; b < t.batch; ++b) fine += ceil_div(t.cu[b + 1] - t.cu[b], 256) * c.planes;
-      if (fine >= 4 * 1024) stretch = 1024;
-      for (int b = 0; b < t.batch; ++b) blocks += ceil_div(t.cu[b + 1] - t.cu[b], stretch) * c.planes;
+      int64_t all = 0;
+      for (int b = 0; b < t.batch; ++b) all += (t.cu[b + 1] - t.cu[b]) * c.planes;
+      const int most = stretch * 8;
+      while (stretch < most && all / (2 * stretch) >= 4 * 256) stretch *= 2;
+      u.reach[0] = 0;
+      for (int b = 0; b < t.batch; ++b) u.reach[b + 1] = u.reach[b] + (int32_t)ceil_div(t.cu[b + 1] - t.cu[b], stretch);
+      blocks += (int64_t)u.reach[t.batch] * c.planes;
     }
     const size_t lds = p.gather ? sizeof(float) * (w.H / c.planes) : 0;
-    with_cache_table(t, [&](const auto& tab) {
+    with_cache_table(u, [&](const auto& tab) {
       using TAB = std::decay_t<decltype(tab)>;
       const dim3 grid((unsigned)blocks);
       if (bf16) cache_combine_kernel<TAB, uint16_t, DP, FEW><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
