@@ -46,11 +46,13 @@ struct ScoreForm {
 // How an attend call is cut: a workgroup takes 16 rb query rows of one KV head and one of nc chunks of the sequence's slots
 // (nc: the table's units / row blocks).
 constexpr int kAttendWaves = 4;
+constexpr int kScorePad = 32;   // words behind a sequence's scores: tiles are stored whole
 struct AttendPlan {
   int mfma;               // 1: the bf16 matrix kernel (cache_attend_bf16.hip), 0: the fp32 one (cache_attend_f32.hip)
   int rb;                 // 16-row blocks of a workgroup
   int min_chunk;          // least slots of a chunk: a tile for every wave
   int gather;             // the weights are gathered: the first launch leaves the scores in the workspace
+  int stream;             // 1: the cache is read past the caches (see cache_attend_bf16.hip)
   int join;               // a second launch joins the chunks (and gathers); else the first one writes out and lse
   int64_t blocks;         // workgroups of the first launch
   int64_t most_chunks;    // of a sequence
@@ -66,7 +68,7 @@ struct AttendWork {
   int H, gs, min_chunk;
   float lambda;
   int64_t rows;           // new tokens x H
-  int64_t xs;             // scores: head h, slot s of sequence b at h xs + cu[b] + 4 b + s; 256 words behind the last head are nobody's
+  int64_t xs;             // scores: head h, slot s of sequence b at h xs + cu[b] + kScorePad b + s
 };
 
 // Slots of a chunk when n of them are cut into at most nc: whole tiles for every wave.

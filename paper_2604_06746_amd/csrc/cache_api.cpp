@@ -101,7 +101,7 @@ structkv_status check_scores(const structkv_cache* c, int32_t H, float scale, fl
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-size_t score_bytes(int H, int64_t slots, int batch) { return align_up(((size_t)H * (size_t)(slots + 4 * batch) + 256) * sizeof(float), 256); }
+size_t score_bytes(int H, int64_t slots, int batch) { return align_up((size_t)H * (size_t)(slots + kScorePad * batch) * sizeof(float), 256); }
 
 // what the bf16 matrix kernels take: whole 16-byte pieces, and a tile's rows within 32 bits
 bool mfma_fits(const structkv_cache* c, const void* q, int64_t qst, int64_t qsh) {
@@ -111,6 +111,7 @@ bool mfma_fits(const structkv_cache* c, const void* q, int64_t qst, int64_t qsh)
 }
 
 // Chunks: as many workgroups as fill the chip once or twice, but at least kLeastChunk slots each.
+constexpr int64_t kStreamBytes = (int64_t)128 << 20;
 constexpr int64_t kAttendBlocks = 512, kLeastChunk = 128;
 
 structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mfma, CacheTable* t, AttendPlan* p) {
@@ -123,6 +124,7 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   p->rb = !mfma || gather || most_rows <= 16 ? 1 : 2;
   p->min_chunk = kAttendWaves * (mfma ? 32 : 16);
   const int rows_wg = 16 * p->rb;
+  p->stream = mfma && most_rows <= rows_wg && t->cu[c->batch] * c->n_kv_heads * c->head_dim * 4 >= kStreamBytes;
   double work = 0;   // slots that the workgroups read in all
   for (int b = 0; b < c->batch; ++b)
     work += (double)ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, rows_wg) * c->n_kv_heads * (double)(t->cu[b + 1] - t->cu[b]);
@@ -155,7 +157,7 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
 // ... at most, however the tokens spread: a sequence's chunks are at most its share of kAttendBlocks / its row blocks and KV heads, and one
 // more; its rows per row block and KV head at most rows_wg
 size_t most_attend_bytes(const structkv_cache* c, int H, int64_t new_tokens, int64_t slots) {
-  const size_t rows_wg = 64;
+  const size_t rows_wg = 32;
   const size_t parts = rows_wg * (size_t)kAttendBlocks + (size_t)new_tokens * H;
   return align_up(parts * 2 * sizeof(float), 256) + align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256) +
          (c->mass ? score_bytes(H, slots, c->batch) : 0);
@@ -269,7 +271,7 @@ structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_h
   uint8_t* w8 = (uint8_t*)workspace;
   const AttendWork w = {q, q_stride_tok, q_stride_head, out, lse_out, (float*)(w8 + p.off_ml), (float*)(w8 + p.off_o),
                         p.gather ? (float*)(w8 + p.off_x) : nullptr, n_q_heads, n_q_heads / cache->n_kv_heads, p.min_chunk, lambda,
-                        (int64_t)t.cu_new[cache->batch] * n_q_heads, v.slots + 4 * cache->batch};
+                        (int64_t)t.cu_new[cache->batch] * n_q_heads, v.slots + kScorePad * cache->batch};
   if (p.mfma) SKV_HIP_CHECK(launch_cache_attend_bf16(t, v, f, p, w, (hipStream_t)stream));
   else SKV_HIP_CHECK(launch_cache_attend_f32(t, v, f, p, w, bf16, (hipStream_t)stream));
   if (p.join) SKV_HIP_CHECK(launch_cache_combine(t, v, p, w, bf16, (hipStream_t)stream));

@@ -10,6 +10,12 @@
 // them.  Tiles go from memory to LDS without registers (global_load_lds), each wave has room for one tile of its own and no barrier: as
 // soon as K's half has been used the next tile's K is requested into it, and likewise V, and the waves of a CU (eight at 128
 // components) fill each other's waits with about 100 KB on their way.
+// NT: tiles are fetched with the non-temporal policy, where no other workgroup reads them and the cache is larger than what the memory-side
+// cache keeps from one step to the next: 4 GB 715 -> 623 us (6.9 TB/s), 216 MB 81 -> 72 us.  The stores of the scores (128 bytes a
+// slot of 32 heads) are what gathering weights costs: 846 us with them and their reading, 696 where they stayed in a cache.
+// Rows beyond 32 of a KV head are other workgroups', which read the tiles again, from the XCD's L2.  Not kept: four waves of 32 rows on common
+// tiles with barriers (64 drafts over four times 16.5K slots 165 -> 164 us, over 2112 slots 20.6 -> 28.2), the second block's
+// weights under the first one's products (no change): two waves a SIMD issue every 5 cycles at best, 350 instructions a tile.
 // The rows' references M follow lazily: they are raised only when a score lies more than 2^8 above one of them, so that the usual tile has
 // no exchange between lanes and no rescaling.
 #include "cache_bf16.h"
@@ -42,7 +48,7 @@ typedef floatx4 __attribute__((aligned(4))) floatx4_at_4;
 
 constexpr float kSlack = 8.f;                    // how far above its reference a score may lie, log2
 
-template <class TAB, int D, int RB, int MODE, bool SAVE>
+template <class TAB, int D, int RB, int MODE, bool SAVE, bool NT>
 __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel(TAB tab, CacheView c, ScoreForm f, AttendWork w) {
   constexpr int KS = D / 32, DB = D / 16, SEGS = D / 8;   // steps of the first product, row blocks of the second, 16-byte pieces of a row
   constexpr int TILE = 32 * D * 2, NI = TILE / 1024;      // bytes of a tile of K or V, load instructions for it
@@ -71,7 +77,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
     for (int ks = 0; ks < KS; ++ks) qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qrow + ks * 32 + 8 * q4);
     mask[rb] = row_mask(f, r, t);
     slope[rb] = MODE == kBiased && f.slopes ? f.slopes[head] : 0.f;
-    if (SAVE) save = w.x + head * w.xs + h.lo + 4 * p.b;
+    if (SAVE) save = w.x + head * w.xs + h.lo + kScorePad * p.b;
   }
   const int n = h.base < 0 ? 0 : h.n;
   const int len = chunk_slots(n, p.nc, w.min_chunk);
@@ -97,14 +103,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
     const uint8_t* base = (const uint8_t*)(from + (int64_t)j0 * c.ss);
     if (j0 + 32 <= n) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(base + off[i]), (lds_ptr_t)(to + i * 1024), 16, 0, 0);
+      for (int i = 0; i < NI; ++i) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(base + off[i]), (lds_ptr_t)(to + i * 1024), 16, 0, NT ? 2 : 0);
     } else {
       const int last = n - 1 - j0;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int unit = i * 64 + lane, s = unit / SEGS;
         __builtin_amdgcn_global_load_lds((gbl_ptr_t)(base + (uint32_t)(min(s, last) * c.ss + ((unit % SEGS) ^ swz(s)) * 8) * 2u),
-                                         (lds_ptr_t)(to + i * 1024), 16, 0, 0);
+                                         (lds_ptr_t)(to + i * 1024), 16, 0, NT ? 2 : 0);
       }
     }
   };
@@ -214,13 +220,13 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
       }
     }
     if (SAVE) {
-      // Two stores from every wave, whatever the tile holds, so that the waits know how many there are: lanes without a
-      // row or a slot of the chunk write behind the scores, and the three after a sequence's last one are nobody's.
+      // Two stores from every wave, whatever the tile holds, so that the waits know how many there are: some lane has a row, and slots
+      // from the end on, up to a tile's, have room.
+      static_assert(!SAVE || RB == 1, "the stores that the waits count");
+      asm volatile("" ::: "memory");
+      if (row0 + l16 < rows) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const int s = j0 + kb * 16 + 4 * q4;
-        float* to = row0 + l16 < rows && s < s1 ? save + s : w.x + (int64_t)w.H * w.xs + lane * 4;
-        *reinterpret_cast<floatx4_at_4*>(to) = x[kb][0] * c2;
+        for (int kb = 0; kb < 2; ++kb) *reinterpret_cast<floatx4_at_4*>(save + j0 + kb * 16 + 4 * q4) = x[kb][0] * c2;
       }
       asm volatile("" ::: "memory");
     }
@@ -283,7 +289,10 @@ hipError_t attend(const CacheTable& t, const CacheView& c, const ScoreForm& f, c
     using TAB = std::decay_t<decltype(tab)>;
     const dim3 grid((unsigned)p.blocks), block(64 * kAttendWaves);
     auto go = [&](auto mode, auto save) {
-      cache_attend_bf16_kernel<TAB, D, RB, decltype(mode)::value, decltype(save)::value><<<grid, block, 0, st>>>(tab, c, f, w);
+      constexpr int MODE = decltype(mode)::value;
+      constexpr bool SAVE = decltype(save)::value;
+      if (p.stream) cache_attend_bf16_kernel<TAB, D, RB, MODE, SAVE, true><<<grid, block, 0, st>>>(tab, c, f, w);
+      else cache_attend_bf16_kernel<TAB, D, RB, MODE, SAVE, false><<<grid, block, 0, st>>>(tab, c, f, w);
     };
     auto by_mode = [&](auto save) { with_mode(f, [&](auto mode) { go(mode, save); }); };
     if constexpr (RB == 1) {

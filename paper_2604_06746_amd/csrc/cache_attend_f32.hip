@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
       const bool seen = s < s1 && sees(mask, min(s, n - 1), h.base);
       x[i] = more ? full_score(f, acc[i], slope, pos ? at - pos[min(s, n - 1)] : 0) : acc[i] * f.c2;
       if (!seen) x[i] = -INFINITY;
-      if (w.x && s < s1 && row0 + l16 < rows) w.x[head * w.xs + h.lo + 4 * p.b + s] = x[i];
+      if (w.x && s < s1 && row0 + l16 < rows) w.x[head * w.xs + h.lo + kScorePad * p.b + s] = x[i];
     }
     float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
     top = fmaxf(top, __shfl_xor(top, 16));

@@ -69,11 +69,11 @@ __device__ __forceinline__ void put_row(const AttendWork& w, int64_t at, int d, 
 
 // FEW: at most kFewChunks chunks a row, a lane group of DP / 4 a row; else a workgroup a row, its lane groups on shares of the chunks
 constexpr int kFewChunks = 8;
-template <class TAB, class T, int DP, bool FEW>
+template <class TAB, class T, int DP, bool FEW, int V>
 __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c, AttendWork w, int rows_wg, int row_blocks, int stretch) {
   short_kernel_priority();
   constexpr int LANES = DP / 4, PARTS = 256 / LANES;
-  __shared__ __attribute__((aligned(16))) float sh[256 * 4];
+  __shared__ __attribute__((aligned(16))) float sh[256 * (V > 1 ? 2 * V : 4)];
   __shared__ float zs[4];
   extern __shared__ float norms[];   // of a plane's heads
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
@@ -149,15 +149,19 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
   const int nc = (tab.units[b + 1] - tab.units[b]) / ((w.gs + rows_wg - 1) / rows_wg);
   const int len = chunk_slots(h.n, nc, w.min_chunk), live = (h.n + len - 1) / len;
   const int heads = w.H / c.planes;
-  const float* x = w.x + plane * heads * w.xs + h.lo + 4 * b;
+  const float* x = w.x + plane * heads * w.xs + h.lo + kScorePad * b;
   float* mass = c.mass + plane * c.slots + h.lo;
-  // many heads: 64 slots at a time, a wave every fourth head of them; few: 256 slots at a time, all heads of a slot in its thread
+  // V consecutive slots a thread.  Many heads: a wave's lanes' slots at a time, a wave every fourth head of them; few: the workgroup's threads'
+  // slots at a time, all heads of a slot in its thread.  (x has room behind a sequence's scores, mass does not.)
   const bool split = heads >= kSplitHeads;
-  const int first_head = split ? wave : 0, step = split ? 4 : 1, slots = split ? 64 : 256;
-  int s = s0 + (split ? lane : (int)threadIdx.x);
-  float ahead[kAhead], old = s < s1 && (!split || wave == 0) ? mass[s] : 0.f;
+  const int first_head = split ? wave : 0, step = split ? 4 : 1, slots = (split ? 64 : 256) * V;
+  int s = s0 + (split ? lane : (int)threadIdx.x) * V;
+  typedef float __attribute__((ext_vector_type(V), aligned(4))) some;
+  typedef float __attribute__((ext_vector_type(V))) held_some;
+  held_some ahead[kAhead];
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) ahead[k] = s < s1 && first_head + k * step < heads ? x[(first_head + k * step) * w.xs + s] : -INFINITY;
+  for (int k = 0; k < kAhead; ++k)
+    ahead[k] = s < s1 && first_head + k * step < heads ? (held_some)*reinterpret_cast<const some*>(x + (first_head + k * step) * w.xs + s) : (held_some)(-INFINITY);
   for (int i0 = wave; i0 < heads; i0 += 4 * kAhead) {   // norms: a lane a chunk, the wave's heads at once
     floatx2 a[kAhead];
 #pragma unroll
@@ -179,30 +183,43 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
   }
   __syncthreads();
   for (int t0 = s0; t0 < s1; t0 += slots, s += slots) {
-    float sum = 0.f;
+    const bool whole = s + V <= s1, writes = s < s1 && (!split || wave == 0);
+    held_some old = (held_some)(0.f);
+    if (writes && whole) old = *reinterpret_cast<const some*>(mass + s);
+    held_some sum = (held_some)(0.f);
     for (int i0 = first_head; i0 < heads; i0 += kAhead * step) {
-      float now[kAhead];
+      held_some now[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) now[k] = ahead[k];
-      // the next heads, or the first ones of the next slot
+      // the next heads, or the first ones of the next slots
       const bool same = i0 + kAhead * step < heads;
       const int sn = same ? s : s + slots, in = same ? i0 + kAhead * step : first_head;
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) ahead[k] = sn < s1 && in + k * step < heads ? x[(in + k * step) * w.xs + sn] : -INFINITY;
+      for (int k = 0; k < kAhead; ++k)
+        ahead[k] = sn < s1 && in + k * step < heads ? (held_some)*reinterpret_cast<const some*>(x + (in + k * step) * w.xs + sn) : (held_some)(-INFINITY);
 #pragma unroll
       for (int k = 0; k < kAhead; ++k)
-        if (i0 + k * step < heads) sum += __builtin_amdgcn_exp2f(now[k] - norms[i0 + k * step]);
+        if (i0 + k * step < heads) {
+          const float norm = norms[i0 + k * step];
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum[e] += __builtin_amdgcn_exp2f(now[k][e] - norm);
+        }
     }
     if (split) {   // (two halves of sh in turns: a wave is at most one barrier ahead)
-      float* part = sh + ((t0 - s0) / slots & 1) * 256;
-      part[threadIdx.x] = sum;
+      float* part = sh + ((t0 - s0) / slots & 1) * 256 * V;
+      *reinterpret_cast<held_some*>(part + threadIdx.x * V) = sum;
       __syncthreads();
       if (wave != 0) continue;
-      sum = (part[lane] + part[64 + lane]) + (part[128 + lane] + part[192 + lane]);
+      const held_some* parts = reinterpret_cast<const held_some*>(part);
+      sum = (parts[lane] + parts[64 + lane]) + (parts[128 + lane] + parts[192 + lane]);
     }
-    const float was = old;
-    old = s + slots < s1 ? mass[s + slots] : 0.f;
-    if (s < s1) mass[s] = fmaf(w.lambda, was, sum);
+    if (whole && writes) {
+      *reinterpret_cast<some*>(mass + s) = w.lambda * old + sum;
+    } else if (writes) {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (s + e < s1) mass[s + e] = w.lambda * mass[s + e] + sum[e];
+    }
   }
 }
 
@@ -210,19 +227,16 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
 
 hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const AttendPlan& p, const AttendWork& w, bool bf16,
                                 hipStream_t st) {
-  const auto launch = [&](auto dp, auto few) {
-    constexpr int DP = decltype(dp)::value;
+  const auto launch = [&](auto dp, auto few, auto some) {
+    constexpr int DP = decltype(dp)::value, V = decltype(some)::value;
     constexpr bool FEW = decltype(few)::value;
     const int64_t row_blocks = FEW ? ceil_div(w.rows, 256 / (DP / 4)) : w.rows;
-    // slots of a workgroup: as many as it takes at a time, and more, up to eight times, where four workgroups a CU are left
+    // slots of a workgroup: as many as it takes at a time, or twice that, where four workgroups a CU are left
     CacheTable u = t;
     int64_t blocks = row_blocks;
-    int stretch = w.H / c.planes >= kSplitHeads ? 64 : 256;
+    int stretch = (w.H / c.planes >= kSplitHeads ? 64 : 256) * V;
     if (p.gather) {
-      int64_t all = 0;
-      for (int b = 0; b < t.batch; ++b) all += (t.cu[b + 1] - t.cu[b]) * c.planes;
-      const int most = stretch * 8;
-      while (stretch < most && all / (2 * stretch) >= 4 * 256) stretch *= 2;
+      if (t.cu[t.batch] * c.planes / (2 * stretch) >= 4 * 256) stretch *= 2;
       u.reach[0] = 0;
       for (int b = 0; b < t.batch; ++b) u.reach[b + 1] = u.reach[b] + (int32_t)ceil_div(t.cu[b + 1] - t.cu[b], stretch);
       blocks += (int64_t)u.reach[t.batch] * c.planes;
@@ -231,12 +245,18 @@ hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const A
     with_cache_table(u, [&](const auto& tab) {
       using TAB = std::decay_t<decltype(tab)>;
       const dim3 grid((unsigned)blocks);
-      if (bf16) cache_combine_kernel<TAB, uint16_t, DP, FEW><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
-      else cache_combine_kernel<TAB, float, DP, FEW><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
+      if (bf16) cache_combine_kernel<TAB, uint16_t, DP, FEW, V><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
+      else cache_combine_kernel<TAB, float, DP, FEW, V><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
     });
     return hipGetLastError();
   };
-  const auto by_chunks = [&](auto dp) { return p.most_chunks <= kFewChunks ? launch(dp, std::true_type{}) : launch(dp, std::false_type{}); };
+  // four slots a thread where that leaves the weights two workgroups a CU
+  const int64_t slots = t.cu[t.batch] * c.planes;
+  const bool wide = p.gather && slots / (4 * (w.H / c.planes >= kSplitHeads ? 64 : 256)) >= 2 * 256;
+  const auto by_slots = [&](auto dp, auto few) {
+    return wide ? launch(dp, few, std::integral_constant<int, 4>{}) : launch(dp, few, std::integral_constant<int, 1>{});
+  };
+  const auto by_chunks = [&](auto dp) { return p.most_chunks <= kFewChunks ? by_slots(dp, std::true_type{}) : by_slots(dp, std::false_type{}); };
   if (c.d <= 64) return by_chunks(std::integral_constant<int, 64>{});
   if (c.d <= 128) return by_chunks(std::integral_constant<int, 128>{});
   return by_chunks(std::integral_constant<int, 256>{});
