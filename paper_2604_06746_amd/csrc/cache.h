@@ -66,6 +66,7 @@ struct AttendWork {
   float* lse;
   float *ml, *o, *x;      // partial results as the table numbers them, [.][2] and [.][padded head dim]; x NULL: no weights
   int H, gs, min_chunk;
+  uint32_t gs_recip;      // floor(2^32 / gs) + 1: divides a sequence's rows (below 2^18) exactly; 0: gs is 1
   float lambda;
   int64_t rows;           // new tokens x H
   int64_t xs;             // scores: head h, slot s of sequence b at h xs + cu[b] + kScorePad b + s
@@ -153,6 +154,9 @@ constexpr float kNothingSeen = -1.0e30f;   // the reference of a row that has se
 
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 
+// token of a sequence's row
+__device__ __forceinline__ int token_of(const AttendWork& w, int row) { return w.gs_recip ? (int)__umulhi((uint32_t)row, w.gs_recip) : row; }
+
 // What an attend kernel's workgroup leaves: the sums O (unnormalised), maxima M and normalisers Z of its chunk, log2 domain.
 // Every wave holds 16 x RB rows over its own slots, in the layout of a 16x16 matrix result of V^T P^T: lane l has row l % 16 of
 // each block and components 16 db + 4 (l / 16) .. +3; M is the same in a row's four lanes, Z each lane's own share.
@@ -209,7 +213,7 @@ __device__ __forceinline__ void finish_chunk(const floatx4 (&O)[DP / 16][RB], co
       z += ml[(i * ROWS + row) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(i * ROWS + row) * 2] - top);
       o += *reinterpret_cast<const floatx4*>(buf + (i * ROWS + row) * W + c);
     }
-    const int r = row0 + row, t = r / w.gs;
+    const int r = row0 + row, t = token_of(w, r);
     const int head = g * w.gs + (r - t * w.gs);
     const int64_t at = (int64_t)(new0 + t) * w.H + head;
     if (nc == 1 && !w.x) {
@@ -232,15 +236,17 @@ struct AttendPlace {
 template <class TAB>
 __device__ __forceinline__ AttendPlace attend_place(const TAB& t, int G, int gs, int rows_wg) {
   AttendPlace p;
-  p.g = blockIdx.x % G;
-  const int u = blockIdx.x / G;
+  const bool shifts = (G & (G - 1)) == 0;   // (a division costs some 40 instructions)
+  const int u = shifts ? (int)(blockIdx.x >> __builtin_ctz(G)) : (int)(blockIdx.x / G);
+  p.g = blockIdx.x - u * G;
   int b = 0;
   while (b + 1 < t.batch && u >= t.units[b + 1]) ++b;
   const int rcs = ((t.cu_new[b + 1] - t.cu_new[b]) * gs + rows_wg - 1) / rows_wg;
   p.b = b;
-  p.nc = (t.units[b + 1] - t.units[b]) / rcs;
-  p.chunk = (u - t.units[b]) / rcs;
-  p.rc = (u - t.units[b]) % rcs;
+  const int units = t.units[b + 1] - t.units[b], at = u - t.units[b];
+  p.nc = rcs == 1 ? units : units / rcs;
+  p.chunk = rcs == 1 ? at : at / rcs;
+  p.rc = at - p.chunk * rcs;
   return p;
 }
 #endif

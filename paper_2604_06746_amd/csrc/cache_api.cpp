@@ -99,6 +99,7 @@ structkv_status check_scores(const structkv_cache* c, int32_t H, float scale, fl
   return STRUCTKV_OK;
 }
 
+uint32_t reciprocal(int gs) { return gs > 1 ? (uint32_t)(((uint64_t)1 << 32) / gs) + 1u : 0u; }
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 size_t score_bytes(int H, int64_t slots, int batch) { return align_up((size_t)H * (size_t)(slots + kScorePad * batch) * sizeof(float), 256); }
@@ -236,8 +237,9 @@ structkv_status structkv_cache_append(const structkv_cache* cache, const void* k
       return fail(STRUCTKV_ERR_INVALID_ARG, "pos_new must be given where the cache keeps positions, and only there");
     if (mass_new && !cache->mass) return fail(STRUCTKV_ERR_INVALID_ARG, "mass_new given, but the cache keeps no mass");
     if (((uintptr_t)pos_new | (uintptr_t)mass_new) & 3) return fail(STRUCTKV_ERR_INVALID_ARG, "pos_new or mass_new is not 4-byte aligned");
-    if (total * cache->head_dim * (int64_t)e / 2 >= ((int64_t)1 << 31) - 4096 || total * cache->planes >= ((int64_t)1 << 31))
-      return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows for one launch (rows*head_dim*element bytes/2 must stay below 2^31)");
+    for (int b = 0; b < cache->batch; ++b)
+      if ((int64_t)(t.cu_new[b + 1] - t.cu_new[b]) * cache->n_kv_heads * cache->head_dim * (int64_t)e >= ((int64_t)1 << 32) - 4096)
+        return fail(STRUCTKV_ERR_UNSUPPORTED, "sequence %d: too many rows for one launch (rows*n_kv_heads*head_dim*element bytes must stay below 2^32)", b);
   }
   SKV_HIP_CHECK(launch_cache_append(t, v, k_new, v_new, new_stride_head, new_stride_tok, pos_new, mass_new, new_stride_plane, e,
                                     lens_out, (hipStream_t)stream));
@@ -269,8 +271,9 @@ structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_h
   if (st == STRUCTKV_OK) st = check_workspace(workspace, workspace_bytes, p.total_bytes);
   if (st != STRUCTKV_OK) return st;
   uint8_t* w8 = (uint8_t*)workspace;
+  const int gs = n_q_heads / cache->n_kv_heads;
   const AttendWork w = {q, q_stride_tok, q_stride_head, out, lse_out, (float*)(w8 + p.off_ml), (float*)(w8 + p.off_o),
-                        p.gather ? (float*)(w8 + p.off_x) : nullptr, n_q_heads, n_q_heads / cache->n_kv_heads, p.min_chunk, lambda,
+                        p.gather ? (float*)(w8 + p.off_x) : nullptr, n_q_heads, gs, p.min_chunk, reciprocal(gs), lambda,
                         (int64_t)t.cu_new[cache->batch] * n_q_heads, v.slots + kScorePad * cache->batch};
   if (p.mfma) SKV_HIP_CHECK(launch_cache_attend_bf16(t, v, f, p, w, (hipStream_t)stream));
   else SKV_HIP_CHECK(launch_cache_attend_f32(t, v, f, p, w, bf16, (hipStream_t)stream));
@@ -298,7 +301,7 @@ structkv_status structkv_cache_accept(const structkv_cache* cache, int32_t n_q_h
   if (weigh && (!q || !lse)) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda > 0 needs q and lse");
   if (weigh) {
     const AttendWork w = {q, q_stride_tok, q_stride_head, nullptr, const_cast<float*>(lse), nullptr, nullptr, nullptr, n_q_heads,
-                          n_q_heads / cache->n_kv_heads, 0, lambda, 0, 0};
+                          n_q_heads / cache->n_kv_heads, 0, reciprocal(n_q_heads / cache->n_kv_heads), lambda, 0, 0};
     if (mfma_fits(cache, q, q_stride_tok, q_stride_head)) SKV_HIP_CHECK(launch_cache_weights_bf16(t, v, f, w, path, n_accept, (hipStream_t)stream));
     else SKV_HIP_CHECK(launch_cache_weights_f32(t, v, f, w, path, n_accept, cache->dtype == STRUCTKV_DTYPE_BF16, (hipStream_t)stream));
   }

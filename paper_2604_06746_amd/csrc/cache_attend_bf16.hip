@@ -70,7 +70,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   float* save = nullptr;   // where this lane's scores go
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int row = min(row0 + rb * 16 + l16, rows - 1), t = row / w.gs, head = p.g * w.gs + row - t * w.gs;
+    const int row = min(row0 + rb * 16 + l16, rows - 1), t = token_of(w, row), head = p.g * w.gs + row - t * w.gs;
     const int64_t r = new0 + t;
     const uint16_t* qrow = (const uint16_t*)w.q + r * w.qst + (int64_t)head * w.qsh;
 #pragma unroll
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   if (mine > 0) { fetch_k(s0 + 32 * wave); fetch_v(s0 + 32 * wave); }
 
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) at[rb] = MODE == kBiased && pos && n > 0 ? pos[h.base + min(row0 + rb * 16 + l16, rows - 1) / w.gs] : 0;
+  for (int rb = 0; rb < RB; ++rb) at[rb] = MODE == kBiased && pos && n > 0 ? pos[h.base + token_of(w, min(row0 + rb * 16 + l16, rows - 1))] : 0;
   // (kept in registers from here on; pinned once all of them are on their way)
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)

@@ -64,12 +64,9 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l16 = lane & 15, q4 = lane >> 4;
   const AttendPlace p = attend_place(tab, c.G, w.gs, 16);
   const Held h = held(tab, c.lens, p.b);
-  const int n = h.base < 0 ? 0 : h.n;
-  const int len = chunk_slots(n, p.nc, w.min_chunk);
-  const int s0 = min((int64_t)n, (int64_t)p.chunk * len), s1 = min(n, s0 + len);
-  if (s0 >= s1 && (p.nc > 1 || w.x)) return;   // (the join reads no more chunks than have slots)
+  // the queries first: the length has no part in their addresses
   const int new0 = tab.cu_new[p.b], rows = h.fresh * w.gs, row0 = p.rc * 16;
-  const int row = min(row0 + l16, rows - 1), t = row / w.gs, head = p.g * w.gs + row - t * w.gs;
+  const int row = min(row0 + l16, rows - 1), t = token_of(w, row), head = p.g * w.gs + row - t * w.gs;
   const int64_t r = new0 + t;
   const T* qrow = (const T*)w.q + r * w.qst + (int64_t)head * w.qsh;
   floatx4 qf[DP / 16];
@@ -78,8 +75,11 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
   const uint64_t mask = row_mask(f, r, t);
   const bool more = f.softcap > 0.f || f.slopes;
   const float slope = f.slopes ? f.slopes[head] : 0.f;
+  const int n = h.base < 0 ? 0 : h.n;
+  const int len = chunk_slots(n, p.nc, w.min_chunk);
+  const int s0 = (int)min((int64_t)n, (int64_t)p.chunk * len), s1 = min(n, s0 + len);
+  if (s0 >= s1 && (p.nc > 1 || w.x)) return;   // (the join reads no more chunks than have slots)
   const int32_t* pos = f.slopes ? c.pos + (c.planes > 1 ? p.g * c.slots : 0) + h.lo : nullptr;
-  const int at = pos && n > 0 ? pos[h.base + t] : 0;
   const T* kg = (const T*)c.k + (int64_t)p.g * c.sh + h.lo * c.ss;
   const T* vg = (const T*)c.v + (int64_t)p.g * c.sh + h.lo * c.ss;
   float* kt = lds + wave * 2 * kTile * W;
@@ -91,7 +91,12 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
   for (int i = 0; i < DP / 16; ++i) O[i][0] = floatx4{0.f, 0.f, 0.f, 0.f};
 
   floatx4 kr[UNITS], vr[UNITS];
+  int from[4] = {};   // positions of the lane's slots
   auto fetch = [&](int j0) __attribute__((always_inline)) {
+    if (pos) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) from[i] = pos[min(j0 + 4 * q4 + i, n - 1)];
+    }
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int e = u * 64 + lane, s = min(j0 + e / (DP / 4), n - 1), col = e % (DP / 4) * 4;
@@ -101,6 +106,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
   };
   int j0 = s0 + wave * kTile;
   if (j0 < s1) fetch(j0);
+  const int at = pos && n > 0 ? pos[h.base + t] : 0;
   for (; j0 < s1; j0 += kAttendWaves * kTile) {
     wave_lds_fence();
 #pragma unroll
@@ -115,6 +121,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
       *reinterpret_cast<floatx4*>(vt + s * W + col) = v;
     }
     wave_lds_fence();
+    const int far[4] = {at - from[0], at - from[1], at - from[2], at - from[3]};
     if (j0 + kAttendWaves * kTile < s1) fetch(j0 + kAttendWaves * kTile);
     const floatx4 acc = tile_scores<DP>(kt, qf, l16, q4);
     float x[4];
@@ -122,7 +129,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
     for (int i = 0; i < 4; ++i) {
       const int s = j0 + 4 * q4 + i;
       const bool seen = s < s1 && sees(mask, min(s, n - 1), h.base);
-      x[i] = more ? full_score(f, acc[i], slope, pos ? at - pos[min(s, n - 1)] : 0) : acc[i] * f.c2;
+      x[i] = more ? full_score(f, acc[i], slope, far[i]) : acc[i] * f.c2;
       if (!seen) x[i] = -INFINITY;
       if (w.x && s < s1 && row0 + l16 < rows) w.x[head * w.xs + h.lo + kScorePad * p.b + s] = x[i];
     }
@@ -181,7 +188,7 @@ __global__ __launch_bounds__(256) void cache_weights_f32_kernel(TAB tab, CacheVi
     }
     wave_lds_fence();
     for (int row0 = 0; row0 < rows; row0 += 16) {
-      const int row = min(row0 + l16, rows - 1), i0 = row / w.gs, head = g * w.gs + row - i0 * w.gs;
+      const int row = min(row0 + l16, rows - 1), i0 = token_of(w, row), head = g * w.gs + row - i0 * w.gs;
       const int t = path ? max(0, min(path[new0 + i0], h.fresh - 1)) : i0;
       const int64_t r = new0 + t;
       const T* qrow = (const T*)w.q + r * w.qst + (int64_t)head * w.qsh;

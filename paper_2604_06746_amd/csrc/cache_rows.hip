@@ -2,50 +2,47 @@
 // Copies: bound by memory, or for the few rows of a decoding step by one launch and its chain of loads (length, row, store).
 #include "cache.h"
 
+#include <algorithm>
+
 namespace skv {
 namespace {
 
-// One thread per unit (16, 4 or 2 bytes) of a row, as in the row gather; the threads of a block of their own at the end take positions,
-// masses and lengths.  blockIdx.y: KV head, blockIdx.z: tensor.
-template <class TAB, class V>
+// One thread per unit (16, 4 or 2 bytes) of a row, as in the row gather.  blockIdx.y: sequence, so that its offsets are scalars (picked from the
+// table by each thread they cost a token of 64 sequences 2 us); its rows of all KV heads and both tensors lie one behind the other, so
+// that a single token still fills workgroups.  The first unit of a key's row, of a plane's first head, also brings position and mass.
+template <class TAB, class V, bool POW2>
 __global__ __launch_bounds__(256) void cache_append_kernel(TAB tab, CacheView c, const uint8_t* __restrict__ k_new,
                                                            const uint8_t* __restrict__ v_new, int64_t nsh, int64_t nst, int elem_bytes,
-                                                           uint32_t units_per_row, const int32_t* __restrict__ pos_new,
-                                                           const float* __restrict__ mass_new, int64_t nsp, unsigned row_blocks,
-                                                           int32_t* __restrict__ lens_out) {
+                                                           uint32_t units_per_row, uint32_t upr_shift, const int32_t* __restrict__ pos_new,
+                                                           const float* __restrict__ mass_new, int64_t nsp, int32_t* __restrict__ lens_out) {
   short_kernel_priority();
-  const int64_t total = tab.cu_new[tab.batch];
-  if (blockIdx.x < row_blocks) {
-    const uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r = (int64_t)(e / units_per_row);
-    if (r >= total) return;
-    const uint32_t u = (uint32_t)(e - (uint64_t)r * units_per_row);
-    int b = 0;
-    for (int i = 1; i < tab.batch; ++i) b += r >= tab.cu_new[i];
-    const int64_t g = blockIdx.y;
-    const uint8_t* src = (blockIdx.z ? v_new : k_new) + (g * nsh + r * nst) * elem_bytes + (int64_t)u * sizeof(V);
-    const V x = load_once<V>(src);   // (on its way while the length is)
-    const Held h = held(tab, c.lens, b);
-    if (h.lo + h.n + h.fresh > tab.cu[b + 1]) return;
-    const int64_t slot = h.lo + h.n + (r - tab.cu_new[b]);
-    *reinterpret_cast<V*>((uint8_t*)(blockIdx.z ? c.v : c.k) + (g * c.sh + slot * c.ss) * elem_bytes + (int64_t)u * sizeof(V)) = x;
-    return;
+  const int b = blockIdx.y;
+  const uint32_t fresh = (uint32_t)(tab.cu_new[b + 1] - tab.cu_new[b]);
+  const int64_t lo = tab.cu[b], cap = tab.cu[b + 1] - lo, first = tab.cu_new[b];
+  const uint32_t per = fresh * units_per_row, e = blockIdx.x * 256 + threadIdx.x;
+  uint32_t plane = 0, t = 0, u = 0;   // (tensor, head) pair, token, unit
+  bool mine = false;
+  V x;
+  if (fresh > 0) {
+    plane = e / per;
+    const uint32_t rest = e - plane * per;
+    t = POW2 ? rest >> upr_shift : rest / units_per_row;
+    u = rest - t * units_per_row;
+    mine = plane < 2u * (uint32_t)c.G;
   }
-  if (blockIdx.y | blockIdx.z) return;
-  const int64_t at = (int64_t)(blockIdx.x - row_blocks) * 256 + threadIdx.x;
-  if (at < tab.batch) {
-    const Held h = held(tab, c.lens, (int)at);
-    lens_out[at] = h.lo + h.n + h.fresh > tab.cu[at + 1] ? h.n : h.n + h.fresh;
+  const bool second = plane >= (uint32_t)c.G;
+  const int64_t g = second ? plane - c.G : plane;
+  if (mine) x = load_once<V>((second ? v_new : k_new) + (g * nsh + (first + t) * nst) * elem_bytes + (int64_t)u * sizeof(V));
+  const int n = max(0, (int)min((int64_t)c.lens[b], cap));   // (the row is on its way while the length is)
+  const bool fits = n + (int64_t)fresh <= cap;
+  if (blockIdx.x == 0 && threadIdx.x == 0) lens_out[b] = fits ? n + (int)fresh : n;
+  if (!mine || !fits) return;
+  const int64_t slot = lo + n + t;
+  *reinterpret_cast<V*>((uint8_t*)(second ? c.v : c.k) + (g * c.sh + slot * c.ss) * elem_bytes + (int64_t)u * sizeof(V)) = x;
+  if (u == 0 && plane < (uint32_t)c.planes) {
+    if (pos_new) c.pos[plane * c.slots + slot] = pos_new[plane * nsp + first + t];
+    if (c.mass) c.mass[plane * c.slots + slot] = mass_new ? mass_new[plane * nsp + first + t] : 0.f;
   }
-  if (at >= total * c.planes) return;
-  const int64_t p = at / total, r = at - p * total;
-  int b = 0;
-  for (int i = 1; i < tab.batch; ++i) b += r >= tab.cu_new[i];
-  const Held h = held(tab, c.lens, b);
-  if (h.lo + h.n + h.fresh > tab.cu[b + 1]) return;
-  const int64_t slot = p * c.slots + h.lo + h.n + (r - tab.cu_new[b]);
-  if (pos_new) c.pos[slot] = pos_new[p * nsp + r];
-  if (c.mass) c.mass[slot] = mass_new ? mass_new[p * nsp + r] : 0.f;
 }
 
 // The accepted rows of one KV head and tensor (blockIdx.y, .z), or a plane's positions and masses (the last blockIdx.z), of sequence
@@ -115,17 +112,21 @@ void with_unit(uintptr_t bits, F f) {
 hipError_t launch_cache_append(const CacheTable& t, const CacheView& c, const void* k_new, const void* v_new, int64_t nsh,
                                int64_t nst, const int32_t* pos_new, const float* mass_new, int64_t nsp, int elem_bytes,
                                int32_t* lens_out, hipStream_t st) {
-  const int64_t total = t.cu_new[t.batch];
+  int64_t most = 0;
+  for (int b = 0; b < t.batch; ++b) most = std::max<int64_t>(most, t.cu_new[b + 1] - t.cu_new[b]);
   const uintptr_t bits = (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)c.k | (uintptr_t)c.v |
                          (uintptr_t)((nsh | nst | c.sh | c.ss | c.d) * elem_bytes);
   with_cache_table(t, [&](const auto& tab) {
     with_unit(bits, [&](auto unit) {
       using V = decltype(unit);
-      const uint32_t upr = (uint32_t)(c.d * elem_bytes / (int)sizeof(V));
-      const unsigned row_blocks = (unsigned)ceil_div(total * upr, 256);
-      const unsigned rest = (unsigned)ceil_div(total * c.planes > t.batch ? total * c.planes : t.batch, 256);
-      cache_append_kernel<std::decay_t<decltype(tab)>, V><<<dim3(row_blocks + rest, (unsigned)c.G, 2), 256, 0, st>>>(
-          tab, c, (const uint8_t*)k_new, (const uint8_t*)v_new, nsh, nst, elem_bytes, upr, pos_new, mass_new, nsp, row_blocks, lens_out);
+      using TAB = std::decay_t<decltype(tab)>;
+      const uint32_t upr = (uint32_t)(c.d * elem_bytes / (int)sizeof(V)), shift = (uint32_t)__builtin_ctz(upr);
+      const dim3 grid((unsigned)std::max<int64_t>(1, ceil_div(most * 2 * c.G * upr, 256)), (unsigned)t.batch);
+      const uint8_t *k8 = (const uint8_t*)k_new, *v8 = (const uint8_t*)v_new;
+      if ((upr & (upr - 1)) == 0)
+        cache_append_kernel<TAB, V, true><<<grid, 256, 0, st>>>(tab, c, k8, v8, nsh, nst, elem_bytes, upr, shift, pos_new, mass_new, nsp, lens_out);
+      else
+        cache_append_kernel<TAB, V, false><<<grid, 256, 0, st>>>(tab, c, k8, v8, nsh, nst, elem_bytes, upr, shift, pos_new, mass_new, nsp, lens_out);
     });
   });
   return hipGetLastError();

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
       if (mine > 1) fetch(1);
       // what the rows need to be known by, a lane a row (one without a norm has weights of zero), then the rows as operands
       {
-        const int row = min(row0 + lane, rows - 1), i = row / w.gs, head = g * w.gs + row - i * w.gs;
+        const int row = min(row0 + lane, rows - 1), i = token_of(w, row), head = g * w.gs + row - i * w.gs;
         const int t = path ? max(0, min(path[new0 + i], h.fresh - 1)) : i;
         const float lse2 = w.lse[(int64_t)(new0 + t) * w.H + head] * 1.4426950408889634f;
         row_norm[lane] = row0 + lane < rows && lse2 > -INFINITY ? lse2 : INFINITY;
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
       bf16x8 qf[kRowBlocks][KS];
 #pragma unroll
       for (int rb = 0; rb < kRowBlocks; ++rb) {
-        const int row = min(row0 + rb * 16 + l16, rows - 1), i = row / w.gs;
+        const int row = min(row0 + rb * 16 + l16, rows - 1), i = token_of(w, row);
         const uint16_t* qrow = (const uint16_t*)w.q + (int64_t)(new0 + row_token[rb * 16 + l16]) * w.qst + (int64_t)(g * w.gs + row - i * w.gs) * w.qsh;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qrow + ks * 32 + 8 * q4);
