@@ -397,9 +397,9 @@ def _require(ok: bool, message: str) -> None:
         raise StructKVError(STRUCTKV_ERR_INVALID_ARG, message)
 
 
-def _vector(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, device, name: str) -> None:
-    if t is not None and (t.dtype != dtype or t.numel() != numel or t.device != device or not t.is_contiguous()):
-        raise StructKVError(STRUCTKV_ERR_INVALID_ARG, "%s must be a contiguous %s tensor of %d elements on %s" % (name, dtype, numel, device))
+def _vector(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, index: int, name: str) -> None:
+    if t is not None and (t.dtype is not dtype or t.numel() != numel or t.get_device() != index or not t.is_contiguous()):
+        raise StructKVError(STRUCTKV_ERR_INVALID_ARG, "%s must be a contiguous %s tensor of %d elements on the cache's GPU" % (name, dtype, numel))
 
 
 def make_cache(k: torch.Tensor, v: torch.Tensor, cu_slots: Sequence[int], lens: torch.Tensor, mass: Optional[torch.Tensor] = None,
@@ -420,39 +420,51 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, cu_slots: Sequence[int], lens: 
             _require(t.dim() in (1, 2), "%s must be [planes, slots] or [slots]" % name)
             planes = t.shape[0] if t.dim() == 2 else 1
             _require(planes in (1, G), "%s must have one plane, or one per KV head" % name)
-    _vector(mass, torch.float32, planes * total, k.device, "mass")
-    _vector(pos, torch.int32, planes * total, k.device, "pos")
-    _vector(lens, torch.int32, batch, k.device, "lens")
-    _require(v.device == k.device and k.device.type == "cuda", "the cache must be on one GPU")
+    index = k.get_device()
+    _vector(mass, torch.float32, planes * total, index, "mass")
+    _vector(pos, torch.int32, planes * total, index, "pos")
+    _vector(lens, torch.int32, batch, index, "lens")
+    _require(v.device == k.device and index >= 0, "the cache must be on one GPU")
     host = _host_i64(cu_slots)
     code = STRUCTKV_DTYPE_BF16 if k.dtype == torch.bfloat16 else STRUCTKV_DTYPE_F32
     c = structkv_cache(_ptr(k), _ptr(v), k.stride(0), k.stride(1), G, d, code, planes, _ptr(mass), _ptr(pos), _ptr(lens),
                        ctypes.addressof(host), batch)
     c.tensors = (k, v, lens, mass, pos, host)
-    c.tensor_dtype, c.device, c.slots = k.dtype, k.device, total
+    c.tensor_dtype, c.device, c.index, c.slots = k.dtype, k.device, index, total
     return c
+
+
+# (torch's own functions check more on every call: 1.2 us a call)
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _cache_call(fn, cache: structkv_cache, stream, *args) -> None:
     """The call on the cache's GPU: on `stream`, or on the current one of that GPU."""
-    index = cache.device.index
-    _require(getattr(stream, "device", cache.device) == cache.device, "the stream belongs to another device than the cache")
-    if index != torch.cuda.current_device():
-        with torch.cuda.device(index):
-            _check(fn(ctypes.byref(cache), *args, _stream(stream)))
+    index = cache.index
+    if stream is None:
+        raw = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
     else:
-        _check(fn(ctypes.byref(cache), *args, _stream(stream)))
+        _require(getattr(stream, "device", cache.device) == cache.device, "the stream belongs to another device than the cache")
+        raw = _stream(stream)
+    if index == _get_device():
+        status = fn(ctypes.byref(cache), *args, raw)
+    else:
+        with torch.cuda.device(index):
+            status = fn(ctypes.byref(cache), *args, raw)
+    if status:
+        _check(status)
 
 
 def _query_strides(cache: structkv_cache, n_q_heads: int, q: torch.Tensor, new: int):
-    _require(q.dim() == 3 and q.shape[0] == new and q.shape[1] == n_q_heads and q.shape[2] == cache.head_dim and
-             q.dtype == cache.tensor_dtype and q.device == cache.device and (q.stride(2) == 1 or cache.head_dim == 1),
-             "q must be [new tokens, n_q_heads, head_dim], of the cache's dtype and device, with contiguous components")
-    return q.stride(0), q.stride(1)
+    if q.shape != (new, n_q_heads, cache.head_dim) or q.dtype is not cache.tensor_dtype or q.get_device() != cache.index:
+        raise StructKVError(STRUCTKV_ERR_INVALID_ARG, "q must be [new tokens, n_q_heads, head_dim], of the cache's dtype and GPU")
+    st, sh, sc = q.stride()
+    _require(sc == 1 or cache.head_dim == 1, "q must have contiguous components")
+    return st, sh
 
 
 def _workspace(cache: structkv_cache, workspace: torch.Tensor) -> int:
-    _require(workspace.device == cache.device and workspace.is_contiguous(), "workspace must be contiguous and on the cache's device")
+    _require(workspace.get_device() == cache.index and workspace.is_contiguous(), "workspace must be contiguous and on the cache's GPU")
     return workspace.numel() * workspace.element_size()
 
 
@@ -466,20 +478,22 @@ def structkv_cache_append(cache: structkv_cache, k_new: torch.Tensor, v_new: tor
     """k_new, v_new: [G, new, d] views sharing strides; pos_new int32, mass_new fp32: [new] for all planes, or [planes, new]."""
     _require(len(cu_new) == cache.batch + 1, "cu_new needs batch + 1 entries")
     new = cu_new[cache.batch]
-    _require(k_new.dim() == 3 and k_new.shape[0] == cache.n_kv_heads and k_new.shape[1] >= new and k_new.shape[2] == cache.head_dim and
-             k_new.dtype == cache.tensor_dtype and k_new.device == cache.device and (k_new.stride(2) == 1 or cache.head_dim == 1) and
-             v_new.shape == k_new.shape and v_new.stride() == k_new.stride() and v_new.dtype == k_new.dtype and v_new.device == k_new.device,
-             "k_new and v_new must be [G, new tokens, head_dim] views sharing strides, of the cache's dtype and device")
+    shape, strides = k_new.shape, k_new.stride()
+    _require(len(shape) == 3 and shape[0] == cache.n_kv_heads and shape[1] >= new and shape[2] == cache.head_dim and v_new.shape == shape and
+             v_new.stride() == strides and (strides[2] == 1 or shape[2] == 1) and k_new.dtype is cache.tensor_dtype and
+             v_new.dtype is cache.tensor_dtype and k_new.get_device() == cache.index and v_new.get_device() == cache.index,
+             "k_new and v_new must be [G, new tokens, head_dim] views sharing strides, of the cache's dtype and GPU, with contiguous components")
     plane = 0
     for t, dtype, name in ((pos_new, torch.int32, "pos_new"), (mass_new, torch.float32, "mass_new")):
         if t is not None:
-            _require(t.shape in ((new,), (cache.planes, new)), "%s must be [new tokens] or [planes, new tokens]" % name)
-            _vector(t, dtype, t.numel(), cache.device, name)
-            plane = new if t.dim() == 2 else 0
+            rows = t.dim()
+            _vector(t, dtype, new if rows == 1 else new * cache.planes, cache.index, name)
+            _require(rows == 1 or t.shape == (cache.planes, new), "pos_new and mass_new must be [new tokens] or [planes, new tokens]")
+            plane = new if rows == 2 else 0
     _require(pos_new is None or mass_new is None or pos_new.dim() == mass_new.dim(), "pos_new and mass_new must have the same shape")
-    _vector(lens_out, torch.int32, cache.batch, cache.device, "lens_out")
-    _cache_call(_lib.structkv_cache_append, cache, stream, _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _host_i64(cu_new),
-                _ptr(pos_new), _ptr(mass_new), plane, _ptr(lens_out))
+    _vector(lens_out, torch.int32, cache.batch, cache.index, "lens_out")
+    _cache_call(_lib.structkv_cache_append, cache, stream, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], _host_i64(cu_new),
+                _ptr(pos_new), _ptr(mass_new), plane, lens_out.data_ptr())
 
 
 def structkv_cache_attend(cache: structkv_cache, n_q_heads: int, q: torch.Tensor, cu_new: Sequence[int], out: torch.Tensor,
@@ -490,12 +504,12 @@ def structkv_cache_attend(cache: structkv_cache, n_q_heads: int, q: torch.Tensor
     _require(len(cu_new) == cache.batch + 1, "cu_new needs batch + 1 entries")
     new = cu_new[cache.batch]
     st, sh = _query_strides(cache, n_q_heads, q, new)
-    _vector(out, cache.tensor_dtype, new * n_q_heads * cache.head_dim, cache.device, "out")
-    _vector(lse_out, torch.float32, new * n_q_heads, cache.device, "lse_out")
-    _vector(tree_mask, torch.int64, new, cache.device, "tree_mask")
-    _vector(slopes, torch.float32, n_q_heads, cache.device, "slopes")
-    _cache_call(_lib.structkv_cache_attend, cache, stream, n_q_heads, scale, softcap, _ptr(slopes), _ptr(q), st, sh, _host_i64(cu_new),
-                _ptr(tree_mask), lam, _ptr(out), _ptr(lse_out), _ptr(workspace), _workspace(cache, workspace))
+    _vector(out, cache.tensor_dtype, new * n_q_heads * cache.head_dim, cache.index, "out")
+    _vector(lse_out, torch.float32, new * n_q_heads, cache.index, "lse_out")
+    _vector(tree_mask, torch.int64, new, cache.index, "tree_mask")
+    _vector(slopes, torch.float32, n_q_heads, cache.index, "slopes")
+    _cache_call(_lib.structkv_cache_attend, cache, stream, n_q_heads, scale, softcap, _ptr(slopes), q.data_ptr(), st, sh, _host_i64(cu_new),
+                _ptr(tree_mask), lam, out.data_ptr(), lse_out.data_ptr(), workspace.data_ptr(), _workspace(cache, workspace))
 
 
 def structkv_cache_accept(cache: structkv_cache, n_q_heads: int, q: Optional[torch.Tensor], lse: Optional[torch.Tensor],
@@ -507,21 +521,21 @@ def structkv_cache_accept(cache: structkv_cache, n_q_heads: int, q: Optional[tor
     _require(len(cu_new) == cache.batch + 1, "cu_new needs batch + 1 entries")
     new = cu_new[cache.batch]
     st, sh = _query_strides(cache, n_q_heads, q, new) if q is not None else (0, 0)
-    _vector(lse, torch.float32, new * n_q_heads, cache.device, "lse")
-    _vector(tree_mask, torch.int64, new, cache.device, "tree_mask")
-    _vector(slopes, torch.float32, n_q_heads, cache.device, "slopes")
-    _vector(path, torch.int32, new, cache.device, "path")
-    _vector(n_accept, torch.int32, cache.batch, cache.device, "n_accept")
-    _vector(lens_out, torch.int32, cache.batch, cache.device, "lens_out")
+    _vector(lse, torch.float32, new * n_q_heads, cache.index, "lse")
+    _vector(tree_mask, torch.int64, new, cache.index, "tree_mask")
+    _vector(slopes, torch.float32, n_q_heads, cache.index, "slopes")
+    _vector(path, torch.int32, new, cache.index, "path")
+    _vector(n_accept, torch.int32, cache.batch, cache.index, "n_accept")
+    _vector(lens_out, torch.int32, cache.batch, cache.index, "lens_out")
     _cache_call(_lib.structkv_cache_accept, cache, stream, n_q_heads, scale, softcap, _ptr(slopes), _ptr(q), st, sh, _ptr(lse),
-                _host_i64(cu_new), _ptr(tree_mask), _ptr(path), _ptr(n_accept), lam, _ptr(lens_out))
+                _host_i64(cu_new), _ptr(tree_mask), _ptr(path), _ptr(n_accept), lam, lens_out.data_ptr())
 
 
 def structkv_cache_evict(cache: structkv_cache, scores: Optional[torch.Tensor], budget: Sequence[int], keep_tail: int,
                          lens_out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """scores: fp32 [planes, slots], or None for the cache's mass."""
     _require(len(budget) == cache.batch, "budget needs batch entries")
-    _vector(scores, torch.float32, cache.planes * cache.slots, cache.device, "scores")
-    _vector(lens_out, torch.int32, cache.batch, cache.device, "lens_out")
-    _cache_call(_lib.structkv_cache_evict, cache, stream, _ptr(scores), _host_i64(budget), keep_tail, _ptr(lens_out), _ptr(workspace),
+    _vector(scores, torch.float32, cache.planes * cache.slots, cache.index, "scores")
+    _vector(lens_out, torch.int32, cache.batch, cache.index, "lens_out")
+    _cache_call(_lib.structkv_cache_evict, cache, stream, _ptr(scores), _host_i64(budget), keep_tail, lens_out.data_ptr(), workspace.data_ptr(),
                 _workspace(cache, workspace))

@@ -25,6 +25,25 @@ void with_cache_table(const CacheTable& s, F f) {
   f(t);
 }
 
+// ... of which the copies need less than half.
+template <int N>
+struct RowTab {
+  int64_t cu[N + 1];
+  int32_t cu_new[N + 1];
+  int32_t batch;
+};
+template <int N>
+RowTab<N> row_table(const CacheTable& s) {
+  RowTab<N> t;
+  for (int i = 0; i <= N; ++i) { t.cu[i] = s.cu[i]; t.cu_new[i] = s.cu_new[i]; }
+  t.batch = s.batch;
+  return t;
+}
+template <class F>
+void with_row_table(const CacheTable& s, F f) {
+  if (s.batch > 8) f(row_table<kMaxBatch>(s)); else f(row_table<8>(s));
+}
+
 // The cache as kernels see it.
 struct CacheView {
   void *k, *v;

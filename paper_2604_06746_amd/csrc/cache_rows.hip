@@ -116,7 +116,7 @@ hipError_t launch_cache_append(const CacheTable& t, const CacheView& c, const vo
   for (int b = 0; b < t.batch; ++b) most = std::max<int64_t>(most, t.cu_new[b + 1] - t.cu_new[b]);
   const uintptr_t bits = (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)c.k | (uintptr_t)c.v |
                          (uintptr_t)((nsh | nst | c.sh | c.ss | c.d) * elem_bytes);
-  with_cache_table(t, [&](const auto& tab) {
+  with_row_table(t, [&](const auto& tab) {
     with_unit(bits, [&](auto unit) {
       using V = decltype(unit);
       using TAB = std::decay_t<decltype(tab)>;
@@ -135,7 +135,7 @@ hipError_t launch_cache_append(const CacheTable& t, const CacheView& c, const vo
 hipError_t launch_cache_accept(const CacheTable& t, const CacheView& c, const int32_t* path, const int32_t* n_accept,
                                int elem_bytes, int32_t* lens_out, hipStream_t st) {
   const uintptr_t bits = (uintptr_t)c.k | (uintptr_t)c.v | (uintptr_t)((c.sh | c.ss | c.d) * elem_bytes);
-  with_cache_table(t, [&](const auto& tab) {
+  with_row_table(t, [&](const auto& tab) {
     with_unit(bits, [&](auto unit) {
       using V = decltype(unit);
       cache_accept_kernel<std::decay_t<decltype(tab)>, V><<<dim3((unsigned)t.batch, (unsigned)c.G, 3), 256, 0, st>>>(
