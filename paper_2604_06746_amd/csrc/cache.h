@@ -62,6 +62,9 @@ struct ScoreForm {
   const uint64_t* tree;
 };
 
+// What a call reads at least of the cache to read it past the caches (half of what the memory-side cache holds).
+constexpr int64_t kStreamBytes = (int64_t)128 << 20;
+
 // How an attend call is cut: a workgroup takes 16 rb query rows of one KV head and one of nc chunks of the sequence's slots
 // (nc: the table's units / row blocks).
 constexpr int kAttendWaves = 4;

@@ -112,7 +112,6 @@ bool mfma_fits(const structkv_cache* c, const void* q, int64_t qst, int64_t qsh)
 }
 
 // Chunks: as many workgroups as fill the chip once or twice, but at least kLeastChunk slots each.
-constexpr int64_t kStreamBytes = (int64_t)128 << 20;
 constexpr int64_t kAttendBlocks = 512, kLeastChunk = 128;
 
 structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mfma, CacheTable* t, AttendPlan* p) {

@@ -15,7 +15,7 @@ namespace {
 constexpr int kRowBlocks = 4;   // 16-row blocks held at a time: a row a lane
 constexpr int kRowBytes = 64 * (8 + 4 * 4);   // what a wave knows of them
 
-template <class TAB, int D, int MODE>
+template <class TAB, int D, int MODE, bool NT>
 __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, CacheView c, ScoreForm f, AttendWork w,
                                                                     const int32_t* __restrict__ path,
                                                                     const int32_t* __restrict__ n_accept, int stretch, int head_waves) {
@@ -28,10 +28,13 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
   int b = 0;
   while (b + 1 < tab.batch && (int)blockIdx.x >= tab.units[b + 1]) ++b;
   const Held h = held(tab, c.lens, b);
+  // the path, a token a lane, and its length are on their way while the sequence's is
+  const int new0 = tab.cu_new[b], accepted = n_accept ? n_accept[b] : 0;
+  const int step = path && lane < h.fresh ? max(0, min(path[new0 + lane], h.fresh - 1)) : lane;
   const int n = h.n, s0 = ((int)blockIdx.x - tab.units[b]) * stretch, s1 = min(n, s0 + stretch);
   if (h.fresh == 0 || h.base < 0 || s0 >= n) return;
-  const int new0 = tab.cu_new[b], plane = blockIdx.y;
-  const int taken = n_accept ? max(0, min(n_accept[b], h.fresh)) : h.fresh, rows = taken * w.gs;
+  const int plane = blockIdx.y;
+  const int taken = n_accept ? max(0, min(accepted, h.fresh)) : h.fresh, rows = taken * w.gs;
   uint8_t* ring = lds + wave * 2 * SLOT;
   uint8_t* about = lds + 4 * 2 * SLOT + wave * kRowBytes;
   uint64_t* row_sees = reinterpret_cast<uint64_t*>(about);
@@ -63,14 +66,14 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
       const uint8_t* base = (const uint8_t*)(kg + (int64_t)j0 * c.ss);
       if (j0 + 32 <= n) {
 #pragma unroll
-        for (int k = 0; k < NI; ++k) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(base + off[k]), (lds_ptr_t)(to + k * 1024), 16, 0, 0);
+        for (int k = 0; k < NI; ++k) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(base + off[k]), (lds_ptr_t)(to + k * 1024), 16, 0, NT ? 2 : 0);
       } else {   // rows past the end re-read the last one (their sums are not kept)
         const int last = n - 1 - j0;
 #pragma unroll
         for (int k = 0; k < NI; ++k) {
           const int unit = k * 64 + lane, s = unit / SEGS;
           __builtin_amdgcn_global_load_lds((gbl_ptr_t)(base + (uint32_t)(min(s, last) * c.ss + ((unit % SEGS) ^ swizzle_k<SEGS>(s)) * 8) * 2u),
-                                           (lds_ptr_t)(to + k * 1024), 16, 0, 0);
+                                           (lds_ptr_t)(to + k * 1024), 16, 0, NT ? 2 : 0);
         }
       }
       if (POS) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(pos ? pos + min(j0 + (lane & 31), n - 1) : c.lens), (lds_ptr_t)(to + TILE), 4, 0, 0);
@@ -82,7 +85,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
       // what the rows need to be known by, a lane a row (one without a norm has weights of zero), then the rows as operands
       {
         const int row = min(row0 + lane, rows - 1), i = token_of(w, row), head = g * w.gs + row - i * w.gs;
-        const int t = path ? max(0, min(path[new0 + i], h.fresh - 1)) : i;
+        const int t = __shfl(step, i);
         const float lse2 = w.lse[(int64_t)(new0 + t) * w.H + head] * 1.4426950408889634f;
         row_norm[lane] = row0 + lane < rows && lse2 > -INFINITY ? lse2 : INFINITY;
         if (MODE == kBiased) {
@@ -182,6 +185,7 @@ hipError_t weights(const CacheTable& t, const CacheView& c, const ScoreForm& f, 
   for (int b = 0; b < t.batch; ++b) all += t.cu[b + 1] - t.cu[b];
   const int least = 32 * (4 / head_waves);
   int stretch = (int)std::max<int64_t>(least, std::min<int64_t>(512, all * c.planes / 512 / 32 * 32));
+  const bool stream = all * c.G * D * 2 >= kStreamBytes;
   CacheTable u = t;
   u.units[0] = 0;
   for (int b = 0; b < t.batch; ++b) u.units[b + 1] = u.units[b] + (int32_t)ceil_div(t.cu[b + 1] - t.cu[b], stretch);
@@ -190,8 +194,10 @@ hipError_t weights(const CacheTable& t, const CacheView& c, const ScoreForm& f, 
     with_mode(f, [&](auto mode) {
       constexpr int MODE = decltype(mode)::value;
       const size_t lds = 4 * (2 * (32 * D * 2 + (MODE == kBiased ? 256 : 0)) + kRowBytes + sizeof(float) * stretch);   // 80 KB at most
-      cache_weights_bf16_kernel<std::decay_t<decltype(tab)>, D, MODE><<<dim3((unsigned)u.units[t.batch], (unsigned)c.planes), 256, lds, st>>>(
-          tab, c, f, w, path, n_accept, stretch, head_waves);
+      using TAB = std::decay_t<decltype(tab)>;
+      const dim3 grid((unsigned)u.units[t.batch], (unsigned)c.planes);
+      if (stream) cache_weights_bf16_kernel<TAB, D, MODE, true><<<grid, 256, lds, st>>>(tab, c, f, w, path, n_accept, stretch, head_waves);
+      else cache_weights_bf16_kernel<TAB, D, MODE, false><<<grid, 256, lds, st>>>(tab, c, f, w, path, n_accept, stretch, head_waves);
     });
   });
   return hipGetLastError();
