@@ -508,7 +508,8 @@ hipError_t launch_cache_evict(const CacheTable& t, const CacheView& c, const Evi
   }
   with_cache_table(u, [&](const auto& tab) {
     using TAB = std::decay_t<decltype(tab)>;
-    if (longest <= 4096) launch_short<512, 8>(tab, c, w, elem_bytes, fused, st);
+    if (longest <= 4096) launch_short<1024, 4>(tab, c, w, elem_bytes, fused, st);   // (2081 slots 6.4 us; 512 threads 6.8, 256 9.4)
+    else if (longest <= 8192) launch_short<1024, 8>(tab, c, w, elem_bytes, fused, st);
     else if (longest <= 16384) launch_short<1024, 16>(tab, c, w, elem_bytes, fused, st);
     else if (longest <= kEvictShort) launch_short<1024, 32>(tab, c, w, elem_bytes, fused, st);
     else {
