@@ -124,7 +124,7 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   p->rb = !mfma || gather || most_rows <= 16 ? 1 : 2;
   p->min_chunk = kAttendWaves * (mfma ? 32 : 16);
   const int rows_wg = 16 * p->rb;
-  p->stream = mfma && most_rows <= rows_wg && t->cu[c->batch] * c->n_kv_heads * c->head_dim * 4 >= kStreamBytes;
+  p->stream = most_rows <= rows_wg && t->cu[c->batch] * c->n_kv_heads * c->head_dim * 2 * elem_bytes(c) >= kStreamBytes;
   double work = 0;   // slots that the workgroups read in all
   for (int b = 0; b < c->batch; ++b)
     work += (double)ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, rows_wg) * c->n_kv_heads * (double)(t->cu[b + 1] - t->cu[b]);

@@ -17,13 +17,14 @@ template <> __device__ __forceinline__ float widen<float>(float x) { return x; }
 template <> __device__ __forceinline__ float widen<uint16_t>(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
 // components c .. c+3 of a row; zeros from component d on.  VEC: the row is aligned to four elements and d a multiple of them
-template <class T, bool VEC>
+template <class T, bool VEC, bool NT = false>
 __device__ __forceinline__ floatx4 load4(const T* row, int c, int d) {
   floatx4 r = {0.f, 0.f, 0.f, 0.f};
   if (VEC) {
     if (c < d) {
       typedef __attribute__((ext_vector_type(4))) T vec;
-      const vec x = *reinterpret_cast<const vec*>(row + c);
+      const vec* at = reinterpret_cast<const vec*>(row + c);
+      const vec x = NT ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
       for (int i = 0; i < 4; ++i) r[i] = widen<T>(x[i]);
     }
@@ -59,7 +60,7 @@ __device__ __forceinline__ floatx4 tile_scores(const float* kt, const floatx4 (&
   return (acc[0] + acc[1]) + (acc[2] + acc[3]);
 }
 
-template <class TAB, class T, int DP, bool VEC>
+template <class TAB, class T, int DP, bool VEC, bool NT>
 __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB tab, CacheView c, ScoreForm f, AttendWork w) {
   constexpr int W = DP + 4, UNITS = kTile * DP / 4 / 64;   // float4 units of a tile per lane
   constexpr int RING = kAttendWaves * 2 * kTile * W, FIN = kFinishFloats<DP, 1>;
@@ -103,8 +104,8 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int e = u * 64 + lane, s = min(j0 + e / (DP / 4), n - 1), col = e % (DP / 4) * 4;
-      kr[u] = load4<T, VEC>(kg + (int64_t)s * c.ss, col, c.d);
-      vr[u] = load4<T, VEC>(vg + (int64_t)s * c.ss, col, c.d);
+      kr[u] = load4<T, VEC, NT>(kg + (int64_t)s * c.ss, col, c.d);
+      vr[u] = load4<T, VEC, NT>(vg + (int64_t)s * c.ss, col, c.d);
     }
   };
   int j0 = s0 + wave * kTile;
@@ -245,8 +246,12 @@ hipError_t dispatch(const CacheTable& t, const CacheView& c, const AttendWork& w
 template <class T>
 hipError_t attend(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p, const AttendWork& w, hipStream_t st) {
   return dispatch<T>(t, c, w, [&](const auto& tab, auto dp, auto vec) {
-    cache_attend_f32_kernel<std::decay_t<decltype(tab)>, T, decltype(dp)::value, decltype(vec)::value>
-        <<<dim3((unsigned)p.blocks), 64 * kAttendWaves, 0, st>>>(tab, c, f, w);
+    using TAB = std::decay_t<decltype(tab)>;
+    constexpr int DP = decltype(dp)::value;
+    constexpr bool VEC = decltype(vec)::value;
+    const dim3 grid((unsigned)p.blocks);
+    if (VEC && p.stream) cache_attend_f32_kernel<TAB, T, DP, VEC, VEC><<<grid, 64 * kAttendWaves, 0, st>>>(tab, c, f, w);
+    else cache_attend_f32_kernel<TAB, T, DP, VEC, false><<<grid, 64 * kAttendWaves, 0, st>>>(tab, c, f, w);
   });
 }
 template <class T>
