@@ -470,3 +470,58 @@ def test_another_stream(B):
     for i in (1, 2):
         assert torch.equal(outs[0][0], outs[i][0]) and torch.equal(outs[0][1], outs[i][1]) and torch.equal(sides[0].mass, sides[i].mass)
         assert torch.equal(sides[0].k.nan_to_num(), sides[i].k.nan_to_num())
+
+
+def test_layer_cache_after_a_sweep(B):
+    """LayerCache behind LayerSweep: a ragged batch's compact caches, then tokens, drafts and evictions, beside the calls themselves."""
+    from paper_2604_06746_amd.cache import LayerCache
+    from paper_2604_06746_amd.sweep import LayerSweep
+    H, G, d, w, lens, keep, dtype = 8, 2, 128, 8, [300, 450], [60, 90], torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(91)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    sw = LayerSweep(H, G, d, w, dtype, lens, keep)
+    sw.layer(normal(2, H, w, d), normal(G, sum(lens), d), normal(G, sum(lens), d))
+    rows = [k + w for k in keep]
+    cu_rows = R.cut(rows)
+    cache = LayerCache(H, G, d, dtype, [n + 30 for n in rows])
+    first = torch.repeat_interleave(torch.tensor([0, lens[0]], device="cuda"), torch.tensor(rows, device="cuda"))
+    idx = sw.idx_kv[:sum(rows)]
+    cache.append(sw.k_cache[0][:, :sum(rows)], sw.v_cache[0][:, :sum(rows)], cu_rows, idx, sw.indeg[first + idx])
+    assert cache.lens.tolist() == rows
+    c = R.make_cache(G, d, 1, [n + 30 for n in rows], rows, dtype, 92)
+
+    def state():
+        torch.cuda.synchronize()
+        c.k, c.v, c.mass, c.pos, c.lens = cache.k.cpu(), cache.v.cpu(), cache.mass.cpu(), cache.pos.cpu(), cache.lens.tolist()
+        return c
+    for step, T in enumerate((1, 7, 1)):
+        rng, cu_new = np.random.default_rng(step), R.cut([T, T])
+        masks = R.random_tree(T, rng) + R.random_tree(T, rng)
+        tree, q = R.as_int64(masks).cuda(), normal(2 * T, H, d)
+        cache.append(normal(G, 2 * T, d), normal(G, 2 * T, d), cu_new, torch.arange(2 * T, device="cuda").int() + 1000 + 10 * step)
+        before = state()
+        lam = 0.9 if T == 1 else 0.0
+        out, lse = cache.attend(q, cu_new, tree, lam)
+        ref, ref_lse, mass, size = R.attend(before, H, q.cpu(), cu_new, masks, lam=lam)
+        within(out.cpu().double(), ref, EPS[dtype] * ref.abs() + 1e-4 * size, "out")
+        within(lse.cpu().double(), ref_lse, torch.tensor(1e-4), "lse")
+        within(cache.mass.cpu().double(), mass, 1e-4 * mass.abs(), "mass")
+        if T > 1:
+            n_accept = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+            path = torch.zeros(2 * T, dtype=torch.int32, device="cuda")
+            path[1], path[T] = T - 1, 3
+            before = state()
+            cache.accept(cu_new, path, n_accept, q, lse, tree, 0.9)
+            *_, mass, new_lens = R.accept(before, H, q.cpu(), lse.cpu(), cu_new, path.cpu(), [2, 1], masks, lam=0.9)
+            assert cache.lens.tolist() == new_lens
+            within(cache.mass.cpu().double(), mass, 1e-4 * mass.abs(), "mass")
+    before = state()
+    cache.evict([40, 50], w)
+    k, v, pos, mass, new_lens = R.evict(before, before.mass, [40, 50], w)
+    after = state()
+    assert after.lens == new_lens == [40, 50] and torch.equal(after.pos, pos) and torch.equal(after.mass, mass)
+    for b in range(2):
+        used = slice(c.cu[b], c.cu[b] + new_lens[b])
+        assert torch.equal(after.k[:, used], k[:, used]) and torch.equal(after.v[:, used], v[:, used])
+    with pytest.raises(B.StructKVError):
+        LayerCache(7, 2, 64, dtype, [10])
