@@ -9,9 +9,8 @@ template <int N>
 struct CacheTab {
   int64_t cu[N + 1];      // first slots (capacities)
   int32_t cu_new[N + 1];  // fresh tokens (append, attend, accept)
-  int32_t units[N + 1];   // cumulative workgroups (attend: x KV heads), or the budgets (evict)
-  int32_t part[N + 1];    // attend: cumulative partial results (rows x chunks)
-  int32_t reach[N + 1];   // ... and stretches of slots whose weights a workgroup gathers
+  int32_t units[N + 1];   // cumulative blocks of query rows (attend) or workgroups (weights), or the budgets (evict)
+  int32_t reach[N + 1];   // attend: cumulative stretches of slots whose weights a workgroup gathers
   int32_t batch;
 };
 using CacheTable = CacheTab<kMaxBatch>;
@@ -20,7 +19,7 @@ template <class F>
 void with_cache_table(const CacheTable& s, F f) {
   if (s.batch > 8) { f(s); return; }
   SmallCacheTable t;
-  for (int i = 0; i <= 8; ++i) { t.cu[i] = s.cu[i]; t.cu_new[i] = s.cu_new[i]; t.units[i] = s.units[i]; t.part[i] = s.part[i]; t.reach[i] = s.reach[i]; }
+  for (int i = 0; i <= 8; ++i) { t.cu[i] = s.cu[i]; t.cu_new[i] = s.cu_new[i]; t.units[i] = s.units[i]; t.reach[i] = s.reach[i]; }
   t.batch = s.batch;
   f(t);
 }
@@ -65,20 +64,20 @@ struct ScoreForm {
 // What a call reads at least of the cache to read it past the caches (half of what the memory-side cache holds).
 constexpr int64_t kStreamBytes = (int64_t)128 << 20;
 
-// How an attend call is cut: a workgroup takes 16 rb query rows of one KV head and one of nc chunks of the sequence's slots
-// (nc: the table's units / row blocks).
+// How an attend call is cut: a workgroup takes `rows` query rows of one KV head and a chunk of a sequence's slots; `units` of them per KV head are
+// shared out by the lengths on the device (Cuts).
 constexpr int kAttendWaves = 4;
 constexpr int kScorePad = 32;   // words behind a sequence's scores: tiles are stored whole
 struct AttendPlan {
-  int mfma;               // 1: the bf16 matrix kernel (cache_attend_bf16.hip), 0: the fp32 one (cache_attend_f32.hip)
-  int rb;                 // 16-row blocks of a workgroup
+  int mfma;               // 1: the bf16 matrix kernels (cache_attend_bf16.hip, 128 rows: cache_attend_rows.hip), 0: the fp32 one
+  int rows;               // query rows of a workgroup
   int min_chunk;          // least slots of a chunk: a tile for every wave
   int gather;             // the weights are gathered: the first launch leaves the scores in the workspace
   int stream;             // 1: the cache is read past the caches (see cache_attend_bf16.hip)
   int join;               // a second launch joins the chunks (and gathers); else the first one writes out and lse
-  int64_t blocks;         // workgroups of the first launch
-  int64_t most_chunks;    // of a sequence
-  size_t off_ml, off_o, off_x, total_bytes;   // workspace: (M, Z) and sums of the chunks, scores [H][slots]
+  int64_t units;          // workgroups of the first launch per KV head
+  int64_t most_chunks;    // of a sequence when all are full
+  size_t off_shares, off_ml, off_o, off_x, total_bytes;   // workspace: shares, (M, Z) and sums of the chunks, scores [H][slots]
 };
 
 struct AttendWork {
@@ -86,26 +85,24 @@ struct AttendWork {
   int64_t qst, qsh;
   void* out;
   float* lse;
-  float *ml, *o, *x;      // partial results as the table numbers them, [.][2] and [.][padded head dim]; x NULL: no weights
-  int H, gs, min_chunk;
+  float *ml, *o, *x;      // partial results [workgroup][row of it], (M, Z) and sums of the padded head dim; x NULL: no weights
+  int4* shares;           // [sequence] how the units were shared out: the first one, chunks, chunks with slots, slots in use
+  int H, gs, min_chunk, units;
   uint32_t gs_recip;      // floor(2^32 / gs) + 1: divides a sequence's rows (below 2^18) exactly; 0: gs is 1
   float lambda;
   int64_t rows;           // new tokens x H
   int64_t xs;             // scores: head h, slot s of sequence b at h xs + cu[b] + kScorePad b + s
 };
 
-// Slots of a chunk when n of them are cut into at most nc: whole tiles for every wave.
-__host__ __device__ inline int chunk_slots(int n, int nc, int min_chunk) {
-  const int per = (n + nc - 1) / nc;
-  return per <= min_chunk ? min_chunk : (per + 31) / 32 * 32;
-}
-
 hipError_t launch_cache_append(const CacheTable& t, const CacheView& c, const void* k_new, const void* v_new, int64_t nsh,
                                int64_t nst, const int32_t* pos_new, const float* mass_new, int64_t nsp, int elem_bytes,
                                int32_t* lens_out, hipStream_t st);
 hipError_t launch_cache_attend_f32(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p,
                                    const AttendWork& w, bool bf16, hipStream_t st);
-// a plan with mfma set
+// a plan with mfma set and 128 rows
+hipError_t launch_cache_attend_rows(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p,
+                                    const AttendWork& w, hipStream_t st);
+// a plan with mfma set and 16 or 32
 hipError_t launch_cache_attend_bf16(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p,
                                     const AttendWork& w, hipStream_t st);
 hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const AttendPlan& p, const AttendWork& w, bool bf16,
@@ -192,10 +189,24 @@ template <> __device__ __forceinline__ void put_out<uint16_t>(uint16_t* p, float
   const uint32_t u = __float_as_uint(x);   // round to nearest, ties to even; NaN stays NaN
   *p = x != x ? 0x7FC0 : (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
 }
+// components c .. c + 3 of row r of a KV head's rows, as the chunk's partial result or, with one chunk, as out and lse
+template <class T, int DP>
+__device__ __forceinline__ void leave(const AttendWork& w, int d, int g, int r, int c, float top, float z, floatx4 o, int new0, int64_t part, int nc) {
+  const int t = token_of(w, r);
+  const int head = g * w.gs + (r - t * w.gs);
+  const int64_t at = (int64_t)(new0 + t) * w.H + head;
+  if (nc == 1 && !w.x) {
+    const float inv = z > 0.f ? 1.f / z : 0.f;
+    for (int i = 0; i < 4 && c + i < d; ++i) put_out<T>((T*)w.out + at * d + c + i, o[i] * inv);
+    if (c == 0) w.lse[at] = z > 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
+  } else {
+    *reinterpret_cast<floatx4*>(w.o + part * DP + c) = o;
+    if (c == 0) { w.ml[part * 2] = top; w.ml[part * 2 + 1] = z; }
+  }
+}
 template <class T, int DP, int RB>
 __device__ __forceinline__ void finish_chunk(const floatx4 (&O)[DP / 16][RB], const float (&M)[RB], const float (&Zl)[RB],
-                                             float* buf, const AttendWork& w, int d, int g, int row0, int rows, int new0, int64_t part0, int nc,
-                                             int chunk) {
+                                             float* buf, const AttendWork& w, int d, int g, int row0, int rows, int new0, int nc) {
   constexpr int ROWS = 16 * RB, W = DP + 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q4 = lane >> 4;
   float* ml = buf + kAttendWaves * ROWS * W;   // [wave][row][2]
@@ -235,40 +246,88 @@ __device__ __forceinline__ void finish_chunk(const floatx4 (&O)[DP / 16][RB], co
       z += ml[(i * ROWS + row) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(i * ROWS + row) * 2] - top);
       o += *reinterpret_cast<const floatx4*>(buf + (i * ROWS + row) * W + c);
     }
-    const int r = row0 + row, t = token_of(w, r);
-    const int head = g * w.gs + (r - t * w.gs);
-    const int64_t at = (int64_t)(new0 + t) * w.H + head;
-    if (nc == 1 && !w.x) {
-      const float inv = z > 0.f ? 1.f / z : 0.f;
-      for (int i = 0; i < 4 && c + i < d; ++i) put_out<T>((T*)w.out + at * d + c + i, o[i] * inv);
-      if (c == 0) w.lse[at] = z > 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
-    } else {
-      const int64_t part = part0 + ((int64_t)t * w.H + head) * nc + chunk;
-      *reinterpret_cast<floatx4*>(w.o + part * DP + c) = o;
-      if (c == 0) { w.ml[part * 2] = top; w.ml[part * 2 + 1] = z; }
-    }
+    leave<T, DP>(w, d, g, row0 + row, c, top, z, o, new0, (int64_t)blockIdx.x * ROWS + row, nc);
   }
 }
 
-// workgroup -> (sequence, chunk, block of rows, KV head): the heads vary fastest, so that the workgroups which read the same
-// slots for other rows are a multiple of the heads apart
-struct AttendPlace {
-  int b, chunk, rc, g, nc;
+// over the 64 lanes, by moves inside the rows of 16 and then between them (six vector instructions; shuffles take as many trips through the
+// LDS crossbar): a lane's sum up to itself
+__device__ __forceinline__ uint32_t sum_up(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+
+// How the units of an attend call are shared out, sequence b in lane b: chunks of one length for all, so that workgroups end together however
+// the lengths differ (a sequence of 16384 slots among 31 of 500, room for 16384 each: 28 us, by their room 86; 32 lengths spread evenly up to
+// 16384: 171 and 182).  The length is the mean slots of a unit, made longer by a 16th until the chunks are no more than the units;
+// the host sees to it that one chunk each is not.
+struct Cuts {
+  uint32_t n;        // slots in use
+  uint32_t rcs, nc;  // blocks of query rows, chunks
+  uint32_t end;      // units of the sequences up to this one
+  int len;           // slots of a chunk, whole tiles
 };
 template <class TAB>
-__device__ __forceinline__ AttendPlace attend_place(const TAB& t, int G, int gs, int rows_wg) {
+__device__ __forceinline__ Cuts cuts_of(const TAB& t, const int32_t* lens, const AttendWork& w) {
+  const int lane = threadIdx.x & 63, b = min(lane, t.batch - 1);
+  Cuts c;
+  const int32_t len = lens[b], fresh = t.cu_new[b + 1] - t.cu_new[b];
+  const int64_t cap = t.cu[b + 1] - t.cu[b];
+  c.n = (uint32_t)max(0, (int)min((int64_t)len, cap));
+  c.rcs = lane < t.batch ? (uint32_t)(t.units[b + 1] - t.units[b]) : 0u;
+  const uint32_t tiles = (int)c.n < fresh ? 0u : (c.n + 31u) / 32u, units = (uint32_t)w.units;
+  const uint64_t mine = (uint64_t)tiles * c.rcs;   // (below 2^26 x 2^18; the sums of its halves stay below 2^32)
+  const uint64_t total = ((uint64_t)from_lane(sum_up((uint32_t)(mine >> 24)), 63) << 24) + from_lane(sum_up((uint32_t)mine & 0xFFFFFFu), 63);
+  uint32_t len32 = total >> 31 ? (uint32_t)((total + units - 1) / units) : ((uint32_t)total + units - 1) / units;
+  len32 = max(len32, (uint32_t)w.min_chunk / 32u);
+  for (;;) {
+    c.nc = max(1u, (tiles + len32 - 1) / len32);
+    c.end = sum_up(c.rcs * c.nc);
+    if (from_lane(c.end, 63) <= units) break;
+    len32 += (len32 + 15) / 16;
+  }
+  c.len = (int)min((uint64_t)len32 * 32, (uint64_t)0x7FFFFFFF);
+  return c;
+}
+
+// workgroup -> (sequence, chunk, block of rows, KV head): the heads vary fastest, so that the workgroups which read the same
+// slots for other rows are a multiple of the heads apart.  b < 0: a unit that nobody needs.
+struct AttendPlace {
+  int b, chunk, rc, g, nc;
+  int s0, s1;   // the chunk's slots
+  Held h;       // (n is 0 for a sequence that holds less than its fresh tokens)
+};
+template <class TAB>
+__device__ __forceinline__ AttendPlace attend_place(const TAB& t, const CacheView& c, const AttendWork& w) {
   AttendPlace p;
-  const bool shifts = (G & (G - 1)) == 0;   // (a division costs some 40 instructions)
-  const int u = shifts ? (int)(blockIdx.x >> __builtin_ctz(G)) : (int)(blockIdx.x / G);
-  p.g = blockIdx.x - u * G;
-  int b = 0;
-  while (b + 1 < t.batch && u >= t.units[b + 1]) ++b;
-  const int rcs = ((t.cu_new[b + 1] - t.cu_new[b]) * gs + rows_wg - 1) / rows_wg;
-  p.b = b;
-  const int units = t.units[b + 1] - t.units[b], at = u - t.units[b];
-  p.nc = rcs == 1 ? units : units / rcs;
+  const Cuts k = cuts_of(t, c.lens, w);
+  const bool shifts = (c.G & (c.G - 1)) == 0;   // (a division costs some 40 instructions)
+  const int u = shifts ? (int)(blockIdx.x >> __builtin_ctz(c.G)) : (int)(blockIdx.x / c.G);
+  p.g = blockIdx.x - u * c.G;
+  if (w.shares && blockIdx.x == 0 && (int)threadIdx.x < t.batch) {
+    const int fresh = t.cu_new[threadIdx.x + 1] - t.cu_new[threadIdx.x];
+    w.shares[threadIdx.x] = make_int4((int)(k.end - k.rcs * k.nc), (int)k.nc, (int)k.n < fresh || k.n == 0 ? 0 : (int)k.nc, (int)k.n);
+  }
+  p.b = __popcll(__ballot(k.end <= (uint32_t)u));
+  if (p.b >= t.batch) { p.b = -1; return p; }
+  const int rcs = (int)from_lane(k.rcs, p.b);
+  p.nc = (int)from_lane(k.nc, p.b);
+  const int at = u - ((int)from_lane(k.end, p.b) - rcs * p.nc);
   p.chunk = rcs == 1 ? at : at / rcs;
   p.rc = at - p.chunk * rcs;
+  p.h.lo = t.cu[p.b];
+  p.h.n = (int)from_lane(k.n, p.b);
+  p.h.fresh = t.cu_new[p.b + 1] - t.cu_new[p.b];
+  p.h.base = p.h.n - p.h.fresh;
+  if (p.h.base < 0) p.h.n = 0;
+  p.s0 = (int)min((int64_t)p.h.n, (int64_t)p.chunk * k.len);
+  p.s1 = (int)min((int64_t)p.h.n, (int64_t)p.s0 + k.len);
   return p;
 }
 #endif

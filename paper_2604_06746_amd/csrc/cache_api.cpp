@@ -111,7 +111,7 @@ bool mfma_fits(const structkv_cache* c, const void* q, int64_t qst, int64_t qsh)
          (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)q) & 15) == 0 && c->stride_slot < ((int64_t)1 << 25);
 }
 
-// Chunks: as many workgroups as fill the chip once or twice, but at least kLeastChunk slots each.
+// Workgroups: two a CU (more or fewer, 256 to 4096, were slower), at least kLeastChunk slots each.
 constexpr int64_t kAttendBlocks = 512, kLeastChunk = 128;
 
 structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mfma, CacheTable* t, AttendPlan* p) {
@@ -121,32 +121,39 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   p->gather = gather;
   int64_t most_rows = 0;
   for (int b = 0; b < c->batch; ++b) most_rows = std::max<int64_t>(most_rows, (int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs);
-  p->rb = !mfma || gather || most_rows <= 16 ? 1 : 2;
-  p->min_chunk = kAttendWaves * (mfma ? 32 : 16);
-  const int rows_wg = 16 * p->rb;
-  p->stream = most_rows <= rows_wg && t->cu[c->batch] * c->n_kv_heads * c->head_dim * 2 * elem_bytes(c) >= kStreamBytes;
-  double work = 0;   // slots that the workgroups read in all
+  // 128 rows (32 a wave, the tiles shared) where there are more than two blocks of 32 and where enough chunks of them fill the chip: four trees
+  // of 64 drafts over 16512 slots 150 us with, 163 without (one call behind the other); of 16 drafts (64 rows) 68 and 60, one of 64 over 2000
+  // slots 25 and 20
+  int64_t wide_units = 0;
   for (int b = 0; b < c->batch; ++b)
-    work += (double)ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, rows_wg) * c->n_kv_heads * (double)(t->cu[b + 1] - t->cu[b]);
-  const int64_t each = std::max<int64_t>(kLeastChunk, (int64_t)std::ceil(work / kAttendBlocks));
-  int64_t units = 0, part = 0, stretches = 0;   // (of 64 slots, the fewest whose weights a workgroup of the join gathers)
-  p->join = gather;
+    wide_units += ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, 128) * ceil_div(t->cu[b + 1] - t->cu[b], kLeastChunk);
+  const bool wide = most_rows > 64 && wide_units >= kAttendBlocks / c->n_kv_heads;
+  p->rows = !mfma || gather || most_rows <= 16 ? 16 : wide ? 128 : 32;
+  p->min_chunk = kAttendWaves * (mfma ? 32 : 16);
+  const int rows_wg = p->rows;
+  p->stream = most_rows <= rows_wg && t->cu[c->batch] * c->n_kv_heads * c->head_dim * 2 * elem_bytes(c) >= kStreamBytes;
+  // units: what fills the chip twice over the KV heads, no chunk below kLeastChunk slots in full sequences, a chunk at least of each
+  int64_t blocks = 0, chunks = 0, stretches = 0;   // (of 64 slots, the fewest whose weights a workgroup of the join gathers)
+  double work = 0;   // slots that the units of a KV head read in all
   for (int b = 0; b < c->batch; ++b) {
-    const int64_t fresh = t->cu_new[b + 1] - t->cu_new[b], cap = t->cu[b + 1] - t->cu[b];
-    const int64_t nc = std::max<int64_t>(1, ceil_div(cap, each));
-    units += nc * ceil_div(fresh * gs, rows_wg);
-    part += fresh * H * nc;
+    const int64_t rcs = ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, rows_wg), cap = t->cu[b + 1] - t->cu[b];
+    blocks += rcs;
+    chunks += rcs * std::max<int64_t>(1, ceil_div(cap, kLeastChunk));
+    work += (double)rcs * (double)cap;
     stretches += gather ? ceil_div(cap, 64) * c->planes : 0;
-    if (units * c->n_kv_heads >= ((int64_t)1 << 31) || part + stretches >= ((int64_t)1 << 31))
-      return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
-    t->units[b + 1] = (int32_t)units;
-    t->part[b + 1] = (int32_t)part;
-    if (fresh > 0 && nc > 1) p->join = 1;
-    if (fresh > 0) p->most_chunks = std::max(p->most_chunks, nc);
+    t->units[b + 1] = (int32_t)blocks;
   }
-  p->blocks = units * c->n_kv_heads;
+  p->units = std::max(blocks, std::min(chunks, kAttendBlocks / c->n_kv_heads));
+  if (p->units * c->n_kv_heads >= ((int64_t)1 << 31) || stretches >= ((int64_t)1 << 30))
+    return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
+  p->join = gather || p->units > blocks;
+  const int64_t each = std::max<int64_t>(p->min_chunk, (int64_t)std::ceil(work / (double)std::max<int64_t>(1, p->units)));
+  for (int b = 0; b < c->batch; ++b)
+    if (t->cu_new[b + 1] > t->cu_new[b]) p->most_chunks = std::max(p->most_chunks, ceil_div(t->cu[b + 1] - t->cu[b], each));
+  const int64_t part = p->units * c->n_kv_heads * rows_wg;
   const size_t parts = p->join ? (size_t)part : 0;
   size_t off = 0;
+  p->off_shares = off; off += p->join ? align_up(sizeof(int4) * (size_t)c->batch, 256) : 0;
   p->off_ml = off; off += align_up(parts * 2 * sizeof(float), 256);
   p->off_o = off;  off += align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256);
   p->off_x = off;  off += gather ? score_bytes(H, t->cu[c->batch], c->batch) : 0;
@@ -154,12 +161,14 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   return STRUCTKV_OK;
 }
 
-// ... at most, however the tokens spread: a sequence's chunks are at most its share of kAttendBlocks / its row blocks and KV heads, and one
-// more; its rows per row block and KV head at most rows_wg
+// ... at most, however the tokens spread: units per KV head are kAttendBlocks in all, or the blocks of rows, which are joined for single tokens'
+// weights alone
 size_t most_attend_bytes(const structkv_cache* c, int H, int64_t new_tokens, int64_t slots) {
-  const size_t rows_wg = 32;
-  const size_t parts = rows_wg * (size_t)kAttendBlocks + (size_t)new_tokens * H;
-  return align_up(parts * 2 * sizeof(float), 256) + align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256) +
+  const int64_t gs = H / c->n_kv_heads, rows = new_tokens * gs;
+  const bool wide = c->dtype == STRUCTKV_DTYPE_BF16 && (c->head_dim == 64 || c->head_dim == 128);
+  const int64_t rows_wg = !wide || rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
+  const size_t parts = (size_t)std::max(rows_wg * kAttendBlocks, 16 * new_tokens * ceil_div(gs, 16) * c->n_kv_heads);
+  return align_up(sizeof(int4) * (size_t)c->batch, 256) + align_up(parts * 2 * sizeof(float), 256) + align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256) +
          (c->mass ? score_bytes(H, slots, c->batch) : 0);
 }
 
@@ -272,9 +281,10 @@ structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_h
   uint8_t* w8 = (uint8_t*)workspace;
   const int gs = n_q_heads / cache->n_kv_heads;
   const AttendWork w = {q, q_stride_tok, q_stride_head, out, lse_out, (float*)(w8 + p.off_ml), (float*)(w8 + p.off_o),
-                        p.gather ? (float*)(w8 + p.off_x) : nullptr, n_q_heads, gs, p.min_chunk, reciprocal(gs), lambda,
+                        p.gather ? (float*)(w8 + p.off_x) : nullptr, p.join ? (int4*)(w8 + p.off_shares) : nullptr, n_q_heads, gs, p.min_chunk, (int)p.units, reciprocal(gs), lambda,
                         (int64_t)t.cu_new[cache->batch] * n_q_heads, v.slots + kScorePad * cache->batch};
-  if (p.mfma) SKV_HIP_CHECK(launch_cache_attend_bf16(t, v, f, p, w, (hipStream_t)stream));
+  if (p.mfma && p.rows == 128) SKV_HIP_CHECK(launch_cache_attend_rows(t, v, f, p, w, (hipStream_t)stream));
+  else if (p.mfma) SKV_HIP_CHECK(launch_cache_attend_bf16(t, v, f, p, w, (hipStream_t)stream));
   else SKV_HIP_CHECK(launch_cache_attend_f32(t, v, f, p, w, bf16, (hipStream_t)stream));
   if (p.join) SKV_HIP_CHECK(launch_cache_combine(t, v, p, w, bf16, (hipStream_t)stream));
   return STRUCTKV_OK;
@@ -299,8 +309,8 @@ structkv_status structkv_cache_accept(const structkv_cache* cache, int32_t n_q_h
   const bool weigh = lambda > 0.f && t.cu_new[cache->batch] > 0;
   if (weigh && (!q || !lse)) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda > 0 needs q and lse");
   if (weigh) {
-    const AttendWork w = {q, q_stride_tok, q_stride_head, nullptr, const_cast<float*>(lse), nullptr, nullptr, nullptr, n_q_heads,
-                          n_q_heads / cache->n_kv_heads, 0, reciprocal(n_q_heads / cache->n_kv_heads), lambda, 0, 0};
+    const AttendWork w = {q, q_stride_tok, q_stride_head, nullptr, const_cast<float*>(lse), nullptr, nullptr, nullptr, nullptr, n_q_heads,
+                          n_q_heads / cache->n_kv_heads, 0, 0, reciprocal(n_q_heads / cache->n_kv_heads), lambda, 0, 0};
     if (mfma_fits(cache, q, q_stride_tok, q_stride_head)) SKV_HIP_CHECK(launch_cache_weights_bf16(t, v, f, w, path, n_accept, (hipStream_t)stream));
     else SKV_HIP_CHECK(launch_cache_weights_f32(t, v, f, w, path, n_accept, cache->dtype == STRUCTKV_DTYPE_BF16, (hipStream_t)stream));
   }

@@ -13,9 +13,7 @@
 // NT: tiles are fetched with the non-temporal policy, where no other workgroup reads them and the cache is larger than what the memory-side
 // cache keeps from one step to the next: 4 GB 715 -> 623 us (6.9 TB/s), 216 MB 81 -> 72 us.  The stores of the scores (128 bytes a
 // slot of 32 heads) are what gathering weights costs: 846 us with them and their reading, 696 where they stayed in a cache.
-// Rows beyond 32 of a KV head are other workgroups', which read the tiles again, from the XCD's L2.  Not kept: four waves of 32 rows on common
-// tiles with barriers (64 drafts over four times 16.5K slots 165 -> 164 us, over 2112 slots 20.6 -> 28.2), the second block's
-// weights under the first one's products (no change): two waves a SIMD issue every 5 cycles at best, 350 instructions a tile.
+// Rows beyond 32 of a KV head are other workgroups', which read the tiles again, from the XCD's L2; beyond 64 cache_attend_rows.hip has them.
 // The rows' references M follow lazily: they are raised only when a score lies more than 2^8 above one of them, so that the usual tile has
 // no exchange between lanes and no rescaling.
 #include "cache_bf16.h"
@@ -59,8 +57,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   __shared__ __attribute__((aligned(1024))) uint8_t lds[RING > FIN ? RING : FIN];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const AttendPlace p = attend_place(tab, c.G, w.gs, 16 * RB);
-  const Held h = held(tab, c.lens, p.b);
+  const AttendPlace p = attend_place(tab, c, w);
+  if (p.b < 0) return;
+  const Held& h = p.h;
+  const int n = h.n, s0 = p.s0, s1 = p.s1;
   // the queries first: the length has no part in their addresses
   const int new0 = tab.cu_new[p.b], rows = h.fresh * w.gs, row0 = p.rc * 16 * RB;
   bf16x8 qf[RB][KS];
@@ -79,9 +79,6 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
     slope[rb] = MODE == kBiased && f.slopes ? f.slopes[head] : 0.f;
     if (SAVE) save = w.x + head * w.xs + h.lo + kScorePad * p.b;
   }
-  const int n = h.base < 0 ? 0 : h.n;
-  const int len = chunk_slots(n, p.nc, w.min_chunk);
-  const int s0 = (int)min((int64_t)n, (int64_t)p.chunk * len), s1 = min(n, s0 + len);
   if (s0 >= s1 && (p.nc > 1 || w.x)) return;   // (the join reads no more chunks than have slots)
 
   const uint16_t* kg = (const uint16_t*)c.k + (int64_t)p.g * c.sh + h.lo * c.ss;
@@ -280,14 +277,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
     }
     if (i + 1 < mine) fetch_v(next);   // (read_columns has waited)
   }
-  finish_chunk<uint16_t, D, RB>(O, M, Z, reinterpret_cast<float*>(lds), w, D, p.g, row0, rows, new0, tab.part[p.b], p.nc, p.chunk);
+  finish_chunk<uint16_t, D, RB>(O, M, Z, reinterpret_cast<float*>(lds), w, D, p.g, row0, rows, new0, p.nc);
 }
 
 template <int D, int RB>
 hipError_t attend(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p, const AttendWork& w, hipStream_t st) {
   with_cache_table(t, [&](const auto& tab) {
     using TAB = std::decay_t<decltype(tab)>;
-    const dim3 grid((unsigned)p.blocks), block(64 * kAttendWaves);
+    const dim3 grid((unsigned)(p.units * c.G)), block(64 * kAttendWaves);
     auto go = [&](auto mode, auto save) {
       constexpr int MODE = decltype(mode)::value;
       constexpr bool SAVE = decltype(save)::value;
@@ -307,8 +304,8 @@ hipError_t attend(const CacheTable& t, const CacheView& c, const ScoreForm& f, c
 
 hipError_t launch_cache_attend_bf16(const CacheTable& t, const CacheView& c, const ScoreForm& f, const AttendPlan& p,
                                     const AttendWork& w, hipStream_t st) {
-  if (c.d == 128) return p.rb == 1 ? attend<128, 1>(t, c, f, p, w, st) : attend<128, 2>(t, c, f, p, w, st);
-  return p.rb == 1 ? attend<64, 1>(t, c, f, p, w, st) : attend<64, 2>(t, c, f, p, w, st);
+  if (c.d == 128) return p.rows == 16 ? attend<128, 1>(t, c, f, p, w, st) : attend<128, 2>(t, c, f, p, w, st);
+  return p.rows == 16 ? attend<64, 1>(t, c, f, p, w, st) : attend<64, 2>(t, c, f, p, w, st);
 }
 
 }  // namespace skv

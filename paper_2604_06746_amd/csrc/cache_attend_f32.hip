@@ -66,8 +66,10 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
   constexpr int RING = kAttendWaves * 2 * kTile * W, FIN = kFinishFloats<DP, 1>;
   __shared__ __attribute__((aligned(16))) float lds[RING > FIN ? RING : FIN];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l16 = lane & 15, q4 = lane >> 4;
-  const AttendPlace p = attend_place(tab, c.G, w.gs, 16);
-  const Held h = held(tab, c.lens, p.b);
+  const AttendPlace p = attend_place(tab, c, w);
+  if (p.b < 0) return;
+  const Held& h = p.h;
+  const int n = h.n, s0 = p.s0, s1 = p.s1;
   // the queries first: the length has no part in their addresses
   const int new0 = tab.cu_new[p.b], rows = h.fresh * w.gs, row0 = p.rc * 16;
   const int row = min(row0 + l16, rows - 1), t = token_of(w, row), head = p.g * w.gs + row - t * w.gs;
@@ -79,9 +81,6 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
   const uint64_t mask = row_mask(f, r, t);
   const bool more = f.softcap > 0.f || f.slopes;
   const float slope = f.slopes ? f.slopes[head] : 0.f;
-  const int n = h.base < 0 ? 0 : h.n;
-  const int len = chunk_slots(n, p.nc, w.min_chunk);
-  const int s0 = (int)min((int64_t)n, (int64_t)p.chunk * len), s1 = min(n, s0 + len);
   if (s0 >= s1 && (p.nc > 1 || w.x)) return;   // (the join reads no more chunks than have slots)
   const int32_t* pos = f.slopes ? c.pos + (c.planes > 1 ? p.g * c.slots : 0) + h.lo : nullptr;
   const T* kg = (const T*)c.k + (int64_t)p.g * c.sh + h.lo * c.ss;
@@ -154,7 +153,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
         O[db][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[(4 * q4 + i) * W + db * 16 + l16], pr[i], O[db][0], 0, 0, 0);
     }
   }
-  finish_chunk<T, DP, 1>(O, M, Z, lds, w, c.d, p.g, row0, rows, new0, tab.part[p.b], p.nc, p.chunk);
+  finish_chunk<T, DP, 1>(O, M, Z, lds, w, c.d, p.g, row0, rows, new0, p.nc);
 }
 
 // Weights of the accepted drafts: a wave takes 16 slots of a plane, goes through the plane's KV heads and their accepted rows, and adds up
@@ -249,7 +248,7 @@ hipError_t attend(const CacheTable& t, const CacheView& c, const ScoreForm& f, c
     using TAB = std::decay_t<decltype(tab)>;
     constexpr int DP = decltype(dp)::value;
     constexpr bool VEC = decltype(vec)::value;
-    const dim3 grid((unsigned)p.blocks);
+    const dim3 grid((unsigned)(p.units * c.G));
     if (VEC && p.stream) cache_attend_f32_kernel<TAB, T, DP, VEC, VEC><<<grid, 64 * kAttendWaves, 0, st>>>(tab, c, f, w);
     else cache_attend_f32_kernel<TAB, T, DP, VEC, false><<<grid, 64 * kAttendWaves, 0, st>>>(tab, c, f, w);
   });

@@ -25,6 +25,13 @@ __device__ __forceinline__ void wait_lds() {
   asm volatile("" ::: "memory");
 }
 
+// the workgroup's barrier, with loads to LDS left on their way; no access moves across
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 enum { kPlain = 0, kCapped = 1, kBiased = 2 };   // how scores are formed: scaled; capped; in full
 // Up to this cap its quick form is taken, whose error of cap x 2^-22 is a weight's relative one: 2^-14 here, a 64th of a bf16 rounding.
 constexpr float kLargestQuickCap = 256.f;

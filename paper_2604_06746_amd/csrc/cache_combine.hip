@@ -2,8 +2,8 @@
 //
 // Chunk i of a row left (M_i, Z_i, O_i); with M = max M_i: Z = sum 2^(M_i - M) Z_i, out = sum 2^(M_i - M) O_i / Z, lse = ln 2 (M + log2 Z).
 // A workgroup per row.  The workgroups behind the rows' add the weights of a stretch of slots of one plane, 2^(x - lse) from the scores that
-// the first launch left, so that the cache is read once.  Few bytes, so what counts is the chain of loads: length; then the chunks' M and Z
-// beside the sums or the scores themselves, all at once; nothing is loaded after the norms are known.
+// the first launch left, so that the cache is read once.  Few bytes, so what counts is the chain of loads: the sequence's shares, which the
+// first launch left; then the chunks' M and Z beside the sums or the scores themselves, all at once; nothing is loaded after the norms are known.
 #include "cache.h"
 
 namespace skv {
@@ -41,23 +41,23 @@ constexpr int kAhead = 8;   // loads of a thread that are on their way at once
 
 // What joining a row needs to know; n: its slots.
 struct Row {
-  int b, live;
-  int64_t part0;
-  bool written;   // by the first launch
+  int live;
+  int64_t part0, step;   // its first chunk's partial result, and how far the next one's is
+  bool written;          // by the first launch
 };
 template <class TAB>
 __device__ __forceinline__ Row row_of(const TAB& tab, const CacheView& c, const AttendWork& w, int64_t at, int rows_wg) {
-  const int r = (int)((uint32_t)at / (uint32_t)w.H);   // (rows stay below 2^31)
+  const int r = (int)((uint32_t)at / (uint32_t)w.H), head = (int)(at - (int64_t)r * w.H);   // (rows stay below 2^31)
   Row row;
   int b = 0;
   while (b + 1 < tab.batch && r >= tab.cu_new[b + 1]) ++b;
-  const Held h = held(tab, c.lens, b);
-  const int n = h.base < 0 ? 0 : h.n, rcs = (h.fresh * w.gs + rows_wg - 1) / rows_wg, nc = (tab.units[b + 1] - tab.units[b]) / rcs;
-  const int len = chunk_slots(n, nc, w.min_chunk);
-  row.b = b;
-  row.live = (n + len - 1) / len;
-  row.part0 = tab.part[b] + (at - (int64_t)tab.cu_new[b] * w.H) * nc;
-  row.written = nc == 1 && !w.x;
+  const int4 share = w.shares[b];
+  const int rcs = tab.units[b + 1] - tab.units[b];
+  const int g = token_of(w, head), mine = (r - tab.cu_new[b]) * w.gs + head - g * w.gs, rc = mine >> __builtin_ctz(rows_wg);
+  row.live = share.z;
+  row.part0 = ((int64_t)(share.x + rc) * c.G + g) * rows_wg + (mine & (rows_wg - 1));
+  row.step = (int64_t)rcs * c.G * rows_wg;
+  row.written = share.y == 1 && !w.x;
   return row;
 }
 template <class T>
@@ -67,7 +67,8 @@ __device__ __forceinline__ void put_row(const AttendWork& w, int64_t at, int d, 
   if (col == 0) w.lse[at] = z > 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
 }
 
-// FEW: at most kFewChunks chunks a row, a lane group of DP / 4 a row; else a workgroup a row, its lane groups on shares of the chunks
+// FEW: a lane group of DP / 4 a row, for sequences that have some kFewChunks chunks when all are full (more, in rounds, where the others are
+// short); else a workgroup a row, its lane groups on shares of the chunks
 constexpr int kFewChunks = 8;
 template <class TAB, class T, int DP, bool FEW, int V>
 __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c, AttendWork w, int rows_wg, int row_blocks, int stretch) {
@@ -84,42 +85,51 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
     if (row.written) return;
     const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + row.part0;
     const float* po = w.o + row.part0 * DP + col;
+    const int64_t step = row.step;
     const bool mine = col < c.d;
-    constexpr int STEP = FEW ? 1 : PARTS;
-    const int i0 = FEW ? 0 : part;
     floatx4 first[kAhead];
     floatx2 stat[kAhead];
+    auto load = [&](int i0, int stride) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int i = i0 + k * STEP;
-      stat[k] = i < row.live ? ml[i] : floatx2{kNothingSeen, 0.f};
-      first[k] = mine && i < row.live ? *reinterpret_cast<const floatx4*>(po + (int64_t)i * DP) : floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    float top = kNothingSeen;
-    if (FEW) {
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) top = fmaxf(top, stat[k][0]);
-    } else {
-      for (int i = lane; i < row.live; i += 64) top = fmaxf(top, ml[i][0]);
-      top = wave_top(top);
-    }
-    float z = 0.f;
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k * stride;
+        stat[k] = i < row.live ? ml[i * step] : floatx2{kNothingSeen, 0.f};
+        first[k] = mine && i < row.live ? *reinterpret_cast<const floatx4*>(po + i * step * DP) : floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+    };
+    float top = kNothingSeen, z = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const float s = __builtin_amdgcn_exp2f(stat[k][0] - top);
-      z = fmaf(s, stat[k][1], z);
-      o += first[k] * s;
-    }
+      for (int k = 0; k < kAhead; ++k) {
+        const float s = __builtin_amdgcn_exp2f(stat[k][0] - top);
+        z = fmaf(s, stat[k][1], z);
+        o += first[k] * s;
+      }
+    };
     if (FEW) {
-      static_assert(kFewChunks == kAhead, "all of a row's chunks at once");
+      for (int i0 = 0; i0 < row.live; i0 += kAhead) {
+        load(i0, 1);
+        const float old = top;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) top = fmaxf(top, stat[k][0]);
+        const float shrink = __builtin_amdgcn_exp2f(old - top);
+        z *= shrink;
+        o *= shrink;
+        add();
+      }
       if (mine) put_row<T>(w, at, c.d, col, o, top, z);
       return;
     }
+    load(part, PARTS);
+    for (int i = lane; i < row.live; i += 64) top = fmaxf(top, ml[i * step][0]);
+    top = wave_top(top);
+    add();
     for (int i = part + kAhead * PARTS; i < row.live; i += PARTS) {
-      const float s = __builtin_amdgcn_exp2f(ml[i][0] - top);
-      z = fmaf(s, ml[i][1], z);
-      if (mine) o += *reinterpret_cast<const floatx4*>(po + (int64_t)i * DP) * s;
+      const floatx2 m = ml[i * step];
+      const float s = __builtin_amdgcn_exp2f(m[0] - top);
+      z = fmaf(s, m[1], z);
+      if (mine) o += *reinterpret_cast<const floatx4*>(po + i * step * DP) * s;
     }
     // the shares: lanes of a wave that have the same components, then the waves
     for (int m = LANES; m < 64; m <<= 1) {
@@ -143,14 +153,14 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
   const int u = ((int)blockIdx.x - row_blocks) / c.planes, plane = ((int)blockIdx.x - row_blocks) % c.planes;
   int b = 0;
   while (b + 1 < tab.batch && u >= tab.reach[b + 1]) ++b;
-  const Held h = held(tab, c.lens, b);
-  const int s0 = (u - tab.reach[b]) * stretch, s1 = min(s0 + stretch, h.n);
-  if (h.fresh != 1 || h.base < 0 || s0 >= s1) return;
-  const int nc = (tab.units[b + 1] - tab.units[b]) / ((w.gs + rows_wg - 1) / rows_wg);
-  const int len = chunk_slots(h.n, nc, w.min_chunk), live = (h.n + len - 1) / len;
+  const int4 share = w.shares[b];
+  const int first = share.x, live = share.z;
+  const int s0 = (u - tab.reach[b]) * stretch, s1 = min(s0 + stretch, share.w);
+  if (tab.cu_new[b + 1] - tab.cu_new[b] != 1 || s0 >= s1) return;
+  const int64_t chunk_step = (int64_t)(tab.units[b + 1] - tab.units[b]) * c.G * rows_wg;
   const int heads = w.H / c.planes;
-  const float* x = w.x + plane * heads * w.xs + h.lo + kScorePad * b;
-  float* mass = c.mass + plane * c.slots + h.lo;
+  const float* x = w.x + plane * heads * w.xs + tab.cu[b] + kScorePad * b;
+  float* mass = c.mass + plane * c.slots + tab.cu[b];
   // V consecutive slots a thread.  Many heads: a wave's lanes' slots at a time, a wave every fourth head of them; few: the workgroup's threads'
   // slots at a time, all heads of a slot in its thread.  (x has room behind a sequence's scores, mass does not.)
   const bool split = heads >= kSplitHeads;
@@ -167,11 +177,13 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int i = i0 + 4 * j;
-      const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + tab.part[b] + (int64_t)(plane * heads + i) * nc;
-      a[j] = i < heads && lane < live ? ml[lane] : floatx2{kNothingSeen, 0.f};
+      const int head = plane * heads + i, g = token_of(w, head), r = head - g * w.gs;
+      const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + ((int64_t)(first + (r >> __builtin_ctz(rows_wg))) * c.G + g) * rows_wg + (r & (rows_wg - 1));
+      a[j] = i < heads && lane < live ? ml[lane * chunk_step] : floatx2{kNothingSeen, 0.f};
       for (int k = lane + 64; i < heads && k < live; k += 64) {
-        const float top = fmaxf(a[j][0], ml[k][0]);
-        a[j] = floatx2{top, a[j][1] * __builtin_amdgcn_exp2f(a[j][0] - top) + ml[k][1] * __builtin_amdgcn_exp2f(ml[k][0] - top)};
+        const floatx2 m = ml[k * chunk_step];
+        const float top = fmaxf(a[j][0], m[0]);
+        a[j] = floatx2{top, a[j][1] * __builtin_amdgcn_exp2f(a[j][0] - top) + m[1] * __builtin_amdgcn_exp2f(m[0] - top)};
       }
     }
 #pragma unroll
@@ -245,8 +257,8 @@ hipError_t launch_cache_combine(const CacheTable& t, const CacheView& c, const A
     with_cache_table(u, [&](const auto& tab) {
       using TAB = std::decay_t<decltype(tab)>;
       const dim3 grid((unsigned)blocks);
-      if (bf16) cache_combine_kernel<TAB, uint16_t, DP, FEW, V><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
-      else cache_combine_kernel<TAB, float, DP, FEW, V><<<grid, 256, lds, st>>>(tab, c, w, 16 * p.rb, (int)row_blocks, stretch);
+      if (bf16) cache_combine_kernel<TAB, uint16_t, DP, FEW, V><<<grid, 256, lds, st>>>(tab, c, w, p.rows, (int)row_blocks, stretch);
+      else cache_combine_kernel<TAB, float, DP, FEW, V><<<grid, 256, lds, st>>>(tab, c, w, p.rows, (int)row_blocks, stretch);
     });
     return hipGetLastError();
   };

@@ -305,43 +305,40 @@ hipError_t launch_gather(const void*, const void*, int64_t, int64_t, void*, void
 namespace skv {
 
 static AttendPlan g_last_attend;
-static int32_t g_last_chunks;   // of the latest attend call: workgroups per KV head
-// rows per workgroup, workgroups, whether the chunks are joined, whether by the bf16 kernels
+// rows per workgroup, units, whether the chunks are joined, whether by the bf16 kernels, bytes of workspace, chunks of the longest sequence
 extern "C" void structkv_stub_last_attend(int64_t* out) {
-  out[0] = 16 * g_last_attend.rb; out[1] = g_last_attend.blocks; out[2] = g_last_attend.join; out[3] = g_last_attend.mfma;
-  out[4] = (int64_t)g_last_attend.total_bytes; out[5] = g_last_chunks;
+  out[0] = g_last_attend.rows; out[1] = g_last_attend.units; out[2] = g_last_attend.join; out[3] = g_last_attend.mfma;
+  out[4] = (int64_t)g_last_attend.total_bytes; out[5] = g_last_attend.most_chunks;
 }
-// the bookkeeping that the attend kernels go by: whole row blocks times chunks for every sequence, partial results side by side
+// the bookkeeping that the attend kernels go by: whole blocks of rows for every sequence, units and partial results for all of them
 static bool attend_fits(const CacheTable& t, const AttendPlan& p, const AttendWork& w, int G) {
   ++g_launches;
   g_last_attend = p;
-  g_last_chunks = t.units[t.batch];
-  bool ok = p.rb >= 1 && p.rb <= 4 && p.min_chunk >= 16 * kAttendWaves && p.min_chunk % 32 == 0 && t.units[0] == 0 && t.part[0] == 0 &&
-            p.blocks == (int64_t)t.units[t.batch] * G && w.rows == (int64_t)t.cu_new[t.batch] * w.H;
+  bool ok = (p.rows == 16 || p.rows == 32 || p.rows == 128) && p.min_chunk >= 16 * kAttendWaves && p.min_chunk % 32 == 0 && t.units[0] == 0 &&
+            w.rows == (int64_t)t.cu_new[t.batch] * w.H && w.units == p.units && w.min_chunk == p.min_chunk;
   for (int b = 0; ok && b < t.batch; ++b) {
-    const int fresh = t.cu_new[b + 1] - t.cu_new[b], blocks = (fresh * w.gs + 16 * p.rb - 1) / (16 * p.rb), units = t.units[b + 1] - t.units[b];
-    ok = fresh == 0 ? units == 0 && t.part[b + 1] == t.part[b] : units > 0 && units % blocks == 0;
-    if (ok && fresh) {
-      const int64_t nc = units / blocks, cap = t.cu[b + 1] - t.cu[b];
-      ok = t.part[b + 1] - t.part[b] == nc * fresh * w.H && (nc == 1 || p.join) && (!p.gather || p.join);
-      for (int64_t n : {cap, cap / 3, (int64_t)1}) {   // whatever the length, the chunks cover it
-        const int len = chunk_slots((int)n, (int)nc, p.min_chunk);
-        ok = ok && (int64_t)len * nc >= n && len % 32 == 0 && len >= p.min_chunk;
-      }
-    }
+    const int fresh = t.cu_new[b + 1] - t.cu_new[b];
+    ok = t.units[b + 1] - t.units[b] == (fresh * w.gs + p.rows - 1) / p.rows;
   }
-  return ok;
+  // a unit at least for every block of rows, the join where there may be more than one, room for every unit's partial results
+  return ok && p.units >= t.units[t.batch] && (p.join || p.units == t.units[t.batch]) && (!p.gather || p.join) &&
+         (!p.join || (p.off_o - p.off_ml >= (size_t)(p.units * G * p.rows) * 8 && p.off_x - p.off_o >= (size_t)(p.units * G * p.rows) * 256));
 }
 hipError_t launch_cache_append(const CacheTable&, const CacheView&, const void*, const void*, int64_t, int64_t, const int32_t*,
                                const float*, int64_t, int, int32_t*, hipStream_t) { ++g_launches; return hipSuccess; }
 hipError_t launch_cache_attend_f32(const CacheTable& t, const CacheView& c, const ScoreForm&, const AttendPlan& p, const AttendWork& w,
                                    bool, hipStream_t) {
-  return attend_fits(t, p, w, c.G) && !p.mfma ? hipSuccess : hipErrorInvalidValue;
+  return attend_fits(t, p, w, c.G) && !p.mfma && p.rows == 16 ? hipSuccess : hipErrorInvalidValue;
 }
 hipError_t launch_cache_attend_bf16(const CacheTable& t, const CacheView& c, const ScoreForm&, const AttendPlan& p, const AttendWork& w,
                                     hipStream_t) {
-  const bool ok = p.mfma && (c.d == 64 || c.d == 128) && (p.rb == 1 || p.rb == 2 || p.rb == 4) && p.min_chunk >= 32 * kAttendWaves &&
-                  (!p.gather || p.rb == 1) && (c.sh | c.ss | w.qst | w.qsh) % 8 == 0 && c.ss < (1 << 25);
+  const bool ok = p.mfma && (c.d == 64 || c.d == 128) && (p.rows == 16 || p.rows == 32) && p.min_chunk >= 32 * kAttendWaves &&
+                  (!p.gather || p.rows == 16) && (c.sh | c.ss | w.qst | w.qsh) % 8 == 0 && c.ss < (1 << 25);
+  return attend_fits(t, p, w, c.G) && ok ? hipSuccess : hipErrorInvalidValue;
+}
+hipError_t launch_cache_attend_rows(const CacheTable& t, const CacheView& c, const ScoreForm&, const AttendPlan& p, const AttendWork& w,
+                                    hipStream_t) {
+  const bool ok = p.mfma && (c.d == 64 || c.d == 128) && p.rows == 128 && !p.gather && (c.sh | c.ss | w.qst | w.qsh) % 8 == 0 && c.ss < (1 << 25);
   return attend_fits(t, p, w, c.G) && ok ? hipSuccess : hipErrorInvalidValue;
 }
 hipError_t launch_cache_combine(const CacheTable&, const CacheView&, const AttendPlan& p, const AttendWork&, bool, hipStream_t) {

@@ -200,6 +200,38 @@ def test_attend_long(B, dtype, d):
     check_attend(B, c, 8, [20], tree=True, softcap=30.0, seed=22)
 
 
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("form", [dict(tree=True), dict(), dict(tree=True, softcap=30.0), dict(tree=True, slopes=True, softcap=5.0, scale=0.2)])
+def test_attend_trees_of_many_rows(B, d, form):
+    """More than two blocks of 32 rows and chunks enough: tiles shared by four waves, some without rows; fewer slots than drafts."""
+    c = R.make_cache(16, d, 16, [1400, 70, 901, 2100, 40], [1391, 70, 17, 2099, 33], torch.bfloat16, 41)
+    check_attend(B, c, 48, [64, 0, 20, 33, 33], layout="slots" if "softcap" in form else "heads", strided=True, seed=41, **form)
+    c = R.make_cache(64, d, 1, [100] * 9, [100, 99, 50, 41, 40, 39, 0, 65, 97], torch.bfloat16, 42)    # a chunk each: written at once
+    check_attend(B, c, 128, [34, 3, 35, 1, 33, 36, 2, 0, 1], seed=42, **form)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_attend_many_rows_that_see_nothing(B, d):
+    c = R.make_cache(32, d, 1, [1300, 900], [64, 800], torch.bfloat16, 43)
+    c.k[:, 20], c.v[:, 20] = math.nan, math.inf                     # drafts that nobody sees and that are not numbers
+    c.k[:, c.cu[1] + 799], c.v[:, c.cu[1] + 799] = math.inf, math.nan
+    masks = [0 if t % 3 else ((2 << t) - 1) & ~(1 << 20) for t in range(64)] + [(2 << t) - 1 for t in range(39)] + [0b1011 | 1 << 50]
+    check_attend(B, c, 128, [64, 40], masks=masks, seed=43)
+
+
+@pytest.mark.parametrize("dtype,d", DIMS[:3])
+def test_attend_lengths_far_apart(B, dtype, d):
+    """One long sequence among short and empty ones of the same capacity: it takes their share of the workgroups."""
+    lens = [1, 2000, 2, 33, 0, 5, 64, 1, 3, 1, 130, 1]
+    c = R.make_cache(8, d, 1, [2000] * 12, lens, dtype, 44)
+    check_attend(B, c, 8, [1] * 12, lam=0.9, seed=44)
+    check_attend(B, c, 8, [1] * 12, seed=45)
+    check_attend(B, c, 16, [1, 7, 2, 7, 3, 0, 7, 1, 3, 1, 7, 0], tree=True, seed=46)
+    c = R.make_cache(2, d, 2, [9000, 400], [300, 400], dtype, 47)
+    check_attend(B, c, 8, [1, 1], lam=0.5, seed=47)
+    check_attend(B, c, 8, [64, 3], tree=True, seed=48)
+
+
 @pytest.mark.parametrize("dtype,d", DIMS)
 @pytest.mark.parametrize("planes", [1, 3])
 def test_append(B, dtype, d, planes):
