@@ -366,15 +366,18 @@ structkv_status structkv_cache_append(const structkv_cache* cache, const void* k
  *   out[r][h] = sum_s a_s v[g][s],  a = softmax_s(x),  lse_out[r][h] = ln sum_s e^{x_s}
  * over the slots s that row t sees: all s < B_b, and B_b + j where bit j of tree_mask[r] is set (a tree of drafts: a draft's
  * ancestors and itself); tree_mask NULL: B_b + j for j <= t.  A row that sees nothing gets out 0 and lse_out -infinity.  Bits from
- * T_b on are ignored.  What fresh slots hold, NaN among it, does not reach rows that do not see them.
+ * T_b on are ignored.  What fresh slots hold, NaN among it, does not reach rows that do not see them; a row that sees a fresh slot
+ * whose values are not all finite gets NaN throughout.
  * lambda in (0, 1] (only with T_b <= 1 everywhere): the weights are gathered,
  *   mass[p][s] = lambda * mass[p][s] + sum of a_s over the plane's query heads, for the slots in use of sequences with T_b = 1.
  * lambda = 0: mass stays as it is.  Drafts gather theirs when they are accepted (structkv_cache_accept).
  * q: element (r, h, c) at r*q_stride_tok + h*q_stride_head + c; out [new][H_q][d] contiguous; lse_out [new][H_q] fp32.
- * scale: >= 0, 0 selects 1/sqrt(head_dim).  slopes: DEVICE fp32 [H_q] or NULL, needs pos.  cu_new: HOST [batch+1].
+ * scale: >= 0, 0 selects 1/sqrt(head_dim); 4 scale / softcap must be finite in fp32.  slopes: DEVICE fp32 [H_q] or NULL, needs pos.
+ * cu_new: HOST [batch+1].
  * A sequence with lens[b] < T_b is one whose rows see nothing.
- * Deterministic.  bf16 with head_dim 64 or 128, 16-byte aligned pointers and strides of whole 16 bytes goes through the bf16
- * matrix kernels, the rest through fp32 ones.
+ * Deterministic: the same call on the same lengths gives the same bits.  (Sums are cut by the lengths of the whole batch, so a sequence's
+ * last bits may differ in other company.)  bf16 with head_dim 64 or 128, 16-byte aligned pointers and strides of whole 16 bytes goes
+ * through the bf16 matrix kernels, the rest through fp32 ones.
  */
 structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_heads, float scale, float softcap,
                                       const float* slopes, const void* q, int64_t q_stride_tok, int64_t q_stride_head,
@@ -385,7 +388,7 @@ structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_h
  * The verified part of the drafts stays.  path[cu_new[b] + i], i < A_b = n_accept[b], are the accepted fresh tokens t of
  * sequence b (path NULL: i; n_accept NULL: all T_b):
  *   mass[p][s] = lambda * mass[p][s] + sum over i and the plane's query heads of e^{x_s - lse[cu_new[b] + path[i]][h]},
- *                s < lens[b], x and what a row sees as in structkv_cache_attend, which gave lse   (lambda = 0: left out)
+ *                s < lens[b], x and what a row sees as in structkv_cache_attend, which gave lse   (lambda = 0, or T_b = 0: left out)
  *   slot B_b + i  <-  slot B_b + path[i]   for keys, values, mass and pos, as if all were read before any is written
  *   lens_out[b] = B_b + A_b
  * The other drafts' slots are no longer in use.  q, strides, cu_new, tree_mask, scale, softcap, slopes as in the attend call;

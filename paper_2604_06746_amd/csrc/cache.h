@@ -196,9 +196,9 @@ __device__ __forceinline__ void leave(const AttendWork& w, int d, int g, int r, 
   const int head = g * w.gs + (r - t * w.gs);
   const int64_t at = (int64_t)(new0 + t) * w.H + head;
   if (nc == 1 && !w.x) {
-    const float inv = z > 0.f ? 1.f / z : 0.f;
+    const float inv = z != 0.f ? 1.f / z : 0.f;   // (NaN stays NaN)
     for (int i = 0; i < 4 && c + i < d; ++i) put_out<T>((T*)w.out + at * d + c + i, o[i] * inv);
-    if (c == 0) w.lse[at] = z > 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
+    if (c == 0) w.lse[at] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
   } else {
     *reinterpret_cast<floatx4*>(w.o + part * DP + c) = o;
     if (c == 0) { w.ml[part * 2] = top; w.ml[part * 2 + 1] = z; }

@@ -88,6 +88,8 @@ structkv_status check_scores(const structkv_cache* c, int32_t H, float scale, fl
   if (st != STRUCTKV_OK) return st;
   if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(STRUCTKV_ERR_INVALID_ARG, "scale must be finite and >= 0 (0 = 1/sqrt(head_dim))");
   if (!(softcap >= 0.f) || !std::isfinite(softcap)) return fail(STRUCTKV_ERR_INVALID_ARG, "softcap must be finite and >= 0 (0 = none)");
+  if (softcap > 0.f && !std::isfinite((scale > 0.f ? scale : 1.f) / softcap * 4.f))
+    return fail(STRUCTKV_ERR_UNSUPPORTED, "scale / softcap leaves fp32's range");
   if (!(lambda >= 0.f && lambda <= 1.f)) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda must be in [0,1]");
   if (lambda > 0.f && !c->mass) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda > 0 needs the cache's mass");
   if (slopes && !c->pos) return fail(STRUCTKV_ERR_INVALID_ARG, "slopes need the cache's pos");

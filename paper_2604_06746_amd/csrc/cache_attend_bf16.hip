@@ -140,6 +140,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   // from here on rows differ in what they see: the first fresh slot, or the end
   const int edge = min(s1, f.tree || h.fresh > 1 ? max(h.base, 0) : n);
   const QuickCap cap(f);
+  uint64_t odd = 0;   // fresh slots whose values are not all numbers
 
   for (int i = 0; i < mine; ++i) {
     const int j0 = s0 + 32 * (wave + kAttendWaves * i), next = j0 + 32 * kAttendWaves;
@@ -246,20 +247,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
       Z[rb] += z;
     }
     if (i + 1 < mine) wait_loads<NS + NK>(); else wait_loads<NS>();
-    if (ragged && h.base >= 0 && j0 + 32 > h.base) {   // fresh slots that are not numbers would reach rows that do not see them (0 x NaN)
-      typedef __attribute__((ext_vector_type(8))) uint16_t u16x8;
-#pragma unroll
-      for (int u = 0; u < NI; ++u) {
-        u16x8* piece = reinterpret_cast<u16x8*>(vt + (u * 64 + lane) * 16);
-        if (j0 + (u * 64 + lane) / SEGS >= h.base) {
-          u16x8 v = *piece;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = (v[e] & 0x7F80) == 0x7F80 ? 0 : v[e];
-          *piece = v;
-        }
-      }
-      wait_lds();
-    }
+    if (h.base >= 0 && j0 + 32 > h.base) odd |= clear_odd_values<SEGS, NI>(vt, j0 - h.base, h.fresh, 0);
     // (the swizzle is a whole number of 32-byte pairs, so the block of components enters the address as an exclusive or)
     const int vs = 4 * q4 + (l16 >> 2);
     const uint32_t va = (uint32_t)(uintptr_t)(lds_ptr_t)vt + (vs * SEGS + (((l16 >> 1) & 1) ^ swz_v(vs))) * 16 + (l16 & 1) * 8;
@@ -276,6 +264,12 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
         }
     }
     if (i + 1 < mine) fetch_v(next);   // (read_columns has waited)
+  }
+  if (odd) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) O[db][rb] *= mask[rb] & odd ? NAN : 1.f;
   }
   finish_chunk<uint16_t, D, RB>(O, M, Z, reinterpret_cast<float*>(lds), w, D, p.g, row0, rows, new0, p.nc);
 }

@@ -108,6 +108,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
     }
   };
   int j0 = s0 + wave * kTile;
+  uint64_t odd = 0;
   if (j0 < s1) fetch(j0);
   const int at = pos && n > 0 ? pos[h.base + t] : 0;
   for (; j0 < s1; j0 += kAttendWaves * kTile) {
@@ -118,7 +119,12 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
       floatx4 v = vr[u];
       if (j0 + s >= h.base) {   // a fresh slot: what is not a number would reach rows that do not see it (0 x NaN)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = fabsf(v[i]) < INFINITY ? v[i] : 0.f;
+        for (int i = 0; i < 4; ++i) {
+          if (!(fabsf(v[i]) < INFINITY)) {
+            v[i] = 0.f;
+            if (j0 + s < n) odd |= 1ull << (j0 + s - h.base);   // (rows that see it get NaN in the end)
+          }
+        }
       }
       *reinterpret_cast<floatx4*>(kt + s * W + col) = kr[u];
       *reinterpret_cast<floatx4*>(vt + s * W + col) = v;
@@ -152,6 +158,11 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
       for (int i = 0; i < 4; ++i)
         O[db][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[(4 * q4 + i) * W + db * 16 + l16], pr[i], O[db][0], 0, 0, 0);
     }
+  }
+  if (__any(odd != 0)) {
+    for (int m = 1; m < 64; m <<= 1) odd |= (uint64_t)__shfl_xor((unsigned long long)odd, m);
+#pragma unroll
+    for (int db = 0; db < DP / 16; ++db) O[db][0] *= mask & odd ? NAN : 1.f;
   }
   finish_chunk<T, DP, 1>(O, M, Z, lds, w, c.d, p.g, row0, rows, new0, p.nc);
 }

@@ -32,6 +32,49 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
+// A tile of V whose first slot is fresh slot `first` (or lies that far before them): what is not a number in fresh slots would reach rows
+// that do not see them (0 x NaN), so there are zeros in its place; the fresh slots where there was some are returned, and rows that see one
+// of those get NaN in the end.  By the lanes of a wave, PIECES of 64 units from `from` on.  The usual tile, which has none, costs a look.
+template <int SEGS, int PIECES>
+__device__ __forceinline__ uint64_t clear_odd_values(uint8_t* vt, int first, int fresh, int from) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t four;
+  constexpr int ROWS = 64 / SEGS;
+  const int lane = threadIdx.x & 63;
+  uint32_t any = 0;
+#pragma unroll
+  for (int u = 0; u < PIECES; ++u) {
+    const four v = *reinterpret_cast<const four*>(vt + ((from + u) * 64 + lane) * 16);
+    uint32_t odd = 0;   // a half's exponent of ones carries into its sign's place
+#pragma unroll
+    for (int e = 0; e < 4; ++e) odd |= (v[e] & 0x7F807F80u) + 0x00800080u;
+    any |= first + (from + u) * ROWS + lane / SEGS >= 0 ? odd & 0x80008000u : 0u;
+  }
+  if (!__any(any != 0)) return 0;
+  uint64_t odd_slots = 0;
+#pragma unroll 1
+  for (int u = from; u < from + PIECES; ++u) {
+    four* piece = reinterpret_cast<four*>(vt + (u * 64 + lane) * 16);
+    four v = *piece;
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool low = (v[e] & 0x7F80u) == 0x7F80u, high = (v[e] & 0x7F800000u) == 0x7F800000u;
+      odd |= low || high;
+      v[e] &= (low ? 0xFFFF0000u : ~0u) & (high ? 0xFFFFu : ~0u);
+    }
+    odd &= first + u * ROWS + lane / SEGS >= 0;
+    if (odd) *piece = v;
+    const uint64_t lanes = __ballot(odd);
+#pragma unroll 1
+    for (int r = 0; r < ROWS; ++r) {
+      const int s = first + u * ROWS + r;
+      if (((lanes >> (r * SEGS)) & ((1ull << SEGS) - 1)) && s < fresh) odd_slots |= 1ull << s;
+    }
+  }
+  wait_lds();
+  return odd_slots;
+}
+
 enum { kPlain = 0, kCapped = 1, kBiased = 2 };   // how scores are formed: scaled; capped; in full
 // Up to this cap its quick form is taken, whose error of cap x 2^-22 is a weight's relative one: 2^-14 here, a 64th of a bf16 rounding.
 constexpr float kLargestQuickCap = 256.f;

@@ -62,9 +62,9 @@ __device__ __forceinline__ Row row_of(const TAB& tab, const CacheView& c, const 
 }
 template <class T>
 __device__ __forceinline__ void put_row(const AttendWork& w, int64_t at, int d, int col, floatx4 o, float top, float z) {
-  const float inv = z > 0.f ? 1.f / z : 0.f;
+  const float inv = z != 0.f ? 1.f / z : 0.f;   // (NaN stays NaN)
   for (int e = 0; e < 4 && col + e < d; ++e) put_out<T>((T*)w.out + at * d + col + e, o[e] * inv);
-  if (col == 0) w.lse[at] = z > 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
+  if (col == 0) w.lse[at] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
 }
 
 // FEW: a lane group of DP / 4 a row, for sequences that have some kFewChunks chunks when all are full (more, in rounds, where the others are
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
     for (int j = 0; j < kAhead; ++j) {
       if (i0 + 4 * j >= heads) break;
       const float top = wave_top(a[j][0]), z = wave_total(a[j][1] * __builtin_amdgcn_exp2f(a[j][0] - top));
-      if (lane == 0) norms[i0 + 4 * j] = z > 0.f ? top + __builtin_amdgcn_logf(z) : INFINITY;
+      if (lane == 0) norms[i0 + 4 * j] = z != 0.f ? top + __builtin_amdgcn_logf(z) : INFINITY;
     }
   }
   __syncthreads();

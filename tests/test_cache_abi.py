@@ -95,7 +95,7 @@ def test_attend_refusals(B):
                 dict(q=None), dict(q=P + 1), dict(st=-1), dict(sh=-8), dict(cu=None), dict(cu=i64(0, 3, 1)), dict(cu=i64(2, 3, 4)),
                 dict(lam=0.9, cu=i64(0, 2, 3)), dict(out=None), dict(out=P + 1), dict(lse=None), dict(lse=P + 2)):
         assert call(**bad) == 1, (bad, B.structkv_last_error())
-    assert call(H=8192) == 2 and call(cu=i64(0, 65, 66)) == 2
+    assert call(H=8192) == 2 and call(cu=i64(0, 65, 66)) == 2 and call(cap=1e-41) == 2 and call(scale=1e10, cap=1e-29) == 2
     assert call(ws=None) == 3 and call(ws=P + 128) == 3 and call(size=100, lam=0.9) == 3
     assert call(cu=i64(0, 0, 0), q=None, out=None, lse=None, ws=None) == 0 and call(changes=dict(batch=0), cu=i64(0), ws=None) == 0
 
@@ -109,7 +109,7 @@ def test_accept_refusals(B):
                 dict(changes=dict(mass=None)), dict(q=None), dict(lse=None), dict(lse=P + 1), dict(path=P + 2), dict(n=P + 1), dict(st=-1),
                 dict(cu=None), dict(cu=i64(0, 3, 1)), dict(out=None), dict(out=P), dict(out=Q + 2), dict(tree=P + 1)):
         assert call(**bad) == 1, (bad, B.structkv_last_error())
-    assert call(cu=i64(0, 65, 66)) == 2
+    assert call(cu=i64(0, 65, 66)) == 2 and call(cap=1e-41) == 2
     assert call(changes=dict(batch=0), cu=i64(0)) == 0
 
 

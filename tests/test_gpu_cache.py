@@ -175,6 +175,31 @@ def test_attend_rows_that_see_nothing(B, dtype, d):
     check_attend(B, c, 4, [4, 4, 1], masks=masks, seed=11)
 
 
+@pytest.mark.parametrize("dtype,d,G,H,T", [(torch.bfloat16, 128, 2, 4, 5), (torch.bfloat16, 64, 2, 10, 5), (torch.float32, 64, 2, 4, 5),
+                                           (torch.bfloat16, 80, 2, 4, 5), (torch.bfloat16, 128, 32, 128, 20), (torch.bfloat16, 64, 2, 4, 1)])
+def test_attend_values_that_are_not_numbers(B, dtype, d, G, H, T):
+    """Rows that see them are not numbers either, the others are what they would be: a fresh value, a fresh key, a key among the old ones."""
+    bad = min(3, T - 1)
+    for caps, lens in (([3000, 40, 70], [2900, 40, 60]), ([3008, 32, 64], [3008, 32, 64])):
+        c = R.make_cache(G, d, 1, caps, lens, dtype, 51)
+        cu_new = R.cut([T] * 3)
+        q, q_gpu = queries(3 * T, H, d, dtype, 51)
+        ref, ref_lse, _, size = R.attend(c, H, q, cu_new, None, 0.0, 0.0, None, 0.0)
+        c.v[:, lens[0] - T + bad, 1] = math.inf
+        c.k[:, c.cu[1] + lens[1] - T + bad] = math.nan
+        c.k[:, c.cu[2] + 7, 0] = math.nan
+        on = OnGpu(B, c)
+        out, lse = torch.empty(3 * T, H, d, dtype=dtype, device="cuda"), torch.empty(3 * T, H, device="cuda")
+        B.structkv_cache_attend(on.handle, H, q_gpu, cu_new, out, lse, on.workspace(B, H, 3 * T), lam=0.9 if T == 1 else 0.0)
+        got, got_lse = out.cpu().double(), lse.cpu().double()
+        assert torch.isnan(got[bad:T]).all() and torch.isnan(got[T + bad:]).all()
+        assert torch.isnan(got_lse[T + bad:]).all()
+        a_err = 2 * score_error(c, q, 1 / math.sqrt(d), float(ref_lse.abs().max()) + 16) + (3008 / 16 + 64) * 2.0 ** -24
+        fine = [r for r in range(2 * T) if r % T < bad]
+        within(got_lse[fine + list(range(bad, T))], ref_lse[fine + list(range(bad, T))], a_err + 2.0 ** -22 * ref_lse[fine + list(range(bad, T))].abs(), "lse")
+        within(got[fine], ref[fine], EPS[dtype] * ref[fine].abs() + (2 * a_err + 2.0 ** -16) * size[fine], "out")
+
+
 def test_attend_large_scores(B):
     """Scores that grow along the cache by far more than 2^8 at a time, and ones of hundreds."""
     for dtype in (torch.bfloat16, torch.float32):
