@@ -7,7 +7,7 @@
 // the one before are formed, and its first half's values are while the second half's weights are: per tile 24 matrix instructions of
 // 32 cycles and some 150 others of 4, which one wave alone would do in turns.
 //
-// Bound by the matrix units at the clock that they leave: four trees of 64 drafts over 12K to 16.5K slots (52 GFLOP; with the weights' second
+// Bound by the matrix units at the clock that they leave: four trees of 64 drafts over 8K to 16.5K slots (52 GFLOP; with the weights' second
 // part 78) 92 us, 850 TFLOP/s of matrix instructions.  Four waves with tiles of their own and 16x16x32 instructions: 106 to 113 us.
 #include "cache_bf16.h"
 

@@ -424,7 +424,6 @@ __global__ __launch_bounds__(kThreads) void cache_evict_place_kernel(TAB tab, Ca
   uint32_t tie_rank = total(mine, sh[3]), hole_at = total(holes, sh[4]), move_at = total(moves, sh[5]);
   all_moves = total(all_moves, sh[6]);
   if (s.blk == 0 && threadIdx.x == 0) w.count[blockIdx.y * tab.batch + s.b] = (int32_t)all_moves;
-  const int lane = threadIdx.x & 63;
   for (int j0 = s.lo; j0 < s.hi; j0 += kThreads) {
     const int j = j0 + threadIdx.x;
     const bool in = j < s.hi;
@@ -447,7 +446,6 @@ __global__ __launch_bounds__(kThreads) void cache_evict_place_kernel(TAB tab, Ca
     hole_at += all_holes;
     move_at += moved_here;
   }
-  (void)lane;
 }
 
 constexpr int64_t kRowBlocks = 8192;   // workgroups that move rows, at most
@@ -455,8 +453,8 @@ constexpr int64_t kRowBlocks = 8192;   // workgroups that move rows, at most
 // ---- rows -----------------------------------------------------------------------------------------------------------------------
 // blockIdx.y: KV head and tensor, blockIdx.z: sequence; a thread per unit of a moved row at a time, and the first one of a key's row, of a plane's
 // first head, also moves the slot's mass and position.  How many rows move is known on the device alone: workgroups for all
-// that might would mostly find nothing (16 caches of 8 heads, 40 % of the possible rows move: 57.9 us, and 47.8 with the 8192 workgroups here, 52.6 with 2048), so a few go
-// through them in turns.
+// that might would mostly find nothing (16 caches of 8 heads, 40 % of the possible rows move: 57.9 us, and 47.8 with the 8192 workgroups
+// here, 52.6 with 2048), so a few go through them in turns.
 template <class TAB, class V>
 __global__ __launch_bounds__(256) void cache_evict_rows_kernel(TAB tab, CacheView c, EvictWork w, int elem_bytes, uint32_t units_per_row) {
   short_kernel_priority();
