@@ -22,7 +22,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
   constexpr int KS = D / 32, SEGS = D / 8, TILE = 32 * D * 2, NI = TILE / 1024;
   constexpr int POS = MODE == kBiased ? 256 : 0, NK = NI + (POS ? 1 : 0), SLOT = TILE + POS;
   typedef __attribute__((ext_vector_type(4))) int intx4;
-  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];   // two places a wave, what it knows of its rows, [4][stretch] sums
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];   // two places a wave, what it knows of its rows, [head_waves][stretch] sums
   const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   int b = 0;
@@ -42,11 +42,13 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
   float* row_slope = row_norm + 64;
   int* row_at = reinterpret_cast<int*>(row_norm + 128);
   int* row_token = reinterpret_cast<int*>(row_norm + 192);
-  float* sums = reinterpret_cast<float*>(lds + 4 * (2 * SLOT + kRowBytes)) + wave * stretch;
-  for (int s = lane; s < stretch; s += 64) sums[s] = 0.f;
   const int32_t* pos = MODE == kBiased && f.slopes ? c.pos + (int64_t)plane * c.slots + h.lo : nullptr;
   // this wave's heads and tiles
   const int tile_waves = 4 / head_waves, hw = wave / tile_waves, tw = wave % tile_waves;
+  float* all = reinterpret_cast<float*>(lds + 4 * (2 * SLOT + kRowBytes));
+  float* sums = all + hw * stretch;
+  for (int s = threadIdx.x; s < head_waves * stretch; s += 256) all[s] = 0.f;
+  __syncthreads();
   const int g0 = c.planes > 1 ? plane : 0, g1 = c.planes > 1 ? plane + 1 : c.G;
   const int tiles = (s1 - s0 + 31) / 32, mine = tiles > tw ? (tiles - tw + tile_waves - 1) / tile_waves : 0;
   const QuickCap cap(f);
@@ -167,11 +169,12 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
     }
   }
   __syncthreads();
-  const float* all = reinterpret_cast<const float*>(lds + 4 * (2 * SLOT + kRowBytes));
   float* mass = c.mass + (int64_t)plane * c.slots + h.lo;
   for (int s = s0 + threadIdx.x; s < s1; s += 256) {
     const int i = s - s0;
-    mass[s] = fmaf(w.lambda, mass[s], (all[i] + all[stretch + i]) + (all[2 * stretch + i] + all[3 * stretch + i]));
+    float sum = all[i];
+    for (int h = 1; h < head_waves; ++h) sum += all[h * stretch + i];
+    mass[s] = fmaf(w.lambda, mass[s], sum);
   }
 }
 
@@ -180,11 +183,13 @@ hipError_t weights(const CacheTable& t, const CacheView& c, const ScoreForm& f, 
                    const int32_t* n_accept, hipStream_t st) {
   // waves by heads: as many as there are heads for one mass
   const int heads = c.planes > 1 ? 1 : c.G, head_waves = heads >= 4 ? 4 : heads >= 2 ? 2 : 1;
-  // slots of a workgroup: at least a tile for every wave; longer ones, up to 512, where that leaves 512 workgroups (twice the CUs)
+  // slots of a workgroup: at least a tile for every wave; longer ones where that leaves 512 workgroups (twice the CUs), up to 512, or 1024 where the
+  // waves share the tiles (eight caches of 8K to 16.5K slots, 8 planes: 46.4 -> 44.7 us; 1536 and 2048 slots 49)
   int64_t all = 0;
   for (int b = 0; b < t.batch; ++b) all += t.cu[b + 1] - t.cu[b];
   const int least = 32 * (4 / head_waves);
-  int stretch = (int)std::max<int64_t>(least, std::min<int64_t>(512, all * c.planes / 512 / 32 * 32));
+  const int64_t most = head_waves == 1 ? 1024 : 512;
+  int stretch = (int)std::max<int64_t>(least, std::min<int64_t>(most, all * c.planes / 512 / 32 * 32));
   const bool stream = all * c.G * D * 2 >= kStreamBytes;
   CacheTable u = t;
   u.units[0] = 0;
@@ -193,7 +198,7 @@ hipError_t weights(const CacheTable& t, const CacheView& c, const ScoreForm& f, 
   with_cache_table(u, [&](const auto& tab) {
     with_mode(f, [&](auto mode) {
       constexpr int MODE = decltype(mode)::value;
-      const size_t lds = 4 * (2 * (32 * D * 2 + (MODE == kBiased ? 256 : 0)) + kRowBytes + sizeof(float) * stretch);   // 80 KB at most
+      const size_t lds = 4 * (2 * (32 * D * 2 + (MODE == kBiased ? 256 : 0)) + kRowBytes) + sizeof(float) * head_waves * stretch;   // 80 KB at most
       using TAB = std::decay_t<decltype(tab)>;
       const dim3 grid((unsigned)u.units[t.batch], (unsigned)c.planes);
       if (stream) cache_weights_bf16_kernel<TAB, D, MODE, true><<<grid, 256, lds, st>>>(tab, c, f, w, path, n_accept, stretch, head_waves);
