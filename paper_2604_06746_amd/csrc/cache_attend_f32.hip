@@ -5,7 +5,13 @@
 // 2^(x-M) and O = sum 2^(x-M) v, and rescales Z and O when M grows.  S^T = K Q^T puts a row's scores of 16 slots into four lanes,
 // four consecutive slots each, which is how the second product, O^T = V^T P^T, wants its right operand: P never leaves the lane.
 // A wave works on its own tiles of 16 slots (LDS of its own, no barrier in the loop), the next tile's rows are loaded into registers
-// meanwhile; the four waves of a workgroup take turns at a chunk's tiles and are joined at its end (finish_chunk).
+// meanwhile; the four waves of a workgroup take turns at a chunk's tiles and are joined at its end (finish_chunk).  M follows lazily, as in
+// cache_attend_bf16.hip: the usual tile has no exchange between lanes and no rescaling.
+//
+// Single tokens are bound by reading the cache (8 x 32768 slots of 8 heads, 128 components: 338 us, 6.4 TB/s), trees by the waits between matrix
+// and other instructions of two waves a SIMD (64 drafts over 8192 slots 129 us, 67 TFLOP/s of 154; 13 over four times 12.9K 228 us).  On these two, lazy M
+// gave 142 -> 136 and 247 -> 233, the priority the rest; two blocks of rows a workgroup 155 and 254 (registers), operands straight from memory
+// 151 and 270.
 #include "cache.h"
 
 namespace skv {
@@ -43,6 +49,7 @@ __device__ __forceinline__ void wave_lds_fence() {
 }
 
 constexpr int kTile = 16;
+constexpr float kSlack = 8.f;   // how far above its reference a score may lie, log2
 
 // S^T of a tile in LDS against 16 rows held as operands: lane l gets row l % 16, slots 4 (l / 16) .. +3.  Four sums that are added up at the
 // end: a score of 45 is a dot product of 500, whose 128 terms added one behind the other are off by three times as much.
@@ -130,8 +137,11 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
       *reinterpret_cast<floatx4*>(vt + s * W + col) = v;
     }
     wave_lds_fence();
+    __builtin_amdgcn_s_setprio(0);
     const int far[4] = {at - from[0], at - from[1], at - from[2], at - from[3]};
     if (j0 + kAttendWaves * kTile < s1) fetch(j0 + kAttendWaves * kTile);
+    // ahead of the other workgroup's waves until the tile is done, lest both be at the same instructions
+    __builtin_amdgcn_s_setprio(1);
     const floatx4 acc = tile_scores<DP>(kt, qf, l16, q4);
     float x[4];
 #pragma unroll
@@ -143,21 +153,24 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
       if (w.x && s < s1 && row0 + l16 < rows) w.x[head * w.xs + h.lo + kScorePad * p.b + s] = x[i];
     }
     float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float Mn = fmaxf(M[0], top), shrink = __builtin_amdgcn_exp2f(M[0] - Mn);
-    M[0] = Mn;
+    if (__any(top - M[0] > kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float Mn = fmaxf(M[0], top), shrink = __builtin_amdgcn_exp2f(M[0] - Mn);
+      M[0] = Mn;
+      Z[0] *= shrink;
+#pragma unroll
+      for (int db = 0; db < DP / 16; ++db) O[db][0] *= shrink;
+    }
     float pr[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_exp2f(x[i] - Mn);
-    Z[0] = Z[0] * shrink + ((pr[0] + pr[1]) + (pr[2] + pr[3]));
+    for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_exp2f(x[i] - M[0]);
+    Z[0] += (pr[0] + pr[1]) + (pr[2] + pr[3]);
 #pragma unroll
-    for (int db = 0; db < DP / 16; ++db) {
-      O[db][0] *= shrink;
+    for (int db = 0; db < DP / 16; ++db)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         O[db][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[(4 * q4 + i) * W + db * 16 + l16], pr[i], O[db][0], 0, 0, 0);
-    }
   }
   if (__any(odd != 0)) {
     for (int m = 1; m < 64; m <<= 1) odd |= (uint64_t)__shfl_xor((unsigned long long)odd, m);
