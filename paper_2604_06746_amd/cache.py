@@ -16,7 +16,8 @@ class LayerCache:
 
     planes: 1 where all KV heads keep the same tokens, n_kv_heads where each evicts by its own mass.  Calls that change the lengths
     read one array of them and write the other, which is the current one from then on (`lens`): a captured step that is replayed has to
-    make an even number of such calls."""
+    make an even number of such calls.  The calls of one LayerCache share its workspace and lengths, so they belong on one stream, or in order.
+    max_new: most fresh tokens of a sequence in an attend call."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, capacities: Sequence[int], planes: int = 1,
                  max_new: int = B.STRUCTKV_MAX_DRAFTS, device="cuda"):

@@ -512,6 +512,61 @@ def test_captured_step(B):
     assert eager[3][-1].tolist() == [300, 300]
 
 
+@pytest.mark.parametrize("dtype,d,G,H,T", [(torch.bfloat16, 128, 32, 96, 23), (torch.bfloat16, 64, 2, 8, 7), (torch.float32, 64, 2, 8, 7)])
+def test_captured_drafts(B, dtype, d, G, H, T):
+    """Drafts appended, attended to and accepted in a graph, replayed while lengths, trees and paths change: as the eager calls, every time."""
+    c = R.make_cache(G, d, 1, [900, 2100], [300, 1200], dtype, 73)
+    g = torch.Generator(device="cuda").manual_seed(74)
+    cu_new = [0, T, 2 * T]
+
+    def fresh():
+        on = OnGpu(B, c)
+        lens = [on.lens, on.lens_out]
+        handles = [B.make_cache(on.k, on.v, c.cu, x, on.mass, on.pos) for x in lens]
+        ws = on.workspace(B, H, 2 * T)
+        normal = [torch.zeros(*s, dtype=dtype, device="cuda") for s in ((2 * T, H, d), (G, 2 * T, d), (G, 2 * T, d))]
+        whole = [torch.zeros(2 * T, dtype=torch.int64, device="cuda")] + [torch.zeros(n, dtype=torch.int32, device="cuda") for n in (2 * T, 2 * T, 2)]
+        out, lse = torch.empty(2 * T, H, d, dtype=dtype, device="cuda"), torch.empty(2 * T, H, device="cuda")
+
+        def step():
+            q, k_new, v_new = normal
+            mask, path, pos, n_accept = whole
+            B.structkv_cache_append(handles[0], k_new, v_new, cu_new, lens[1], pos_new=pos)
+            B.structkv_cache_attend(handles[1], H, q, cu_new, out, lse, ws, tree_mask=mask)
+            B.structkv_cache_accept(handles[1], H, q, lse, cu_new, lens[0], path, n_accept, mask, lam=0.9)
+        return on, step, normal, whole, (out, lse, on.k, on.v, on.mass, on.pos, on.lens)
+
+    eager, replayed = fresh(), fresh()
+    start = [x.clone() for x in replayed[4]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        replayed[1]()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        replayed[1]()
+    for x, y in zip(replayed[4], start):
+        x.copy_(y)
+    rng, grown = np.random.default_rng(75), np.array([300, 1200])
+    for i in range(30):
+        taken = rng.integers(0, T + 1, 2)
+        grown += taken
+        inputs = [torch.randn(x.shape, generator=g, device="cuda").to(dtype) for x in eager[2]]
+        masks = R.as_int64(R.random_tree(T, rng) + R.random_tree(T, rng))
+        whole = [masks, torch.from_numpy(rng.integers(0, T, 2 * T)), torch.arange(2 * T) + 9000 + 100 * i, torch.from_numpy(taken)]
+        for side_of in (eager, replayed):
+            for x, y in zip(side_of[2] + side_of[3], inputs + whole):
+                x.copy_(y)
+        eager[1]()
+        graph.replay()
+        torch.cuda.synchronize()
+        for j, (x, y) in enumerate(zip(eager[4], replayed[4])):
+            assert torch.equal(x.nan_to_num(), y.nan_to_num()), (i, j)
+        assert eager[4][-1].tolist() == grown.tolist()
+
+
 def test_another_stream(B):
     """Calls on a stream of their own, two at once with workspaces of their own."""
     c = R.make_cache(2, 128, 1, [3000], [2900], torch.bfloat16, 81)
@@ -527,6 +582,62 @@ def test_another_stream(B):
     for i in (1, 2):
         assert torch.equal(outs[0][0], outs[i][0]) and torch.equal(outs[0][1], outs[i][1]) and torch.equal(sides[0].mass, sides[i].mass)
         assert torch.equal(sides[0].k.nan_to_num(), sides[i].k.nan_to_num())
+
+
+@pytest.mark.parametrize("dtype,d,G,H,pad,T", [(torch.bfloat16, 128, 2, 8, 1 << 24, 7), (torch.bfloat16, 64, 32, 128, 1 << 20, 20),
+                                              (torch.float32, 64, 2, 4, 1 << 25, 5), (torch.bfloat16, 1, 2, 4, 1 << 22, 3)])
+def test_behind_a_long_cache(B, dtype, d, G, H, pad, T):
+    """Slots whose elements lie beyond 2^31 (a sequence of `pad` slots before them, empty): as in a cache of their own.  The copies are exact;
+    two results of the same sums differ by twice what either may be off."""
+    c = R.make_cache(G, d, G, [2100], [2000], dtype, 61)
+    new, cu_new, budget = T + 1, [0, 0, T], 1500
+    small = OnGpu(B, c)
+    big = OnGpu.__new__(OnGpu)
+    big.k, big.v = (torch.full((G, pad + 2100, d), math.nan, dtype=dtype, device="cuda") for _ in range(2))
+    big.mass, big.pos = torch.zeros(G, pad + 2100, device="cuda"), torch.zeros(G, pad + 2100, dtype=torch.int32, device="cuda")
+    for name in ("k", "v", "mass", "pos"):
+        getattr(big, name)[:, pad:] = getattr(small, name)
+    q, q_gpu = queries(T, H, d, dtype, 61)
+    g = torch.Generator(device="cuda").manual_seed(62)
+    k_new, v_new = (torch.randn(G, T, d, generator=g, device="cuda").to(dtype) for _ in range(2))
+    pos_new = torch.arange(20000, 20000 + T, device="cuda").int()
+    mask = R.as_int64(R.random_tree(T, np.random.default_rng(6))).cuda()
+    path = torch.arange(T - 1, -1, -1, device="cuda").int()
+    got = []
+    for on, cu, new_cu in ((small, [0, 2100], [0, T]), (big, [0, pad, pad + 2100], cu_new)):
+        n = len(cu) - 1
+        lens = [torch.tensor([0] * (n - 1) + [2000], dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")]
+        a, b = (B.make_cache(on.k, on.v, cu, x, on.mass, on.pos) for x in lens)
+        ws = torch.empty(B.structkv_cache_workspace_bytes(a, H, new), dtype=torch.uint8, device="cuda")
+        out, lse = torch.empty(T, H, d, dtype=dtype, device="cuda"), torch.empty(T, H, device="cuda")
+        one, one_lse = torch.empty(1, H, d, dtype=dtype, device="cuda"), torch.empty(1, H, device="cuda")
+        B.structkv_cache_append(a, k_new, v_new, new_cu, lens[1], pos_new=pos_new)
+        B.structkv_cache_attend(b, H, q_gpu, new_cu, out, lse, ws, tree_mask=mask, softcap=30.0)
+        B.structkv_cache_attend(b, H, q_gpu[:1], [0] * n + [1], one, one_lse, ws, lam=0.5)
+        mass = on.mass[:, cu[-2]:].clone()
+        on.mass[:, cu[-2]:] = small.c.mass.cuda()
+        B.structkv_cache_accept(b, H, q_gpu, lse, new_cu, lens[0], path, torch.tensor([0] * (n - 1) + [T - 1], dtype=torch.int32, device="cuda"), mask,
+                                softcap=30.0, lam=0.5)
+        accepted = on.mass[:, cu[-2]:].clone()
+        on.mass[:, cu[-2]:] = small.c.mass.cuda()
+        B.structkv_cache_evict(a, None, [0] * (n - 1) + [budget], 50, lens[1], ws)
+        assert lens[0].tolist()[-1] == 2000 + T - 1 and lens[1].tolist()[-1] == budget
+        got.append((out, one, lse, one_lse, mass, accepted, on.k[:, cu[-2]:], on.v[:, cu[-2]:], on.pos[:, cu[-2]:]))
+    for x, y in zip(got[0][6:], got[1][6:]):
+        assert torch.equal(x[:, :budget], y[:, :budget])
+    slots = slice(0, 2000)
+    x_max = float(got[0][2].abs().max()) + 16
+    a_err = 2 * score_error(c, q, 1 / math.sqrt(d), x_max) + (2100 / 16 + 64) * 2.0 ** -24
+    v_max = float(torch.nan_to_num(c.v.float(), 0.0, 0.0, 0.0).abs().max().clamp(min=float(v_new.abs().max())))
+    for x, y in zip(got[0][:2], got[1][:2]):
+        x, y = x.double(), y.double()
+        within(y.cpu(), x.cpu(), (2 * EPS[dtype] * x.abs() + 2 * (2 * a_err + 2.0 ** -16) * v_max).cpu(), "out")
+    for x, y in zip(got[0][2:4], got[1][2:4]):
+        x, y = x.double(), y.double()
+        within(y.cpu(), x.cpu(), 2 * (a_err + 2.0 ** -23 * x.abs()).cpu(), "lse")
+    for x, y in zip(got[0][4:6], got[1][4:6]):
+        x, y = x[:, slots].double(), y[:, slots].double()
+        within(y.cpu(), x.cpu(), 2 * ((2.0 ** -22 + 2 * a_err + 4 * x_max * 2.0 ** -24) * x.abs()).cpu(), "mass")
 
 
 def test_layer_cache_after_a_sweep(B):
