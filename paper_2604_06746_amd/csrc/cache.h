@@ -54,7 +54,7 @@ struct CacheView {
   int G, d, planes;
 };
 
-// How scores are formed: c2 = scale log2(e); with a cap or slopes in full (MORE in the kernels).
+// How scores are formed: c2 = scale log2(e); with a cap or slopes in full (kBiased, and kCapped where it is quick).
 struct ScoreForm {
   float scale, c2, softcap, inv_cap;
   const float* slopes;

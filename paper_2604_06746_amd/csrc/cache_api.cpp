@@ -145,7 +145,11 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
     stretches += gather ? ceil_div(cap, 64) * c->planes : 0;
     t->units[b + 1] = (int32_t)blocks;
   }
-  p->units = std::max(blocks, std::min(chunks, kAttendBlocks / c->n_kv_heads));
+  // Two a block of rows at least, so that long sequences of large batches are cut too, where that pays for the launch that joins them: 64
+  // sequences of 8192 slots 309 us without, 320 with, one of 8192 among 63 of 400 88 and 34; with gathered weights, where the join is there
+  // anyway, 64 of 2112 slots 113 and 114, one among short ones 41 and 25, but 64 of 300 27 and 31.
+  const bool cut = rows_wg == 16 && work >= (gather ? 1024. : 4096.) * (double)blocks;
+  p->units = std::max(blocks, std::min(chunks, std::max(kAttendBlocks / c->n_kv_heads, cut ? 2 * blocks : 0)));
   if (p->units * c->n_kv_heads >= ((int64_t)1 << 31) || stretches >= ((int64_t)1 << 30))
     return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
   p->join = gather || p->units > blocks;
@@ -169,7 +173,7 @@ size_t most_attend_bytes(const structkv_cache* c, int H, int64_t new_tokens, int
   const int64_t gs = H / c->n_kv_heads, rows = new_tokens * gs;
   const bool wide = c->dtype == STRUCTKV_DTYPE_BF16 && (c->head_dim == 64 || c->head_dim == 128);
   const int64_t rows_wg = !wide || rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
-  const size_t parts = (size_t)std::max(rows_wg * kAttendBlocks, 16 * new_tokens * ceil_div(gs, 16) * c->n_kv_heads);
+  const size_t parts = (size_t)std::max(rows_wg * kAttendBlocks, 2 * 16 * new_tokens * ceil_div(gs, 16) * c->n_kv_heads);
   return align_up(sizeof(int4) * (size_t)c->batch, 256) + align_up(parts * 2 * sizeof(float), 256) + align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256) +
          (c->mass ? score_bytes(H, slots, c->batch) : 0);
 }

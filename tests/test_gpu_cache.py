@@ -252,6 +252,8 @@ def test_attend_lengths_far_apart(B, dtype, d):
     check_attend(B, c, 8, [1] * 12, lam=0.9, seed=44)
     check_attend(B, c, 8, [1] * 12, seed=45)
     check_attend(B, c, 16, [1, 7, 2, 7, 3, 0, 7, 1, 3, 1, 7, 0], tree=True, seed=46)
+    c = R.make_cache(16, d, 1, [1100] * 40, [3] * 20 + [1100] + [0, 40] * 9 + [700], dtype, 49)    # more blocks of rows than half the workgroups
+    check_attend(B, c, 16, [1] * 40, lam=0.9, seed=49)
     c = R.make_cache(2, d, 2, [9000, 400], [300, 400], dtype, 47)
     check_attend(B, c, 8, [1, 1], lam=0.5, seed=47)
     check_attend(B, c, 8, [64, 3], tree=True, seed=48)
