@@ -330,6 +330,8 @@ typedef struct {
   const int32_t* lens;     /* DEVICE [batch] */
   const int64_t* cu_slots; /* HOST [batch+1], cu_slots[0] = 0, non-decreasing, capacities below 2^31 */
   int32_t batch;           /* 0 .. STRUCTKV_MAX_BATCH */
+  int32_t* missed;         /* DEVICE [batch], or NULL: set to 1 for a sequence that rows were to be appended to for which it had no room,
+                              and never cleared; while it is not 0, attend and accept take the sequence for one without fresh rows */
 } structkv_cache;
 
 /* Most fresh tokens of a sequence in structkv_cache_attend and structkv_cache_accept. */
@@ -348,7 +350,9 @@ size_t structkv_cache_workspace_bytes(const structkv_cache* cache, int32_t n_q_h
  *   pos[p][same slot]  = pos_new[p*new_stride_plane + r]               (both NULL: positions are not kept)
  *   mass[p][same slot] = mass_new ? mass_new[p*new_stride_plane + r] : 0   (skipped where the cache keeps no mass)
  * For a prefill's compact cache (k_dst, v_dst, idx_out of structkv_layer_step) as for the tokens of a decoding step.
- * A sequence whose rows do not fit its capacity is left as it was, lens_out[b] = lens[b].
+ * A sequence whose rows do not fit its capacity is left as it was, lens_out[b] = lens[b], and cache->missed[b] = 1.  The calls behind take
+ * its last slots in use for the fresh ones, unless they are told by `missed`: where it is NULL, the caller sees to it that rows fit.  To
+ * go on with such a sequence: make room, set missed[b] to 0, append again.
  * k_new, v_new: element (g, r, c) at g*new_stride_head + r*new_stride_tok + c.  cu_new: HOST [batch+1], cu_new[0] = 0,
  * non-decreasing.  new_stride_plane: 0 where the planes share pos_new and mass_new.  The new rows must not overlap the cache.
  */
@@ -374,7 +378,7 @@ structkv_status structkv_cache_append(const structkv_cache* cache, const void* k
  * q: element (r, h, c) at r*q_stride_tok + h*q_stride_head + c; out [new][H_q][d] contiguous; lse_out [new][H_q] fp32.
  * scale: >= 0, 0 selects 1/sqrt(head_dim); 4 scale / softcap must be finite in fp32.  slopes: DEVICE fp32 [H_q] or NULL, needs pos.
  * cu_new: HOST [batch+1].
- * A sequence with lens[b] < T_b is one whose rows see nothing.
+ * A sequence with lens[b] < T_b or missed[b] != 0 is one whose rows see nothing, and whose mass stays as it is.
  * Deterministic: the same call on the same lengths gives the same bits.  (Sums are cut by the lengths of the whole batch, so a sequence's
  * last bits may differ in other company.)  bf16 with head_dim 64 or 128, 16-byte aligned pointers and strides of whole 16 bytes goes
  * through the bf16 matrix kernels, the rest through fp32 ones.
@@ -393,7 +397,8 @@ structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_h
  *   lens_out[b] = B_b + A_b
  * The other drafts' slots are no longer in use.  q, strides, cu_new, tree_mask, scale, softcap, slopes as in the attend call;
  * with lambda = 0 q and lse may be NULL.  path, n_accept, lse: DEVICE.  A row whose lse is -infinity adds nothing; path entries
- * outside [0, T_b) and n_accept outside [0, T_b] are taken as the nearer bound; a sequence with lens[b] < T_b is left as it was.
+ * outside [0, T_b) and n_accept outside [0, T_b] are taken as the nearer bound; a sequence with lens[b] < T_b or missed[b] != 0 is left as
+ * it was.
  */
 structkv_status structkv_cache_accept(const structkv_cache* cache, int32_t n_q_heads, float scale, float softcap,
                                       const float* slopes, const void* q, int64_t q_stride_tok, int64_t q_stride_head,

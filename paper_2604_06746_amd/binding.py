@@ -51,7 +51,7 @@ class structkv_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride_head", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("planes", ctypes.c_int32),
                 ("mass", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("cu_slots", ctypes.c_void_p),
-                ("batch", ctypes.c_int32)]
+                ("batch", ctypes.c_int32), ("missed", ctypes.c_void_p)]
 
 
 class StructKVError(RuntimeError):
@@ -403,9 +403,10 @@ def _vector(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, index: in
 
 
 def make_cache(k: torch.Tensor, v: torch.Tensor, cu_slots: Sequence[int], lens: torch.Tensor, mass: Optional[torch.Tensor] = None,
-               pos: Optional[torch.Tensor] = None) -> structkv_cache:
+               pos: Optional[torch.Tensor] = None, missed: Optional[torch.Tensor] = None) -> structkv_cache:
     """k, v: [G, slots, d] views sharing strides, d contiguous; lens: int32 [batch]; mass fp32, pos int32: [planes, slots] (or [slots]),
-    planes = 1 or G.  The tensors are kept alive by the result; `lens` is read by the calls, whose lens_out is another tensor."""
+    planes = 1 or G; missed: int32 [batch], zeros, where an append leaves a mark for a sequence without room.  The tensors are kept
+    alive by the result; `lens` is read by the calls, whose lens_out is another tensor."""
     _require(k.dim() == 3 and v.dim() == 3 and v.shape == k.shape and v.stride() == k.stride() and v.dtype == k.dtype,
              "k and v must be [G, slots, d] views of one dtype that share shape and strides")
     _require(k.dtype in (torch.float32, torch.bfloat16), "k and v must be float32 or bfloat16")
@@ -424,12 +425,13 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, cu_slots: Sequence[int], lens: 
     _vector(mass, torch.float32, planes * total, index, "mass")
     _vector(pos, torch.int32, planes * total, index, "pos")
     _vector(lens, torch.int32, batch, index, "lens")
+    _vector(missed, torch.int32, batch, index, "missed")
     _require(v.device == k.device and index >= 0, "the cache must be on one GPU")
     host = _host_i64(cu_slots)
     code = STRUCTKV_DTYPE_BF16 if k.dtype == torch.bfloat16 else STRUCTKV_DTYPE_F32
     c = structkv_cache(_ptr(k), _ptr(v), k.stride(0), k.stride(1), G, d, code, planes, _ptr(mass), _ptr(pos), _ptr(lens),
-                       ctypes.addressof(host), batch)
-    c.tensors = (k, v, lens, mass, pos, host)
+                       ctypes.addressof(host), batch, _ptr(missed))
+    c.tensors = (k, v, lens, mass, pos, missed, host)
     c.tensor_dtype, c.device, c.index, c.slots = k.dtype, k.device, index, total
     return c
 

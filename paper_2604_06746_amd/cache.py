@@ -17,6 +17,8 @@ class LayerCache:
     planes: 1 where all KV heads keep the same tokens, n_kv_heads where each evicts by its own mass.  Calls that change the lengths
     read one array of them and write the other, which is the current one from then on (`lens`): a captured step that is replayed has to
     make an even number of such calls.  The calls of one LayerCache share its workspace and lengths, so they belong on one stream, or in order.
+    A sequence that has no room for what is appended stays as it was, and `missed` (int32 [batch] on the device) has a 1 for it: until the
+    program sets that back to 0, attend gives the sequence's rows zeros and accept leaves its tokens as they are.
     max_new: most fresh tokens of a sequence in an attend call."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, capacities: Sequence[int], planes: int = 1,
@@ -32,7 +34,8 @@ class LayerCache:
         self.mass = torch.zeros(planes, total, device=dev)
         self.pos = torch.zeros(planes, total, dtype=torch.int32, device=dev)
         self._lens = [torch.zeros(self.batch, dtype=torch.int32, device=dev) for _ in range(2)]
-        self._handles = [B.make_cache(self.k, self.v, self.cu, x, self.mass, self.pos) for x in self._lens]
+        self.missed = torch.zeros(self.batch, dtype=torch.int32, device=dev)
+        self._handles = [B.make_cache(self.k, self.v, self.cu, x, self.mass, self.pos, self.missed) for x in self._lens]
         self._now = 0
         size = B.structkv_cache_workspace_bytes(self._handles[0], n_q_heads, max_new * self.batch)
         if size == 0:
@@ -50,6 +53,7 @@ class LayerCache:
 
     def reset(self) -> None:
         self.lens.zero_()
+        self.missed.zero_()
 
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: Sequence[int], pos_new: torch.Tensor,
                mass_new: Optional[torch.Tensor] = None) -> None:

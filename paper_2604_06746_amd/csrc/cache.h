@@ -51,6 +51,7 @@ struct CacheView {
   float* mass;
   int32_t* pos;
   const int32_t* lens;
+  int32_t* missed;
   int G, d, planes;
 };
 
@@ -133,18 +134,19 @@ struct EvictWork {
 hipError_t launch_cache_evict(const CacheTable& t, const CacheView& c, const EvictWork& w, int elem_bytes, hipStream_t st);
 
 #ifdef __HIPCC__
-// a sequence's slots in use, and its fresh tokens' first slot; see: false where its rows see nothing
+// a sequence's slots in use, and its fresh tokens' first slot: negative where they are not there
 struct Held {
   int n, base, fresh;
   int64_t lo;
 };
 template <class TAB>
-__device__ __forceinline__ Held held(const TAB& t, const int32_t* lens, int b) {
+__device__ __forceinline__ Held held(const TAB& t, const CacheView& c, int b) {
   Held h;
   h.lo = t.cu[b];
-  h.n = max(0, (int)min((int64_t)lens[b], t.cu[b + 1] - t.cu[b]));
+  const int32_t len = c.lens[b], missed = c.missed ? c.missed[b] : 0;
+  h.n = max(0, (int)min((int64_t)len, t.cu[b + 1] - t.cu[b]));
   h.fresh = t.cu_new[b + 1] - t.cu_new[b];
-  h.base = h.n - h.fresh;
+  h.base = missed ? -1 : h.n - h.fresh;
   return h;
 }
 
@@ -268,18 +270,18 @@ __device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (ui
 // 16384: 171 and 182).  The length is the mean slots of a unit, made longer by a 16th until the chunks are no more than the units;
 // the host sees to it that one chunk each is not.
 struct Cuts {
-  uint32_t n;        // slots in use
+  uint32_t n;        // slots in use, 0 where the fresh tokens are not among them for want of room
   uint32_t rcs, nc;  // blocks of query rows, chunks
   uint32_t end;      // units of the sequences up to this one
   int len;           // slots of a chunk, whole tiles
 };
 template <class TAB>
-__device__ __forceinline__ Cuts cuts_of(const TAB& t, const int32_t* lens, const AttendWork& w) {
+__device__ __forceinline__ Cuts cuts_of(const TAB& t, const CacheView& cache, const AttendWork& w) {
   const int lane = threadIdx.x & 63, b = min(lane, t.batch - 1);
   Cuts c;
-  const int32_t len = lens[b], fresh = t.cu_new[b + 1] - t.cu_new[b];
+  const int32_t len = cache.lens[b], missed = cache.missed ? cache.missed[b] : 0, fresh = t.cu_new[b + 1] - t.cu_new[b];
   const int64_t cap = t.cu[b + 1] - t.cu[b];
-  c.n = (uint32_t)max(0, (int)min((int64_t)len, cap));
+  c.n = missed ? 0u : (uint32_t)max(0, (int)min((int64_t)len, cap));
   c.rcs = lane < t.batch ? (uint32_t)(t.units[b + 1] - t.units[b]) : 0u;
   const uint32_t tiles = (int)c.n < fresh ? 0u : (c.n + 31u) / 32u, units = (uint32_t)w.units;
   const uint64_t mine = (uint64_t)tiles * c.rcs;   // (below 2^26 x 2^18; the sums of its halves stay below 2^32)
@@ -306,7 +308,7 @@ struct AttendPlace {
 template <class TAB>
 __device__ __forceinline__ AttendPlace attend_place(const TAB& t, const CacheView& c, const AttendWork& w) {
   AttendPlace p;
-  const Cuts k = cuts_of(t, c.lens, w);
+  const Cuts k = cuts_of(t, c, w);
   const bool shifts = (c.G & (c.G - 1)) == 0;   // (a division costs some 40 instructions)
   const int u = shifts ? (int)(blockIdx.x >> __builtin_ctz(c.G)) : (int)(blockIdx.x / c.G);
   p.g = blockIdx.x - u * c.G;

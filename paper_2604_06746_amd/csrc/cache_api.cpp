@@ -44,8 +44,9 @@ structkv_status check_cache(const structkv_cache* c, CacheTable* t, CacheView* v
   if (slots > 0 && (!c->k || !c->v)) return fail(STRUCTKV_ERR_INVALID_ARG, "k or v is NULL");
   const uintptr_t esz = c->dtype == STRUCTKV_DTYPE_BF16 ? 2 : 4;
   if (((uintptr_t)c->k | (uintptr_t)c->v) & (esz - 1)) return fail(STRUCTKV_ERR_INVALID_ARG, "k or v is not aligned to its elements");
-  if (((uintptr_t)c->mass | (uintptr_t)c->pos) & 3) return fail(STRUCTKV_ERR_INVALID_ARG, "mass or pos is not 4-byte aligned");
-  *v = CacheView{c->k, c->v, c->n_kv_heads > 1 ? c->stride_head : 0, c->stride_slot, slots, c->mass, c->pos, c->lens,
+  if (((uintptr_t)c->mass | (uintptr_t)c->pos | (uintptr_t)c->missed) & 3)
+    return fail(STRUCTKV_ERR_INVALID_ARG, "mass, pos or missed is not 4-byte aligned");
+  *v = CacheView{c->k, c->v, c->n_kv_heads > 1 ? c->stride_head : 0, c->stride_slot, slots, c->mass, c->pos, c->lens, c->missed,
                  c->n_kv_heads, c->head_dim, c->planes};
   return STRUCTKV_OK;
 }

@@ -190,7 +190,7 @@ __global__ __launch_bounds__(256) void cache_weights_f32_kernel(TAB tab, CacheVi
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l16 = lane & 15, q4 = lane >> 4;
   int b = 0;
   while (b + 1 < tab.batch && (int)blockIdx.x >= tab.units[b + 1]) ++b;
-  const Held h = held(tab, c.lens, b);
+  const Held h = held(tab, c, b);
   const int j0 = (((int)blockIdx.x - tab.units[b]) * 4 + wave) * kTile;
   if (h.fresh == 0 || h.base < 0 || j0 >= h.n) return;
   const int n = h.n, new0 = tab.cu_new[b], plane = blockIdx.y;

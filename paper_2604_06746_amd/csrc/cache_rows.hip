@@ -35,7 +35,10 @@ __global__ __launch_bounds__(256) void cache_append_kernel(TAB tab, CacheView c,
   if (mine) x = load_once<V>((second ? v_new : k_new) + (g * nsh + (first + t) * nst) * elem_bytes + (int64_t)u * sizeof(V));
   const int n = max(0, (int)min((int64_t)c.lens[b], cap));   // (the row is on its way while the length is)
   const bool fits = n + (int64_t)fresh <= cap;
-  if (blockIdx.x == 0 && threadIdx.x == 0) lens_out[b] = fits ? n + (int)fresh : n;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    lens_out[b] = fits ? n + (int)fresh : n;
+    if (!fits && c.missed) c.missed[b] = 1;
+  }
   if (!mine || !fits) return;
   const int64_t slot = lo + n + t;
   *reinterpret_cast<V*>((uint8_t*)(second ? c.v : c.k) + (g * c.sh + slot * c.ss) * elem_bytes + (int64_t)u * sizeof(V)) = x;
@@ -55,7 +58,7 @@ __global__ __launch_bounds__(256) void cache_accept_kernel(TAB tab, CacheView c,
   short_kernel_priority();
   __shared__ int from[STRUCTKV_MAX_DRAFTS];
   const int b = blockIdx.x;
-  const Held h = held(tab, c.lens, b);
+  const Held h = held(tab, c, b);
   const bool whole = h.base >= 0;
   const int taken = !whole ? 0 : n_accept ? max(0, min(n_accept[b], h.fresh)) : h.fresh;
   if (blockIdx.y == 0 && blockIdx.z == 2 && threadIdx.x == 0) lens_out[b] = whole ? h.base + taken : h.n;

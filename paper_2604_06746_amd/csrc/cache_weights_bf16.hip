@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   int b = 0;
   while (b + 1 < tab.batch && (int)blockIdx.x >= tab.units[b + 1]) ++b;
-  const Held h = held(tab, c.lens, b);
+  const Held h = held(tab, c, b);
   // the path, a token a lane, and its length are on their way while the sequence's is
   const int new0 = tab.cu_new[b], accepted = n_accept ? n_accept[b] : 0;
   const int step = path && lane < h.fresh ? max(0, min(path[new0 + lane], h.fresh - 1)) : lane;

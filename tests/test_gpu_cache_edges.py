@@ -1,0 +1,103 @@
+"""GPU tests of the operators on a cache in use, beside test_gpu_cache.py: sequences without room, and values and sizes at their limits.
+
+Tolerances as derived there, unless a test says otherwise."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import cache_reference as R
+from test_gpu_cache import B, EPS, within  # noqa: F401  (B is the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def full_cache(dtype, d, G, H, planes, caps, lens, seed):
+    """A LayerCache that holds lens[b] tokens, and what it holds."""
+    from paper_2604_06746_amd.cache import LayerCache
+    c = R.make_cache(G, d, planes, caps, lens, dtype, seed)
+    cache = LayerCache(H, G, d, dtype, caps, planes)
+    for name in ("k", "v", "mass", "pos"):
+        getattr(cache, name).copy_(getattr(c, name))
+    cache.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    return cache, c
+
+
+def rows(G, H, d, new, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    return tuple(torch.randn(*s, generator=g).to(dtype) for s in ((G, new, d), (G, new, d), (new, H, d)))
+
+
+def same_slots(cache, c, b, n):
+    used = slice(c.cu[b], c.cu[b] + n)
+    for name in ("k", "v", "mass", "pos"):
+        assert torch.equal(getattr(cache, name)[:, used].cpu(), getattr(c, name)[:, used]), name
+
+
+@pytest.mark.parametrize("dtype,d,G,H,T", [(torch.bfloat16, 128, 2, 8, 4), (torch.bfloat16, 128, 32, 128, 40), (torch.float32, 64, 2, 4, 4),
+                                           (torch.bfloat16, 80, 2, 4, 7)])
+def test_drafts_that_do_not_fit(B, dtype, d, G, H, T):  # noqa: F811
+    """append, attend, accept in a row: the sequence without room loses nothing, its rows see nothing, its neighbour is what it is by itself."""
+    cache, c = full_cache(dtype, d, G, H, 1, [1300, 1400], [1298, 1200], 7)
+    cu_new, masks = [0, T, 2 * T], R.random_tree(T, np.random.default_rng(1)) + R.random_tree(T, np.random.default_rng(2))
+    k, v, q = rows(G, H, d, 2 * T, dtype, 8)
+    tree, path = R.as_int64(masks).cuda(), torch.zeros(2 * T, dtype=torch.int32, device="cuda")
+    cache.append(k.cuda(), v.cuda(), cu_new, torch.arange(2 * T, device="cuda").int() + 9000)
+    out, lse = cache.attend(q.cuda(), cu_new, tree)
+    cache.accept(cu_new, path, torch.tensor([1, 1], dtype=torch.int32, device="cuda"), q.cuda(), lse, tree, 0.9)
+    assert cache.lens.tolist() == [1298, 1201]
+    same_slots(cache, c, 0, 1298)
+    assert torch.all(out[:T] == 0) and torch.all(lse[:T] == -math.inf)
+    assert cache.missed.tolist() == [1, 0]
+    c.k[:, c.cu[1] + 1200: c.cu[1] + 1200 + T], c.v[:, c.cu[1] + 1200: c.cu[1] + 1200 + T] = k[:, T:], v[:, T:]
+    c.lens = [0, 1200 + T]
+    ref, ref_lse, _, size = R.attend(c, H, q, cu_new, masks)
+    within(out[T:].cpu().double(), ref[T:], EPS[dtype] * ref[T:].abs() + 1e-4 * size[T:], "out")
+    within(lse[T:].cpu().double(), ref_lse[T:], torch.tensor(1e-4), "lse")
+    # with room made and the mark taken away, the rows come in
+    cache.evict([1000, 1400], 8)
+    cache.missed.zero_()
+    cache.append(k[:, :T].contiguous().cuda(), v[:, :T].contiguous().cuda(), [0, T, T], torch.arange(T, device="cuda").int() + 9000)
+    out, lse = cache.attend(q[:T].cuda(), [0, T, T], tree[:T])
+    cache.accept([0, T, T], None, None, q[:T].cuda(), lse, tree[:T], 0.9)
+    assert cache.lens.tolist() == [1000 + T, 1201] and cache.missed.tolist() == [0, 0] and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("dtype,d,planes", [(torch.bfloat16, 128, 2), (torch.float32, 64, 1)])
+def test_tokens_that_do_not_fit_in_a_replayed_step(B, dtype, d, planes):  # noqa: F811
+    """Steps captured once and replayed past the capacity of one sequence: it stops as it is, the other goes on."""
+    G, H = 2, 8
+    cache, c = full_cache(dtype, d, G, H, planes, [300, 400], [296, 200], 9)
+    k, v, q = (x.cuda() for x in rows(G, H, d, 2, dtype, 10))
+    pos, results = torch.full((2,), 9000, dtype=torch.int32, device="cuda"), []
+
+    def step():
+        cache.append(k, v, [0, 1, 2], pos)
+        results[:] = cache.attend(q, [0, 1, 2], lam=0.9)
+        cache.append(k, v, [0, 1, 2], pos)
+        results.extend(cache.attend(q, [0, 1, 2], lam=0.9))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert cache.lens.tolist() == [300, 204] and cache.missed.tolist() == [0, 0]
+    before = {name: getattr(cache, name).clone() for name in ("k", "v", "mass", "pos")}
+    for i in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert cache.lens.tolist() == [300, 206 + 2 * i] and cache.missed.tolist() == [1, 0]
+        for name, x in before.items():
+            assert torch.equal(getattr(cache, name)[:, :300], x[:, :300]), name
+        for out, lse in (results[:2], results[2:]):
+            assert torch.all(out[0] == 0) and torch.all(lse[0] == -math.inf) and torch.isfinite(lse[1]).all() and torch.any(out[1] != 0)
+    assert not torch.equal(cache.mass[:, 300:500], before["mass"][:, 300:500])
+    cache.reset()
+    assert cache.lens.tolist() == [0, 0] and cache.missed.tolist() == [0, 0]
