@@ -396,7 +396,8 @@ structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_h
  *   slot B_b + i  <-  slot B_b + path[i]   for keys, values, mass and pos, as if all were read before any is written
  *   lens_out[b] = B_b + A_b
  * The other drafts' slots are no longer in use.  q, strides, cu_new, tree_mask, scale, softcap, slopes as in the attend call;
- * with lambda = 0 q and lse may be NULL.  path, n_accept, lse: DEVICE.  A row whose lse is -infinity adds nothing; path entries
+ * with lambda = 0 q and lse may be NULL.  path, n_accept, lse: DEVICE.  A row whose lse is -infinity adds nothing, one whose lse is NaN makes
+ * the mass of what it sees NaN, as a single token's does in structkv_cache_attend; path entries
  * outside [0, T_b) and n_accept outside [0, T_b] are taken as the nearer bound; a sequence with lens[b] < T_b or missed[b] != 0 is left as
  * it was.
  */

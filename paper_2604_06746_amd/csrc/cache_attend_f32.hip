@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256) void cache_weights_f32_kernel(TAB tab, CacheVi
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s) qf[s] = load4<T, VEC>(qrow, s * 16 + 4 * q4, c.d);
       const float lse2 = w.lse[r * w.H + head] * 1.4426950408889634f;
-      const bool counts = row0 + l16 < rows && lse2 > -INFINITY;
+      const bool counts = row0 + l16 < rows && lse2 != -INFINITY;   // (one that is not a number counts)
       const uint64_t mask = row_mask(f, r, t);
       const float slope = f.slopes ? f.slopes[head] : 0.f;
       const int at = pos ? pos[h.base + t] : 0;

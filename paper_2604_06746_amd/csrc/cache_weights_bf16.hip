@@ -84,12 +84,12 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
       const int blocks = min(kRowBlocks, (rows - row0 + 15) / 16);
       fetch(0);
       if (mine > 1) fetch(1);
-      // what the rows need to be known by, a lane a row (one without a norm has weights of zero), then the rows as operands
+      // what the rows need to be known by, a lane a row (one without a norm has weights of zero, one whose norm is not a number has those), then the rows as operands
       {
         const int row = min(row0 + lane, rows - 1), i = token_of(w, row), head = g * w.gs + row - i * w.gs;
         const int t = __shfl(step, i);
         const float lse2 = w.lse[(int64_t)(new0 + t) * w.H + head] * 1.4426950408889634f;
-        row_norm[lane] = row0 + lane < rows && lse2 > -INFINITY ? lse2 : INFINITY;
+        row_norm[lane] = row0 + lane < rows && lse2 != -INFINITY ? lse2 : INFINITY;
         if (MODE == kBiased) {
           row_slope[lane] = pos ? f.slopes[head] : 0.f;
           row_at[lane] = pos ? pos[h.base + t] : 0;

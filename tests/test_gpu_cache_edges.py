@@ -101,3 +101,34 @@ def test_tokens_that_do_not_fit_in_a_replayed_step(B, dtype, d, planes):  # noqa
     assert not torch.equal(cache.mass[:, 300:500], before["mass"][:, 300:500])
     cache.reset()
     assert cache.lens.tolist() == [0, 0] and cache.missed.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("dtype,d,H", [(torch.bfloat16, 128, 8), (torch.bfloat16, 64, 40), (torch.float32, 64, 8), (torch.bfloat16, 80, 4)])
+@pytest.mark.parametrize("planes", [1, 2])
+def test_accepted_rows_whose_norm_is_not_a_number(B, dtype, d, H, planes):  # noqa: F811
+    """Their weights are not numbers either: so is the mass of what they see, in the planes of their heads; all else is as without them."""
+    T, lens, masks = 8, [300, 9], [0b1, 0b11, 0b100, 0b1001, 0b10010, 0b100101, 0b1001011, 0b10000000]
+    c = R.make_cache(2, d, planes, [310, 9], lens, dtype, 21)
+    k, v, q = rows(2, H, d, 2 * T, dtype, 22)
+    lse = R.attend(c, H, q, [0, T, 2 * T], masks * 2)[1].float()
+    lse[1, 0], lse[T + 3, H - 1], lse[2] = math.nan, math.nan, math.nan     # (the last one's token is not accepted)
+    path = torch.tensor([1, 4, 0, 0, 0, 0, 0, 0] + [0, 3, 7, 0, 0, 0, 0, 0], dtype=torch.int32)
+    n_accept = [2, 3]
+    cuda = {name: getattr(c, name).cuda() for name in ("k", "v", "mass", "pos")}
+    lens_in, lens_out = torch.tensor(lens, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    handle = B.make_cache(cuda["k"], cuda["v"], c.cu, lens_in, cuda["mass"], cuda["pos"])
+    B.structkv_cache_accept(handle, H, q.cuda(), lse.cuda(), [0, T, 2 * T], lens_out, path.cuda(), torch.tensor(n_accept, dtype=torch.int32).cuda(),
+                            R.as_int64(masks * 2).cuda(), lam=0.9)
+    norms = lse.nan_to_num(-math.inf, neginf=-math.inf)                     # (rows without a norm add nothing)
+    *_, mass, new_lens = R.accept(c, H, q, norms, [0, T, 2 * T], path, n_accept, masks * 2, lam=0.9)
+    odd = torch.zeros(c.mass.shape, dtype=torch.bool)
+    for b, t, h in ((0, 1, 0), (1, 3, H - 1)):
+        plane = h // (H // 2) if planes > 1 else 0
+        odd[plane, [c.cu[b] + s for s in R.visible(lens[b], lens[b] - T, t, masks)]] = True
+    for b in range(2):
+        first, steps = c.cu[b] + lens[b] - T, path[T * b:T * b + n_accept[b]].long()
+        odd[:, first:first + n_accept[b]] = odd[:, first + steps].clone()
+    got = cuda["mass"].cpu().double()
+    assert lens_out.tolist() == new_lens and odd.any() and not odd.all()
+    assert torch.equal(torch.isnan(got), odd)
+    within(got[~odd], mass[~odd], 1e-4 * mass[~odd].abs(), "mass")
