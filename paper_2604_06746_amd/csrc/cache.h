@@ -55,7 +55,7 @@ struct CacheView {
   int G, d, planes;
 };
 
-// How scores are formed: c2 = scale log2(e); with a cap or slopes in full (kBiased, and kCapped where it is quick).
+// How scores are formed: c2 = scale log2(e); capped (Cap), and biased by distance (biased).
 struct ScoreForm {
   float scale, c2, softcap, inv_cap;
   const float* slopes;
@@ -150,21 +150,48 @@ __device__ __forceinline__ Held held(const TAB& t, const CacheView& c, int b) {
   return h;
 }
 
-// z of a score in full: capped, and biased by distance; in the log2 domain.
-// tanh(y) = (1 - e) / (1 + e), e = exp(-2 |y|); below 1/4, where 1 - e cancels, its series (relative error of either < 4e-7).
-__device__ __forceinline__ float tanh_of(float y) {
-  const float a = fabsf(y), y2 = y * y;
-  const float e = __builtin_amdgcn_exp2f(-2.885390082f * a);
-  const float big = copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), y);
-  const float small = fmaf(y * y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), y);
-  return a < 0.25f ? small : big;
+constexpr float kLog2e = 1.4426950408889634f;
+// c tanh(y / c) of products s, y = scale s, in units of which the scores' own has `unit`, with errors of a few 2^-24 of the result: what is off by
+// c's own roundings, as c - 2 c / (1 + e) is, shows in lse and in the weights of accepted drafts, which are fp32.
+// u = y / c.  Near zero c u (1 + w P(w)), w = u^2, P of five terms that fit (tanh(u) / u - 1) / w up to u = 3/4 (1 + w P off by 3.3e-8 of itself).
+// Beyond, c (1 - e) / (1 + e), e = exp(-2 |u|) < 0.23: what e is off by counts 2 e / (1 - e^2) < 0.48.
+struct Cap {
+  float in, in2, reach, top, c1, c2, c3, c4, c5;   // reach: the largest product near zero
+  __device__ __forceinline__ Cap(const ScoreForm& f, float unit)
+      : in(f.scale * f.inv_cap), in2(in * 2.885390082f), reach(0.75f / in), top(f.softcap * unit), c1(top * -0.33333068f),
+        c2(top * 0.13326522f), c3(top * -0.05339028f), c4(top * 0.01966496f), c5(top * -0.00476953f) {}
+  __device__ __forceinline__ float near_zero(float s) const {
+    const float u = s * in, w = u * u;
+    return u * fmaf(w, fmaf(w, fmaf(w, fmaf(w, fmaf(w, c5, c4), c3), c2), c1), top);
+  }
+  __device__ __forceinline__ float operator()(float s) const {
+    const float e = __builtin_amdgcn_exp2f(-in2 * fabsf(s));
+    const float far = copysignf(top * ((1.f - e) * __builtin_amdgcn_rcpf(1.f + e)), s);
+    return fabsf(s) > reach ? far : near_zero(s);   // (NaN stays NaN)
+  }
+  // four at once: mostly all of a wave's are near zero, which spares them the exponential and the reciprocal (four trees of 64 drafts over 8K to
+  // 16.5K slots, capped at 30: 114 us, sixteen at once 123, where rows with a few large scores hold up the others; without a cap 97)
+  __device__ __forceinline__ void apply(float (&x)[4]) const {
+    if (__any(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))) > reach)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (*this)(x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = near_zero(x[i]);
+    }
+  }
+};
+// products as scores in their own units, capped or not
+__device__ __forceinline__ void scaled(const ScoreForm& f, const Cap& cap, float (&x)[4]) {
+  if (f.softcap > 0.f) {
+    cap.apply(x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] *= f.scale;
+  }
 }
-__device__ __forceinline__ float full_score(const ScoreForm& f, float s, float slope, int distance) {
-  float y = s * f.scale;
-  if (f.softcap > 0.f) y = f.softcap * tanh_of(y * f.inv_cap);
-  if (f.slopes) y = fmaf(-slope, (float)distance, y);
-  return y * 1.4426950408889634f;
-}
+// a score biased by distance, in the log2 domain
+__device__ __forceinline__ float biased(float y, float slope, int distance) { return fmaf(-slope, (float)distance, y) * kLog2e; }
 // whether fresh token t (mask: its bits) sees slot s < n
 __device__ __forceinline__ bool sees(uint64_t mask, int s, int base) { return s < base || ((mask >> (s - base)) & 1); }
 __device__ __forceinline__ uint64_t row_mask(const ScoreForm& f, int64_t r, int t) {

@@ -76,14 +76,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qrow + ks * 32 + 8 * q4);
     mask[rb] = row_mask(f, r, t);
-    slope[rb] = MODE == kBiased && f.slopes ? f.slopes[head] : 0.f;
+    slope[rb] = MODE == kBiased ? f.slopes[head] : 0.f;
     if (SAVE) save = w.x + head * w.xs + h.lo + kScorePad * p.b;
   }
   if (s0 >= s1 && (p.nc > 1 || w.x)) return;   // (the join reads no more chunks than have slots)
 
   const uint16_t* kg = (const uint16_t*)c.k + (int64_t)p.g * c.sh + h.lo * c.ss;
   const uint16_t* vg = (const uint16_t*)c.v + (int64_t)p.g * c.sh + h.lo * c.ss;
-  const int32_t* pos = MODE == kBiased && f.slopes ? c.pos + (c.planes > 1 ? p.g * c.slots : 0) + h.lo : nullptr;
+  const int32_t* pos = MODE == kBiased ? c.pos + (c.planes > 1 ? p.g * c.slots : 0) + h.lo : nullptr;
   uint8_t* kt = lds + wave * SLOT;
   uint8_t* vt = kt + TILE;
   auto swz_k = [](int s) { return swizzle_k<SEGS>(s); };
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   };
   auto fetch_k = [&](int j0) __attribute__((always_inline)) {
     fetch(kg, koff, swz_k, j0, kt);
-    if (POS) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(pos ? pos + min(j0 + (lane & 31), n - 1) : c.lens), (lds_ptr_t)(kt + 2 * TILE), 4, 0, 0);
+    if (POS) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(pos + min(j0 + (lane & 31), n - 1)), (lds_ptr_t)(kt + 2 * TILE), 4, 0, 0);
   };
   auto fetch_v = [&](int j0) __attribute__((always_inline)) { fetch(vg, voff, swz_v, j0, vt); };
 
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   if (mine > 0) { fetch_k(s0 + 32 * wave); fetch_v(s0 + 32 * wave); }
 
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) at[rb] = MODE == kBiased && pos && n > 0 ? pos[h.base + token_of(w, min(row0 + rb * 16 + l16, rows - 1))] : 0;
+  for (int rb = 0; rb < RB; ++rb) at[rb] = MODE == kBiased && n > 0 ? pos[h.base + token_of(w, min(row0 + rb * 16 + l16, rows - 1))] : 0;
   // (kept in registers from here on; pinned once all of them are on their way)
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   }
   // from here on rows differ in what they see: the first fresh slot, or the end
   const int edge = min(s1, f.tree || h.fresh > 1 ? max(h.base, 0) : n);
-  const QuickCap cap(f);
+  const Cap cap(f, MODE == kCapped ? kLog2e : 1.f);
   uint64_t odd = 0;   // fresh slots whose values are not all numbers
 
   for (int i = 0; i < mine; ++i) {
@@ -165,19 +165,23 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[kb][rb][e] = cap(x[kb][rb][e]);
+        for (int rb = 0; rb < RB; ++rb) {
+          float y[4] = {x[kb][rb][0], x[kb][rb][1], x[kb][rb][2], x[kb][rb][3]};
+          cap.apply(y);
+          x[kb][rb] = floatx4{y[0], y[1], y[2], y[3]};
+        }
     } else if (MODE == kBiased) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         typedef __attribute__((ext_vector_type(4))) int intx4;
         const intx4 fr = *reinterpret_cast<const intx4*>(kt + 2 * TILE + (kb * 16 + 4 * q4) * 4);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
+        for (int rb = 0; rb < RB; ++rb) {
+          float y[4] = {x[kb][rb][0], x[kb][rb][1], x[kb][rb][2], x[kb][rb][3]};
+          scaled(f, cap, y);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[kb][rb][e] = full_score(f, x[kb][rb][e], slope[rb], at[rb] - fr[e]);
+          for (int e = 0; e < 4; ++e) x[kb][rb][e] = biased(y[e], slope[rb], at[rb] - fr[e]);
+        }
       }
     }
     wait_lds();   // K has been read: its place is free

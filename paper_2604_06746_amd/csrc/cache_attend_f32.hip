@@ -87,6 +87,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
   for (int s = 0; s < DP / 16; ++s) qf[s] = load4<T, VEC>(qrow, s * 16 + 4 * q4, c.d);
   const uint64_t mask = row_mask(f, r, t);
   const bool more = f.softcap > 0.f || f.slopes;
+  const Cap cap(f, 1.f);
   const float slope = f.slopes ? f.slopes[head] : 0.f;
   if (s0 >= s1 && (p.nc > 1 || w.x)) return;   // (the join reads no more chunks than have slots)
   const int32_t* pos = f.slopes ? c.pos + (c.planes > 1 ? p.g * c.slots : 0) + h.lo : nullptr;
@@ -143,12 +144,13 @@ __global__ __launch_bounds__(64 * kAttendWaves) void cache_attend_f32_kernel(TAB
     // ahead of the other workgroup's waves until the tile is done, lest both be at the same instructions
     __builtin_amdgcn_s_setprio(1);
     const floatx4 acc = tile_scores<DP>(kt, qf, l16, q4);
-    float x[4];
+    float x[4] = {acc[0], acc[1], acc[2], acc[3]};
+    if (more) scaled(f, cap, x);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int s = j0 + 4 * q4 + i;
       const bool seen = s < s1 && sees(mask, min(s, n - 1), h.base);
-      x[i] = more ? full_score(f, acc[i], slope, far[i]) : acc[i] * f.c2;
+      x[i] = more ? biased(x[i], slope, far[i]) : x[i] * f.c2;
       if (!seen) x[i] = -INFINITY;
       if (w.x && s < s1 && row0 + l16 < rows) w.x[head * w.xs + h.lo + kScorePad * p.b + s] = x[i];
     }
@@ -196,6 +198,7 @@ __global__ __launch_bounds__(256) void cache_weights_f32_kernel(TAB tab, CacheVi
   const int n = h.n, new0 = tab.cu_new[b], plane = blockIdx.y;
   const int taken = n_accept ? max(0, min(n_accept[b], h.fresh)) : h.fresh, rows = taken * w.gs;
   const bool more = f.softcap > 0.f || f.slopes;
+  const Cap cap(f, 1.f);
   const int32_t* pos = f.slopes ? c.pos + plane * c.slots + h.lo : nullptr;
   int from[4] = {};
   if (pos) {
@@ -228,9 +231,11 @@ __global__ __launch_bounds__(256) void cache_weights_f32_kernel(TAB tab, CacheVi
       const float slope = f.slopes ? f.slopes[head] : 0.f;
       const int at = pos ? pos[h.base + t] : 0;
       const floatx4 acc = tile_scores<DP>(kt, qf, l16, q4);
+      float y[4] = {acc[0], acc[1], acc[2], acc[3]};
+      if (more) scaled(f, cap, y);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = more ? full_score(f, acc[i], slope, at - from[i]) : acc[i] * f.c2;
+        const float x = more ? biased(y[i], slope, at - from[i]) : y[i] * f.c2;
         if (counts && sees(mask, min(j0 + 4 * q4 + i, n - 1), h.base)) sum[i] += __builtin_amdgcn_exp2f(x - lse2);
       }
     }

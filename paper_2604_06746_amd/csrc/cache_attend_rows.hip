@@ -78,9 +78,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
   const uint64_t mask = row_mask(f, new0 + t, t);
   const uint16_t* kg = (const uint16_t*)c.k + (int64_t)p.g * c.sh + h.lo * c.ss;
   const uint16_t* vg = (const uint16_t*)c.v + (int64_t)p.g * c.sh + h.lo * c.ss;
-  const int32_t* pos = MODE == kBiased && f.slopes ? c.pos + (c.planes > 1 ? p.g * c.slots : 0) + h.lo : nullptr;
-  const float slope = pos ? f.slopes[head] : 0.f;
-  const int at = pos && n > 0 ? pos[h.base + t] : 0;
+  const int32_t* pos = MODE == kBiased ? c.pos + (c.planes > 1 ? p.g * c.slots : 0) + h.lo : nullptr;
+  const float slope = MODE == kBiased ? f.slopes[head] : 0.f;
+  const int at = MODE == kBiased && n > 0 ? pos[h.base + t] : 0;
   uint32_t koff[NI], voff[NI];   // of the pieces this lane fetches, from the tile's first row
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
       }
     }
     // (by every wave, the same to the same place, so that the waits know how many there are)
-    if (POS) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(pos ? pos + min(j0 + l32, n - 1) : c.lens), (lds_ptr_t)(to + 2 * TILE), 4, 0, 0);
+    if (POS) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(pos + min(j0 + l32, n - 1)), (lds_ptr_t)(to + 2 * TILE), 4, 0, 0);
   };
   // (kept in registers from here on; nothing of it is on its way when the first tiles are requested)
 #pragma unroll
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
 #pragma unroll
     for (int e = 0; e < 16; ++e) O[db][e] = 0.f;
   const int edge = min(s1, f.tree || h.fresh > 1 ? max(h.base, 0) : n);
-  const QuickCap cap(f);
+  const Cap cap(f, MODE == kCapped ? kLog2e : 1.f);
   const int ka = l32 * SEGS, kx = swizzle_k<SEGS>(l32);
   const int vs = 4 * half + (l16 >> 2);
   const uint32_t va = (uint32_t)(uintptr_t)(lds_ptr_t)(lds + TILE) + (vs * SEGS + ((2 * ((lane >> 4) & 1) + ((l16 >> 1) & 1)) ^ swizzle_wide<SEGS>(vs))) * 16 + (l16 & 1) * 8;
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
     bf16x8 kf[KS];
     read_rows(kf, 0);
     x = products(kf);
-    top = highest(x);
+    if (MODE == kPlain) top = highest(x);
   }
   for (int i = 0; i < tiles; ++i) {
     const int j0 = s0 + 32 * i;
@@ -184,14 +184,21 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
     if (row0 >= rows) continue;   // (a wave without rows only fetches)
     if (MODE == kCapped) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = cap(x[e]);
+      for (int q = 0; q < 4; ++q) {
+        float y[4] = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+        cap.apply(y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * q + e] = y[e];
+      }
     } else if (MODE == kBiased) {
       typedef __attribute__((ext_vector_type(4))) int intx4;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const intx4 fr = *reinterpret_cast<const intx4*>(lds + (i & (kPlaces - 1)) * SLOT + 2 * TILE + (8 * q + 4 * half) * 4);
+        float y[4] = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+        scaled(f, cap, y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * q + e] = full_score(f, x[4 * q + e], slope, at - fr[e]);
+        for (int e = 0; e < 4; ++e) x[4 * q + e] = biased(y[e], slope, at - fr[e]);
       }
     }
     const float c2 = MODE == kPlain ? f.c2 : 1.f;
@@ -255,7 +262,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
 #pragma unroll
           for (int u = k * 4 / DB; u < (k + 1) * 4 / DB; ++u) weigh(1, u);
         } else if (k == DB) {
-          top = highest(next);
+          if (MODE == kPlain) top = highest(next);
           Z += z;
         }
       }

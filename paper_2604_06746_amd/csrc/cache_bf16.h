@@ -75,21 +75,10 @@ __device__ __forceinline__ uint64_t clear_odd_values(uint8_t* vt, int first, int
   return odd_slots;
 }
 
-enum { kPlain = 0, kCapped = 1, kBiased = 2 };   // how scores are formed: scaled; capped; in full
-// Up to this cap its quick form is taken, whose error of cap x 2^-22 is a weight's relative one: 2^-14 here, a 64th of a bf16 rounding.
-constexpr float kLargestQuickCap = 256.f;
-// in the log2 domain, c tanh(y / c) = c - 2 c / (1 + e^(2 y / c))
-struct QuickCap {
-  float cap2, in;
-  __device__ __forceinline__ explicit QuickCap(const ScoreForm& f) : cap2(f.softcap * 1.4426950408889634f), in(f.scale * f.inv_cap * 2.885390082f) {}
-  __device__ __forceinline__ float operator()(float s) const {
-    return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * in)), cap2);
-  }
-};
-// the mode that a call's scores need
+enum { kPlain = 0, kCapped = 1, kBiased = 2 };   // how scores are formed: scaled; capped; with a bias, and capped or not
 template <class F>
 void with_mode(const ScoreForm& f, F go) {
-  if (f.slopes || f.softcap > kLargestQuickCap) go(std::integral_constant<int, kBiased>{});
+  if (f.slopes) go(std::integral_constant<int, kBiased>{});
   else if (f.softcap > 0.f) go(std::integral_constant<int, kCapped>{});
   else go(std::integral_constant<int, kPlain>{});
 }

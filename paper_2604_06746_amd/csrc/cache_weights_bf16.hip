@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
   float* row_slope = row_norm + 64;
   int* row_at = reinterpret_cast<int*>(row_norm + 128);
   int* row_token = reinterpret_cast<int*>(row_norm + 192);
-  const int32_t* pos = MODE == kBiased && f.slopes ? c.pos + (int64_t)plane * c.slots + h.lo : nullptr;
+  const int32_t* pos = MODE == kBiased ? c.pos + (int64_t)plane * c.slots + h.lo : nullptr;
   // this wave's heads and tiles
   const int tile_waves = 4 / head_waves, hw = wave / tile_waves, tw = wave % tile_waves;
   float* all = reinterpret_cast<float*>(lds + 4 * (2 * SLOT + kRowBytes));
@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
   __syncthreads();
   const int g0 = c.planes > 1 ? plane : 0, g1 = c.planes > 1 ? plane + 1 : c.G;
   const int tiles = (s1 - s0 + 31) / 32, mine = tiles > tw ? (tiles - tw + tile_waves - 1) / tile_waves : 0;
-  const QuickCap cap(f);
+  const Cap cap(f, MODE == kCapped ? kLog2e : 1.f);
   const int edge = f.tree || h.fresh > 1 ? h.base : n;   // from here on rows differ in what they see
 
   uint32_t off[NI];
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
                                            (lds_ptr_t)(to + k * 1024), 16, 0, NT ? 2 : 0);
         }
       }
-      if (POS) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(pos ? pos + min(j0 + (lane & 31), n - 1) : c.lens), (lds_ptr_t)(to + TILE), 4, 0, 0);
+      if (POS) __builtin_amdgcn_global_load_lds((gbl_ptr_t)(pos + min(j0 + (lane & 31), n - 1)), (lds_ptr_t)(to + TILE), 4, 0, 0);
     };
     for (int row0 = 0; row0 < rows; row0 += 16 * kRowBlocks) {
       const int blocks = min(kRowBlocks, (rows - row0 + 15) / 16);
@@ -91,8 +91,8 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
         const float lse2 = w.lse[(int64_t)(new0 + t) * w.H + head] * 1.4426950408889634f;
         row_norm[lane] = row0 + lane < rows && lse2 != -INFINITY ? lse2 : INFINITY;
         if (MODE == kBiased) {
-          row_slope[lane] = pos ? f.slopes[head] : 0.f;
-          row_at[lane] = pos ? pos[h.base + t] : 0;
+          row_slope[lane] = f.slopes[head];
+          row_at[lane] = pos[h.base + t];
         }
         row_token[lane] = t;
         row_sees[lane] = row_mask(f, new0 + t, t);
@@ -143,12 +143,15 @@ __global__ __launch_bounds__(256, 2) void cache_weights_bf16_kernel(TAB tab, Cac
             floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[rb][ks], kf[kb][ks], x, 0, 0, 0);
+            float y[4] = {x[0], x[1], x[2], x[3]};
+            if (MODE == kCapped) cap.apply(y);
+            else if (MODE == kBiased) scaled(f, cap, y);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               float p;
-              if (MODE == kPlain) p = __builtin_amdgcn_exp2f(fmaf(x[e], f.c2, -norm[e]));
-              else if (MODE == kCapped) p = __builtin_amdgcn_exp2f(cap(x[e]) - norm[e]);
-              else p = __builtin_amdgcn_exp2f(full_score(f, x[e], slope[e], at[e] - from[kb]) - norm[e]);
+              if (MODE == kPlain) p = __builtin_amdgcn_exp2f(fmaf(y[e], f.c2, -norm[e]));
+              else if (MODE == kCapped) p = __builtin_amdgcn_exp2f(y[e] - norm[e]);
+              else p = __builtin_amdgcn_exp2f(biased(y[e], slope[e], at[e] - from[kb]) - norm[e]);
               if (ragged) {   // (a slot that the row does not see may hold anything)
                 const int s = j0 + kb * 16 + l16;
                 if (s >= n || norm[e] == INFINITY || !sees(row_sees[rb * 16 + 4 * q4 + e], s, h.base)) p = 0.f;

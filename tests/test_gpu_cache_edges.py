@@ -132,3 +132,66 @@ def test_accepted_rows_whose_norm_is_not_a_number(B, dtype, d, H, planes):  # no
     assert lens_out.tolist() == new_lens and odd.any() and not odd.all()
     assert torch.equal(torch.isnan(got), odd)
     within(got[~odd], mass[~odd], 1e-4 * mass[~odd].abs(), "mass")
+
+
+def lone_scores(H, G, d, T, batch, dtype, softcap, seed):
+    """Drafts that see themselves alone, with one component that counts: each row's score is one exact product, from far below the cap to beyond."""
+    g = torch.Generator().manual_seed(seed)
+    c = R.make_cache(G, d, G, [T + 3] * batch, [T] * batch, dtype, seed)
+    q = torch.zeros(batch * T, H, d, dtype=dtype)
+    used = torch.cat([torch.arange(T) + (T + 3) * b for b in range(batch)])
+    c.k[:, used] = 0
+    c.k[:, used, 0] = torch.exp2(8 * torch.rand(G, batch * T, generator=g) - 4).to(dtype)
+    q[:, :, 0] = (softcap * torch.exp2(8 * torch.rand(batch * T, H, generator=g) - 7) * torch.randn(batch * T, H, generator=g).sign()).to(dtype)
+    masks = [1 << t for t in range(T)] * batch
+    y = q[:, :, 0].double() * c.k[:, used, 0].double().T.repeat_interleave(H // G, 1)      # [row, head]
+    return c, q, masks, y, used
+
+
+# (the bf16 matrix kernels of 16, 32 and 128 rows, the fp32 one)
+CAPPED = [(torch.bfloat16, 128, 2, 8, 2, 3), (torch.bfloat16, 64, 2, 8, 8, 3), (torch.bfloat16, 128, 64, 128, 40, 9), (torch.float32, 64, 2, 8, 40, 2),
+          (torch.bfloat16, 80, 2, 4, 40, 2)]
+
+
+@pytest.mark.parametrize("dtype,d,G,H,T,batch", CAPPED)
+@pytest.mark.parametrize("softcap", [5.0, 30.0, 50.0, 256.0, 1000.0])
+@pytest.mark.parametrize("slopes", [False, True])
+def test_capped_scores_to_their_last_bits(B, dtype, d, G, H, T, batch, softcap, slopes):  # noqa: F811
+    """lse of a row that sees one slot is its score c tanh(y / c), y an exact product (fp32 keys: one rounding).  In halves of an ulp, 2^-24 of the
+    result: near zero y and u = y / c have four roundings (u's count 2 w |P| < 1/4 each), the polynomial's fit 0.6 and its sum and last product 2;
+    beyond, e has its argument's four roundings and the exponential's own ulp, each counting at most 2 |u| 2 e / (1 - e^2) < 0.8, 1 - e, 1 + e and the
+    products 4, the reciprocal's ulp 2, the cap's constants 2; then the change to log2 and back 4 in either.  16 cover both."""
+    c, q, masks, y, used = lone_scores(H, G, d, T, batch, dtype, softcap, 31)
+    cu_new = [T * b for b in range(batch + 1)]
+    slope = torch.zeros(H) if slopes else None          # (distances of zero: the form with a bias)
+    cuda = {name: getattr(c, name).cuda() for name in ("k", "v", "mass", "pos")}
+    lens, lens_out = (torch.tensor(c.lens, dtype=torch.int32, device="cuda") for _ in range(2))
+    handle = B.make_cache(cuda["k"], cuda["v"], c.cu, lens, cuda["mass"], cuda["pos"])
+    out, lse = torch.empty(batch * T, H, d, dtype=dtype, device="cuda"), torch.empty(batch * T, H, device="cuda")
+    ws = torch.empty(B.structkv_cache_workspace_bytes(handle, H, batch * T), dtype=torch.uint8, device="cuda")
+    form = dict(tree_mask=R.as_int64(masks).cuda(), scale=1.0, softcap=softcap, slopes=None if slope is None else slope.cuda())
+    B.structkv_cache_attend(handle, H, q.cuda(), cu_new, out, lse, ws, **form)
+    x = softcap * torch.tanh(y / softcap)
+    within(lse.cpu().double(), x, 16 * 2.0 ** -24 * x.abs(), "lse")
+    # the weights of accepted drafts, against norms that they nearly equal: e^(x - lse), off by what x is, by the norm's two roundings and by a few more
+    norms = x.float()
+    cuda["mass"].zero_()
+    B.structkv_cache_accept(handle, H, q.cuda(), norms.cuda(), cu_new, lens_out, lam=1.0, **form)
+    weights = torch.exp(x - norms.double()).view(batch * T, G, H // G)
+    error = ((16 + 4) * 2.0 ** -24 * x.abs() + 8 * 2.0 ** -24).view(weights.shape)
+    within(cuda["mass"][:, used].cpu().double(), weights.sum(2).T, (weights * error).sum(2).T + H // G * 2.0 ** -24 * weights.sum(2).T, "mass")
+
+
+@pytest.mark.parametrize("softcap", [256.0, 300.0, 1000.0])
+@pytest.mark.parametrize("d", [128, 64])
+def test_large_caps_without_a_bias(B, softcap, d):  # noqa: F811
+    """Caps from 256 on over whole caches: 16, 32 and 128 rows a workgroup, gathered weights, accepted drafts."""
+    from test_gpu_cache import check_accept, check_attend
+    c = R.make_cache(2, d, 2, [300, 90], [280, 90], torch.bfloat16, 33)
+    c.k *= 8
+    check_attend(B, c, 6, [1, 1], softcap=softcap, lam=0.9, seed=33)
+    check_attend(B, c, 6, [5, 9], tree=True, softcap=softcap, seed=34)
+    check_accept(B, c, 6, [9, 64], [[0, 3, 8], list(range(1, 64))], softcap=softcap, lam=0.5, seed=35)
+    c = R.make_cache(16, d, 16, [1400, 70, 901, 2100, 40], [1391, 70, 17, 2099, 33], torch.bfloat16, 36)
+    c.k *= 8
+    check_attend(B, c, 48, [64, 0, 20, 33, 33], tree=True, softcap=softcap, seed=36)
