@@ -376,7 +376,8 @@ structkv_status structkv_cache_append(const structkv_cache* cache, const void* k
  *   mass[p][s] = lambda * mass[p][s] + sum of a_s over the plane's query heads, for the slots in use of sequences with T_b = 1.
  * lambda = 0: mass stays as it is.  Drafts gather theirs when they are accepted (structkv_cache_accept).
  * q: element (r, h, c) at r*q_stride_tok + h*q_stride_head + c; out [new][H_q][d] contiguous; lse_out [new][H_q] fp32.
- * scale: >= 0, 0 selects 1/sqrt(head_dim); 4 scale / softcap must be finite in fp32.  slopes: DEVICE fp32 [H_q] or NULL, needs pos.
+ * scale: >= 0, 0 selects 1/sqrt(head_dim).  With a softcap, 1 / softcap, 2 softcap and 4 scale / softcap must be finite in fp32, and scale /
+ * softcap not denormal.  slopes: DEVICE fp32 [H_q] or NULL, needs pos.
  * cu_new: HOST [batch+1].
  * A sequence with lens[b] < T_b or missed[b] != 0 is one whose rows see nothing, and whose mass stays as it is.
  * Deterministic: the same call on the same lengths gives the same bits.  (Sums are cut by the lengths of the whole batch, so a sequence's

@@ -89,15 +89,16 @@ structkv_status check_scores(const structkv_cache* c, int32_t H, float scale, fl
   if (st != STRUCTKV_OK) return st;
   if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(STRUCTKV_ERR_INVALID_ARG, "scale must be finite and >= 0 (0 = 1/sqrt(head_dim))");
   if (!(softcap >= 0.f) || !std::isfinite(softcap)) return fail(STRUCTKV_ERR_INVALID_ARG, "softcap must be finite and >= 0 (0 = none)");
-  if (softcap > 0.f && !std::isfinite((scale > 0.f ? scale : 1.f) / softcap * 4.f))
-    return fail(STRUCTKV_ERR_UNSUPPORTED, "scale / softcap leaves fp32's range");
+  const float s = scale > 0.f ? scale : 1.0f / std::sqrt((float)c->head_dim);
+  // what the kernels work with (Cap): each by itself, since a product of a tiny and a huge one is no help to a score of zero
+  if (softcap > 0.f && (!std::isfinite(1.f / softcap) || !std::isfinite(2.f * softcap) || !std::isfinite(s / softcap * 4.f) || !std::isnormal(s / softcap)))
+    return fail(STRUCTKV_ERR_UNSUPPORTED, "softcap, 1 / softcap or scale / softcap leaves fp32's range");
   if (!(lambda >= 0.f && lambda <= 1.f)) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda must be in [0,1]");
   if (lambda > 0.f && !c->mass) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda > 0 needs the cache's mass");
   if (slopes && !c->pos) return fail(STRUCTKV_ERR_INVALID_ARG, "slopes need the cache's pos");
   if (((uintptr_t)slopes & 3) || ((uintptr_t)tree & 7)) return fail(STRUCTKV_ERR_INVALID_ARG, "slopes or tree_mask is misaligned");
   if ((uintptr_t)q & (uintptr_t)(elem_bytes(c) - 1)) return fail(STRUCTKV_ERR_INVALID_ARG, "q is not aligned to its elements");
   if (qst < 0 || qsh < 0) return fail(STRUCTKV_ERR_INVALID_ARG, "negative stride of q");
-  const float s = scale > 0.f ? scale : 1.0f / std::sqrt((float)c->head_dim);
   *f = ScoreForm{s, (float)((double)s * 1.4426950408889634), softcap, softcap > 0.f ? 1.f / softcap : 0.f, slopes, tree};
   return STRUCTKV_OK;
 }
