@@ -141,6 +141,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
   const int edge = min(s1, f.tree || h.fresh > 1 ? max(h.base, 0) : n);
   const Cap cap(f, MODE == kCapped ? kLog2e : 1.f);
   uint64_t odd = 0;   // fresh slots whose values are not all numbers
+  bool huge = false;
 
   for (int i = 0; i < mine; ++i) {
     const int j0 = s0 + 32 * (wave + kAttendWaves * i), next = j0 + 32 * kAttendWaves;
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
     }
     wait_lds();   // K has been read: its place is free
     if (i + 1 < mine) fetch_k(next);
-    const float c2 = MODE == kPlain ? f.c2 : 1.f;
+    float c2 = MODE == kPlain ? f.c2 : 1.f;
     const bool ragged = j0 + 32 > edge;
     if (ragged) {
 #pragma unroll
@@ -219,7 +220,15 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_bf16_kernel
         Z[rb] *= shrink;
 #pragma unroll
         for (int db = 0; db < DB; ++db) O[db][rb] *= shrink;
+        if (MODE == kPlain) huge |= __any(fabsf(M[rb]) >= kHuge && M[rb] > kNothingSeen);
       }
+    }
+    if (MODE == kPlain && huge) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) x[kb][rb] *= c2;
+      c2 = 1.f;
     }
     if (SAVE) {
       // Two stores from every wave, whatever the tile holds, so that the waits know how many there are: some lane has a row, and slots

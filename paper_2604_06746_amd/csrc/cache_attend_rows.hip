@@ -131,6 +131,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
   floatx16 O[DB], x;
   float top = kNothingSeen;
   float M = kNothingSeen, Z = 0.f;
+  bool huge = false;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
         for (int e = 0; e < 4; ++e) x[4 * q + e] = biased(y[e], slope, at - fr[e]);
       }
     }
-    const float c2 = MODE == kPlain ? f.c2 : 1.f;
+    float c2 = MODE == kPlain ? f.c2 : 1.f;
     if (ragged) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -218,6 +219,12 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void cache_attend_rows_kernel
       Z *= shrink;
 #pragma unroll
       for (int db = 0; db < DB; ++db) O[db] *= shrink;
+      if (MODE == kPlain) huge = __any(fabsf(M) >= kHuge && M > kNothingSeen);
+    }
+    if (MODE == kPlain && huge) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] *= c2;
+      c2 = 1.f;
     }
     // (ahead of the other workgroup's waves from here on: theirs are then elsewhere in their tiles; 99 -> 91 us)
     __builtin_amdgcn_s_setprio(1);

@@ -75,6 +75,10 @@ __device__ __forceinline__ uint64_t clear_odd_values(uint8_t* vt, int first, int
   return odd_slots;
 }
 
+// From references of this size on a scaled score and its row's reference, both rounded alike, are subtracted: an fma takes them apart by the
+// reference's rounding, 2^-24 of it, which is then beyond what an exponent bears.
+constexpr float kHuge = 16777216.f;
+
 enum { kPlain = 0, kCapped = 1, kBiased = 2 };   // how scores are formed: scaled; capped; with a bias, and capped or not
 template <class F>
 void with_mode(const ScoreForm& f, F go) {

@@ -195,3 +195,33 @@ def test_large_caps_without_a_bias(B, softcap, d):  # noqa: F811
     c = R.make_cache(16, d, 16, [1400, 70, 901, 2100, 40], [1391, 70, 17, 2099, 33], torch.bfloat16, 36)
     c.k *= 8
     check_attend(B, c, 48, [64, 0, 20, 33, 33], tree=True, softcap=softcap, seed=36)
+
+
+@pytest.mark.parametrize("dtype,d,G,H,T", [(torch.bfloat16, 128, 2, 8, 1), (torch.bfloat16, 64, 2, 8, 7), (torch.bfloat16, 128, 32, 128, 40),
+                                           (torch.float32, 64, 2, 8, 7), (torch.bfloat16, 80, 2, 4, 1)])
+@pytest.mark.parametrize("score", [-2.0 ** 40, 2.0 ** 40, -2.0 ** 90, 2.0 ** 110])
+def test_scores_far_from_zero(B, dtype, d, G, H, T, score):  # noqa: F811
+    """A row whose scores are huge attends to the highest: one slot's value as it is, lse its score (to log2 and back), mass of one."""
+    n, best = [1300, 700], [777, 0]
+    c = R.make_cache(G, d, 1, n, n, dtype, 41)
+    c.k[:] = 0
+    small, large = math.copysign(1.1171875, score), math.copysign(2.0, score)       # (products that c2 does not divide evenly)
+    c.k[:, :, 0] = large if score < 0 else small
+    for b in range(2):
+        c.k[:, c.cu[b] + best[b], 0] = small if score < 0 else large
+    q = torch.zeros(2 * T, H, d, dtype=dtype)
+    q[:, :, 0] = 1.2890625 * abs(score)
+    score = 1.2890625 * abs(score) * (small if score < 0 else large)
+    cuda = {name: getattr(c, name).cuda() for name in ("k", "v", "mass", "pos")}
+    handle = B.make_cache(cuda["k"], cuda["v"], c.cu, torch.tensor(n, dtype=torch.int32, device="cuda"), cuda["mass"], cuda["pos"])
+    out, lse = torch.empty(2 * T, H, d, dtype=dtype, device="cuda"), torch.empty(2 * T, H, device="cuda")
+    ws = torch.empty(B.structkv_cache_workspace_bytes(handle, H, 2 * T), dtype=torch.uint8, device="cuda")
+    B.structkv_cache_attend(handle, H, q.cuda(), [0, T, 2 * T], out, lse, ws, scale=1.0, lam=0.5 if T == 1 else 0.0)
+    for b in range(2):
+        v = c.v[:, c.cu[b] + best[b]].repeat_interleave(H // G, 0)
+        assert torch.equal(out[b * T:(b + 1) * T].cpu(), v.expand(T, H, d))
+    assert torch.all((lse.double() / score - 1).abs() <= 6 * 2.0 ** -24)
+    if T == 1:
+        mass = c.mass * 0.5
+        mass[0, [c.cu[b] + best[b] for b in range(2)]] += H
+        assert torch.equal(cuda["mass"].cpu(), mass)
