@@ -198,7 +198,7 @@ __device__ __forceinline__ uint64_t row_mask(const ScoreForm& f, int64_t r, int 
   return f.tree ? f.tree[r] : (t >= 63 ? ~0ull : (2ull << t) - 1ull);
 }
 
-constexpr float kNothingSeen = -1.0e30f;   // the reference of a row that has seen nothing
+constexpr float kNothingSeen = -3.4028235e38f;   // the reference of a row that has seen nothing: no score that counts lies below
 
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 

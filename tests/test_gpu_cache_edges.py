@@ -199,7 +199,7 @@ def test_large_caps_without_a_bias(B, softcap, d):  # noqa: F811
 
 @pytest.mark.parametrize("dtype,d,G,H,T", [(torch.bfloat16, 128, 2, 8, 1), (torch.bfloat16, 64, 2, 8, 7), (torch.bfloat16, 128, 32, 128, 40),
                                            (torch.float32, 64, 2, 8, 7), (torch.bfloat16, 80, 2, 4, 1)])
-@pytest.mark.parametrize("score", [-2.0 ** 40, 2.0 ** 40, -2.0 ** 90, 2.0 ** 110])
+@pytest.mark.parametrize("score", [-2.0 ** 40, 2.0 ** 40, -2.0 ** 90, -2.0 ** 110, 2.0 ** 110, -2.0 ** 125])
 def test_scores_far_from_zero(B, dtype, d, G, H, T, score):  # noqa: F811
     """A row whose scores are huge attends to the highest: one slot's value as it is, lse its score (to log2 and back), mass of one."""
     n, best = [1300, 700], [777, 0]
