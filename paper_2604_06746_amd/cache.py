@@ -19,10 +19,11 @@ class LayerCache:
     make an even number of such calls.  The calls of one LayerCache share its workspace and lengths, so they belong on one stream, or in order.
     A sequence that has no room for what is appended stays as it was, and `missed` (int32 [batch] on the device) has a 1 for it: until the
     program sets that back to 0, attend gives the sequence's rows zeros and accept leaves its tokens as they are.
-    max_new: most fresh tokens of a sequence in an attend call."""
+    max_new: most fresh tokens of a sequence in an attend call.  workspace: another LayerCache's, where the calls of both follow each other (as
+    those of a model's layers do: it holds 34 MB and more for 64 sequences of 64 drafts); by default each has its own."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, capacities: Sequence[int], planes: int = 1,
-                 max_new: int = B.STRUCTKV_MAX_DRAFTS, device="cuda"):
+                 max_new: int = B.STRUCTKV_MAX_DRAFTS, device="cuda", workspace: Optional[torch.Tensor] = None):
         self.Hq, self.G, self.d, self.planes = n_q_heads, n_kv_heads, head_dim, planes
         self.batch = len(capacities)
         self.cu = [0]
@@ -40,7 +41,9 @@ class LayerCache:
         size = B.structkv_cache_workspace_bytes(self._handles[0], n_q_heads, max_new * self.batch)
         if size == 0:
             raise B.StructKVError(B.STRUCTKV_ERR_INVALID_ARG, B.structkv_last_error())
-        self.workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        if workspace is not None and (workspace.numel() * workspace.element_size() < size or workspace.device != self.k.device):
+            raise B.StructKVError(B.STRUCTKV_ERR_WORKSPACE, "the workspace must have %d bytes, on the cache's GPU" % size)
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=dev) if workspace is None else workspace
 
     @property
     def lens(self) -> torch.Tensor:

@@ -117,6 +117,8 @@ bool mfma_fits(const structkv_cache* c, const void* q, int64_t qst, int64_t qsh)
 
 // Workgroups: two a CU (more or fewer, 256 to 4096, were slower), at least kLeastChunk slots each.
 constexpr int64_t kAttendBlocks = 512, kLeastChunk = 128;
+// Mean slots of a block of rows from which on it is cut in two even where the blocks fill the chip (plan_attend).
+constexpr int64_t kCutSlots = 4096, kCutSlotsGathered = 1024;
 
 structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mfma, CacheTable* t, AttendPlan* p) {
   const int gs = H / c->n_kv_heads;
@@ -150,7 +152,7 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   // Two a block of rows at least, so that long sequences of large batches are cut too, where that pays for the launch that joins them: 64
   // sequences of 8192 slots 309 us without, 320 with, one of 8192 among 63 of 400 88 and 34; with gathered weights, where the join is there
   // anyway, 64 of 2112 slots 113 and 114, one among short ones 41 and 25, but 64 of 300 27 and 31.
-  const bool cut = rows_wg == 16 && work >= (gather ? 1024. : 4096.) * (double)blocks;
+  const bool cut = rows_wg == 16 && work >= (double)(gather ? kCutSlotsGathered : kCutSlots) * (double)blocks;
   p->units = std::max(blocks, std::min(chunks, std::max(kAttendBlocks / c->n_kv_heads, cut ? 2 * blocks : 0)));
   if (p->units * c->n_kv_heads >= ((int64_t)1 << 31) || stretches >= ((int64_t)1 << 30))
     return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
@@ -169,13 +171,18 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   return STRUCTKV_OK;
 }
 
-// ... at most, however the tokens spread: units per KV head are kAttendBlocks in all, or the blocks of rows, which are joined for single tokens'
-// weights alone
+// ... at most, however new_tokens spread over the sequences.  Of plan_attend's units per KV head those that are joined are kAttendBlocks in all, or
+// blocks of 16 rows: twice those where sequences are long enough to be cut, once where single tokens gather their weights.  A sequence's T gs rows
+// are at most (T gs + 15) / 16 such blocks.
 size_t most_attend_bytes(const structkv_cache* c, int H, int64_t new_tokens, int64_t slots) {
-  const int64_t gs = H / c->n_kv_heads, rows = new_tokens * gs;
+  const int64_t gs = H / c->n_kv_heads, G = c->n_kv_heads, with_tokens = std::min<int64_t>(c->batch, new_tokens);
+  int64_t longest = 0;
+  for (int b = 0; b < c->batch; ++b) longest = std::max(longest, c->cu_slots[b + 1] - c->cu_slots[b]);
   const bool wide = c->dtype == STRUCTKV_DTYPE_BF16 && (c->head_dim == 64 || c->head_dim == 128);
-  const int64_t rows_wg = !wide || rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
-  const size_t parts = (size_t)std::max(rows_wg * kAttendBlocks, 2 * 16 * new_tokens * ceil_div(gs, 16) * c->n_kv_heads);
+  const int64_t rows = std::min<int64_t>(new_tokens, STRUCTKV_MAX_DRAFTS) * gs, rows_wg = !wide || rows <= 16 ? 16 : rows <= 64 ? 32 : 128;
+  const int64_t any = longest >= kCutSlots ? 2 * ((new_tokens * gs + 15 * with_tokens) / 16) : 0;
+  const int64_t single = c->mass ? (longest >= kCutSlotsGathered ? 2 : 1) * with_tokens * ceil_div(gs, 16) : 0;
+  const size_t parts = (size_t)std::max(rows_wg * kAttendBlocks, 16 * G * std::max(any, single));
   return align_up(sizeof(int4) * (size_t)c->batch, 256) + align_up(parts * 2 * sizeof(float), 256) + align_up(parts * padded_dim(c->head_dim) * sizeof(float), 256) +
          (c->mass ? score_bytes(H, slots, c->batch) : 0);
 }

@@ -225,3 +225,34 @@ def test_scores_far_from_zero(B, dtype, d, G, H, T, score):  # noqa: F811
         mass = c.mass * 0.5
         mass[0, [c.cu[b] + best[b] for b in range(2)]] += H
         assert torch.equal(cuda["mass"].cpu(), mass)
+
+
+def test_layers_that_share_a_workspace(B):  # noqa: F811
+    """Two layers' caches, one behind the other on one stream, as with workspaces of their own; a workspace that is too small is refused."""
+    from paper_2604_06746_amd.cache import LayerCache
+    H, G, d, dtype, caps = 8, 2, 128, torch.bfloat16, [5000, 300]
+    layers = [LayerCache(H, G, d, dtype, caps, max_new=8) for _ in range(2)]
+    shared = [LayerCache(H, G, d, dtype, caps, max_new=8)]
+    shared.append(LayerCache(H, G, d, dtype, caps, max_new=4, workspace=shared[0].workspace))
+    assert shared[1].workspace is shared[0].workspace
+    g = torch.Generator(device="cuda").manual_seed(51)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    k, v = normal(2, 2, G, 4800, d)
+    for i in range(2):
+        for cache in (layers[i], shared[i]):
+            cache.append(k[i], v[i], [0, 4600, 4800], torch.arange(4800, device="cuda").int())
+    for step in range(3):
+        q, k1, v1 = normal(2, 2, H, d), normal(2, G, 2, d), normal(2, G, 2, d)
+        for i in range(2):
+            got = []
+            for cache in (layers[i], shared[i]):
+                cache.append(k1[i], v1[i], [0, 1, 2], torch.full((2,), 5000 + step, dtype=torch.int32, device="cuda"))
+                got.append(cache.attend(q[i], [0, 1, 2], lam=0.9))
+                cache.evict([4500, 200], 8)
+            assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    for i in range(2):
+        assert torch.equal(layers[i].mass, shared[i].mass) and layers[i].lens.tolist() == shared[i].lens.tolist() == [4500, 200]
+    with pytest.raises(B.StructKVError):
+        LayerCache(H, G, d, dtype, [5000] * 9, workspace=shared[0].workspace)
+    with pytest.raises(B.StructKVError):
+        LayerCache(H, G, d, dtype, [100], workspace=torch.empty(1 << 28, dtype=torch.uint8))
