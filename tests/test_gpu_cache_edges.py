@@ -256,3 +256,46 @@ def test_layers_that_share_a_workspace(B):  # noqa: F811
         LayerCache(H, G, d, dtype, [5000] * 9, workspace=shared[0].workspace)
     with pytest.raises(B.StructKVError):
         LayerCache(H, G, d, dtype, [100], workspace=torch.empty(1 << 28, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("dtype,G,H,planes,caps,lens", [(torch.bfloat16, 2, 32, 1, [70000, 70001, 40], [1999, 4097, 33]),
+                                                       (torch.bfloat16, 1, 16, 1, [300000, 230000], [3001, 770]),
+                                                       (torch.float32, 2, 36, 1, [140000, 64], [2050, 1]),
+                                                       (torch.bfloat16, 8, 8, 8, [66000, 100], [2001, 98])])
+def test_weights_gathered_four_slots_a_thread(B, dtype, G, H, planes, caps, lens):  # noqa: F811
+    """Room for so many slots that the join takes four a thread, by waves that share a plane's heads and by threads that have all of them; lengths
+    that are no multiple of four."""
+    from test_gpu_cache import check_attend
+    check_attend(B, R.make_cache(G, 64, planes, caps, lens, dtype, 61), H, [1] * len(caps), lam=0.9, seed=61)
+
+
+def test_bf16_of_256_components(B):  # noqa: F811
+    """Single tokens, trees, caps and biases, accepted drafts (fp32 matrix instructions on widened values)."""
+    from test_gpu_cache import check_accept, check_attend
+    c = R.make_cache(2, 256, 2, [300, 90, 5], [280, 90, 1], torch.bfloat16, 62)
+    check_attend(B, c, 8, [1, 1, 1], lam=0.9, seed=62)
+    check_attend(B, c, 8, [13, 64, 1], tree=True, softcap=30.0, slopes=True, seed=63)
+    check_attend(B, c, 2, [5, 0, 1], layout="odd", softcap=50.0, seed=64)
+    check_accept(B, c, 8, [13, 64, 1], [[0, 4, 7], list(range(30)), [0]], softcap=30.0, lam=0.9, seed=65)
+    check_accept(B, c, 8, [13, 64, 1], [[12], [], [0]], slopes=True, lam=0.9, layout="slots", seed=66)
+
+
+@pytest.mark.parametrize("dtype,d,planes", [(torch.bfloat16, 128, 2), (torch.float32, 33, 1)])
+def test_copies_of_many_sequences(B, dtype, d, planes):  # noqa: F811
+    """More sequences than the small table holds, each call with lengths out of bounds among them."""
+    from test_gpu_cache import OnGpu, check_accept, check_evict
+    rng, n = np.random.default_rng(7), 37
+    caps = [int(x) for x in rng.integers(0, 90, n)]
+    lens = [int(rng.integers(0, x + 1)) for x in caps]
+    lens[3], lens[5], lens[9] = -7, caps[5] + 40, caps[9]
+    c = R.make_cache(2, d, planes, caps, lens, dtype, 67)
+    fresh = [int(x) for x in rng.integers(0, 30, n)]
+    cu_new, g = R.cut(fresh), torch.Generator().manual_seed(68)
+    k_new, v_new = (torch.randn(2, cu_new[-1], d, generator=g).to(dtype) for _ in range(2))
+    pos_new, mass_new = torch.randint(0, 999, (planes, cu_new[-1]), generator=g).int(), torch.rand(planes, cu_new[-1], generator=g)
+    on = OnGpu(B, c)
+    B.structkv_cache_append(on.handle, k_new.cuda(), v_new.cuda(), cu_new, on.lens_out, pos_new=pos_new.cuda(), mass_new=mass_new.cuda())
+    on.same(*R.append(c, k_new, v_new, cu_new, pos_new, mass_new))
+    check_evict(B, c, c.mass, [int(x) for x in rng.integers(0, 60, n)], 9)
+    paths = [rng.integers(0, max(T, 1), int(rng.integers(0, T + 1))).tolist() for T in fresh]
+    check_accept(B, c, 4, fresh, paths, lam=0.9, seed=69)
