@@ -394,13 +394,15 @@ structkv_status structkv_cache_attend(const structkv_cache* cache, int32_t n_q_h
  * sequence b (path NULL: i; n_accept NULL: all T_b):
  *   mass[p][s] = lambda * mass[p][s] + sum over i and the plane's query heads of e^{x_s - lse[cu_new[b] + path[i]][h]},
  *                s < lens[b], x and what a row sees as in structkv_cache_attend, which gave lse   (lambda = 0, or T_b = 0: left out)
+ *                The decay comes once a call, however many tokens are accepted: after a path of five, lambda mass and the sum of their
+ *                weights; after five single tokens (structkv_cache_attend) lambda^5 mass, and their weights the more decayed the older.
+ *                What is evicted later may therefore depend on how tokens were drafted; lambda = 1 counts both alike.
  *   slot B_b + i  <-  slot B_b + path[i]   for keys, values, mass and pos, as if all were read before any is written
  *   lens_out[b] = B_b + A_b
  * The other drafts' slots are no longer in use.  q, strides, cu_new, tree_mask, scale, softcap, slopes as in the attend call;
- * with lambda = 0 q and lse may be NULL.  path, n_accept, lse: DEVICE.  A row whose lse is -infinity adds nothing, one whose lse is NaN makes
- * the mass of what it sees NaN, as a single token's does in structkv_cache_attend; path entries
- * outside [0, T_b) and n_accept outside [0, T_b] are taken as the nearer bound; a sequence with lens[b] < T_b or missed[b] != 0 is left as
- * it was.
+ * with lambda = 0 q and lse may be NULL.  path, n_accept, lse: DEVICE.  A row whose lse is -infinity adds nothing, one whose lse is NaN
+ * makes the mass of what it sees NaN, as a single token's does in structkv_cache_attend; path entries outside [0, T_b) and n_accept
+ * outside [0, T_b] are taken as the nearer bound; a sequence with lens[b] < T_b or missed[b] != 0 is left as it was.
  */
 structkv_status structkv_cache_accept(const structkv_cache* cache, int32_t n_q_heads, float scale, float softcap,
                                       const float* slopes, const void* q, int64_t q_stride_tok, int64_t q_stride_head,

@@ -75,7 +75,8 @@ class LayerCache:
     def accept(self, cu_new: Sequence[int], path: Optional[torch.Tensor] = None, n_accept: Optional[torch.Tensor] = None,
                q: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
                lam: float = 0.0, scale: float = 0.0, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None) -> None:
-        """The verified path of the drafts appended last stays; lam > 0: its weights are gathered (q, lse and the rest as in attend)."""
+        """The verified path of the drafts appended last stays; lam > 0: its weights are gathered (q, lse and the rest as in attend), the mass
+        decayed once for all of them, where single tokens' attend decays it with each."""
         B.structkv_cache_accept(self.handle, self.Hq, q, lse, cu_new, self._lens[1 - self._now], path, n_accept, tree_mask, scale, softcap,
                                 slopes, lam)
         self._now = 1 - self._now

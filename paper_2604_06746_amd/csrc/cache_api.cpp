@@ -128,8 +128,9 @@ structkv_status plan_attend(const structkv_cache* c, int H, bool gather, bool mf
   int64_t most_rows = 0;
   for (int b = 0; b < c->batch; ++b) most_rows = std::max<int64_t>(most_rows, (int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs);
   // 128 rows (32 a wave, the tiles shared) where there are more than two blocks of 32 and where enough chunks of them fill the chip: four trees
-  // of 64 drafts over 16512 slots 150 us with, 163 without (one call behind the other); of 16 drafts (64 rows) 68 and 60, one of 64 over 2000
-  // slots 25 and 20
+  // of 64 drafts over 16512 slots 118 us with, 131 without (one call behind the other); of 16 drafts (64 rows) 68 and 60, one of 64 over 2000
+  // slots 25 and 20.  One tree makes the whole batch take them: beside 31 single tokens of 8K slots each one of 20 drafts 222 and 255, beside 15
+  // one of 64 118 and 123, but beside 63 545 and 407 (a token's workgroup has one wave of four at work).
   int64_t wide_units = 0;
   for (int b = 0; b < c->batch; ++b)
     wide_units += ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, 128) * ceil_div(t->cu[b + 1] - t->cu[b], kLeastChunk);

@@ -9,8 +9,8 @@
 // cache_attend_bf16.hip: the usual tile has no exchange between lanes and no rescaling.
 //
 // Single tokens are bound by reading the cache (8 x 32768 slots of 8 heads, 128 components: 338 us, 6.4 TB/s), trees by the waits between matrix
-// and other instructions of two waves a SIMD (64 drafts over 8192 slots 129 us, 67 TFLOP/s of 154; 13 over four times 12.9K 228 us).  On these two, lazy M
-// gave 142 -> 136 and 247 -> 233, the priority the rest; two blocks of rows a workgroup 155 and 254 (registers), operands straight from memory
+// and other instructions of two waves a SIMD (64 drafts over 8192 slots 129 us, 67 TFLOP/s of 154; 13 over four times 12.9K 228 us; in one run the first took
+// 121 us, capped at 30 124).  On these two, lazy M gave 142 -> 136 and 247 -> 233, the priority the rest; two blocks of rows a workgroup 155 and 254 (registers), operands straight from memory
 // 151 and 270.
 #include "cache.h"
 

@@ -8,7 +8,9 @@
 // 32 cycles and some 150 others of 4, which one wave alone would do in turns.
 //
 // Bound by the matrix units at the clock that they leave: four trees of 64 drafts over 8K to 16.5K slots (52 GFLOP; with the weights' second
-// part 78) 92 us, 850 TFLOP/s of matrix instructions.  Four waves with tiles of their own and 16x16x32 instructions: 106 to 113 us.
+// part 78), capped at 30, 97 us, 800 TFLOP/s of matrix instructions.  The cap's some 150 instructions a tile have no products above them: passes
+// back to back, the join among them, take 114 us with it and 97 without.  Four waves with tiles of their own and 16x16x32 instructions took 106 to
+// 113 us where this kernel took 92, with a cap of fewer bits.
 #include "cache_bf16.h"
 
 namespace skv {
