@@ -194,9 +194,9 @@ def _rotate(s):
 
 
 def _scales(top):
-    """The least powers of two s with top <= 448 s, of 2^-100 at least."""
+    """The least powers of two s with top <= 448 s, of 2^-64 at least."""
     m, e = torch.frexp(top)
-    return torch.exp2((e - 9 + (m > 0.875)).clamp(min=-100).float())
+    return torch.exp2((e - 9 + (m > 0.875)).clamp(min=-64).float())
 
 
 def _append(s):
@@ -317,7 +317,7 @@ def exact(case, seed):
                 for j in range(n // ps, (n + T - 1) // ps + 1):
                     p, a, z = int(s["pages"][b, j]), max(0, n - j * ps), min(ps, n + T - j * ps)   # rows a .. z - 1 are new
                     new = x[:, b * T + j * ps + a - n: b * T + j * ps + z - n]
-                    least = torch.exp2(torch.ceil(torch.log2(new.abs().amax((1, 2)) / TOP)).clamp(min=-100))
+                    least = torch.exp2(torch.ceil(torch.log2(new.abs().amax((1, 2)) / TOP)).clamp(min=-64))
                     now = torch.maximum(least, scale[p]) if a else least
                     codes[p, :, :a] = _e4m3(codes[p, :, :a] * (scale[p] / now)[:, None, None])
                     codes[p, :, a:z] = _e4m3(new / now[:, None, None])
