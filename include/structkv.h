@@ -424,6 +424,132 @@ structkv_status structkv_cache_evict(const structkv_cache* cache, const float* s
                                      int32_t keep_tail, int32_t* lens_out, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
+/* ---- rotary positions -------------------------------------------------------------------------------------------------
+ *
+ * Pairs of components of a query or a key are turned by an angle that grows with its token's position, pair i by turns[i] / 2^64 of a full
+ * turn a position: fractions of 64 bits, so that position times turns modulo 2^64 is the angle, as exact at position 2^30 as at 1.
+ * The first rot_dim components of a head are turned, the others stay:
+ *   interleaved = 0: pairs (i, i + rot_dim/2),   1: pairs (2i, 2i + 1),   i < rot_dim/2
+ *   y_first = m (x_first cos - x_second sin),  y_second = m (x_second cos + x_first sin),  m = magnitude
+ */
+typedef struct {
+  const uint64_t* turns; /* DEVICE [rot_dim/2], 8-byte aligned (structkv_rotary_turns fills them in, on the host) */
+  int32_t rot_dim;       /* even, 2 .. head_dim */
+  int32_t interleaved;   /* 0 or 1 */
+  float magnitude;       /* finite; 1 unless the scaling asks for another */
+} structkv_rotary;
+
+/* How frequencies are scaled for contexts longer than those that a model was trained on (`original` positions). */
+enum {
+  STRUCTKV_ROTARY_PLAIN = 0,  /* f_i = base^(-2i/rot_dim) radians a position */
+  STRUCTKV_ROTARY_LINEAR = 1, /* f_i / factor */
+  STRUCTKV_ROTARY_NTK = 2,    /* base grows to base factor^(rot_dim/(rot_dim-2)): the lowest frequency is divided by factor, the highest stays */
+  STRUCTKV_ROTARY_YARN = 3,   /* from f_i (pairs of more than `low` turns over `original` positions) to f_i / factor (fewer than `high`), by a
+                                 ramp over i between floor(c(low)) and ceil(c(high)), held to [0, rot_dim-1], c(t) = rot_dim ln(original /
+                                 (2 pi t)) / (2 ln base);  magnitude 0.1 ln factor + 1 */
+  STRUCTKV_ROTARY_BANDS = 4   /* f_i / factor below `low` turns over `original` positions, f_i from `high` on, by the turns between */
+};
+
+/*
+ * HOST arithmetic (64 bits and more): turns_out[i] = f_i / (2 pi) 2^64 to the nearest, i < rot_dim/2, and the magnitude that belongs to
+ * the scaling.  base > 1; factor >= 1; original, low and high > 0 where the scaling reads them (YARN: low > high, as in 32 and 1; BANDS:
+ * low < high, as in 1 and 4).  turns_out: HOST [rot_dim/2]; magnitude_out: HOST.
+ */
+structkv_status structkv_rotary_turns(int32_t rot_dim, double base, int32_t scaling, double factor, double original, double low,
+                                      double high, uint64_t* turns_out, float* magnitude_out);
+
+/*
+ * out[r][h] = x[r][h] turned by pos[r], r < tokens, h < n_heads; the components from rot_dim on are copied.  inverse = 1: turned back
+ * by pos[r], and times m as before, which is the gradient of the call with inverse = 0 (with m = 1 also its inverse: with pos the
+ * distance, keys that are in use move to other positions).
+ * x, out: element (r, h, c) at r*stride_tok + h*stride_head + c, of `dtype`; out may be x where the strides are the same, and must not
+ * overlap it otherwise.  pos: DEVICE int32 [tokens], of any sign.  Any alignment to whole elements is taken; 16 bytes are fastest.
+ */
+structkv_status structkv_rotate(const structkv_rotary* rotary, const void* x, int64_t x_stride_tok, int64_t x_stride_head,
+                                int64_t tokens, int32_t n_heads, int32_t head_dim, int32_t dtype, const int32_t* pos, int32_t inverse,
+                                void* out, int64_t out_stride_tok, int64_t out_stride_head, void* stream);
+
+/* ---- a cache held in 8 bits, in pages ---------------------------------------------------------------------------------
+ *
+ * Keys and values as 8-bit floats (e4m3: sign, 4 bits of exponent, 3 of mantissa, largest 448, no infinities) in a pool of pages of
+ * page_size tokens; slot s of sequence b lies in page pages[b][s / page_size], row s % page_size.  A page has one scale for each KV head's
+ * keys and one for its values: what is stored stands for code times scale.
+ * The table, the scales and the lengths live on the device: a captured step can be replayed while they change.  A table entry outside
+ * [0, n_pages), such as -1, is a page that was dropped: attention sees none of its tokens and reads nothing of it.  Sequences may share pages
+ * that are no longer written.  Slots that are not in use are never looked at and may hold anything.
+ * mass[b][j] is the attention weight that the tokens of table entry j have gathered (the block-level score of Sec. 4.1, carried on by the
+ * decay of Eq. 3), what a program goes by when it drops pages.
+ */
+typedef struct {
+  void* k;               /* DEVICE e4m3: element (page p, KV head g, row i, c) at p*stride_page + g*stride_head + i*stride_tok + c */
+  void* v;               /* DEVICE: likewise, the same strides */
+  float* k_scale;        /* DEVICE [n_pages][n_kv_heads], what structkv_paged_append writes: powers of two, 2^-64 .. 2^64.  (A pool that was */
+  float* v_scale;        /* filled otherwise may have any positive scales of that range, if it is not appended to.) */
+  int64_t stride_page;   /* multiples of 16; rows must not overlap */
+  int64_t stride_head;
+  int64_t stride_tok;
+  int32_t n_kv_heads;    /* G >= 1 */
+  int32_t head_dim;      /* a multiple of 16, up to 256 */
+  int32_t dtype;         /* STRUCTKV_DTYPE_F32 or STRUCTKV_DTYPE_BF16: of new rows, queries and outputs */
+  int32_t page_size;     /* 16, 32, 64, 128 or 256 */
+  int32_t n_pages;       /* of the pool, >= 0 */
+  int32_t max_pages;     /* table entries of a sequence, >= 0: its capacity is max_pages*page_size slots, below 2^31 - 1024 */
+  int32_t batch;         /* 0 .. STRUCTKV_MAX_BATCH */
+  int64_t pages_stride;  /* of the table (and of mass), >= max_pages */
+  const int32_t* pages;  /* DEVICE: entry j of sequence b at b*pages_stride + j */
+  const int32_t* lens;   /* DEVICE [batch]: slots in use; outside [0, capacity]: the nearer bound */
+  float* mass;           /* DEVICE, laid out as pages, or NULL */
+  int32_t* missed;       /* DEVICE [batch], or NULL: as in structkv_cache */
+} structkv_paged;
+
+/* Most fresh tokens of a sequence in structkv_paged_attend. */
+#define STRUCTKV_MAX_CHUNK 4096
+
+/* Bytes of scratch of structkv_paged_attend for new_tokens fresh tokens in all, however they spread over the sequences.  0 on invalid
+ * arguments.  The workspace must be 256-byte aligned; it needs no initialisation, nothing in it outlives a call, and calls that may
+ * overlap in time need one each. */
+size_t structkv_paged_workspace_bytes(const structkv_paged* cache, int32_t n_q_heads, int64_t new_tokens);
+
+/*
+ * Store rows in the slots behind those in use, r = cu_new[b] + t, t < T_b = cu_new[b+1] - cu_new[b]:
+ *   slot lens[b] + t  <-  k_new[g][r], turned by the token's position where rotary is given, and v_new[g][r];  lens_out[b] = lens[b] + T_b
+ *   q_out[r][h] = q[r][h], turned likewise (q given: needs rotary)
+ * The position is pos_new[r], or lens[b] + t where pos_new is NULL.  Rotated values are rounded once, to the codes or to q_out's type.
+ * A page's scale for a KV head's keys (values alike): s(A) = the least power of two with A <= 448 s, held to 2^-64 .. 2^64, A the largest
+ * magnitude of the rows that come.  Where the page holds earlier rows of the sequence, the scale becomes max(scale, s(A)); if that is
+ * more than it was, the earlier codes are rounded again (powers of two: only values below 2^-6 of the new scale lose bits).  A code is
+ * value / scale to the nearest, ties to even.  A value that is not finite, or beyond 448 2^64, is stored as NaN, and does not count for A.
+ * A sequence whose rows do not fit its capacity, or would go to a dropped page, is left as it was: lens_out[b] = lens[b], missed[b] = 1
+ * (queries are rotated all the same); the caller clears missed[b] after making room.  The pages that rows go to must be no other
+ * sequence's, and not twice in its table.
+ * k_new, v_new: element (g, r, c) at g*new_stride_head + r*new_stride_tok + c; q, q_out: (r, h, c) at r*q_stride_tok + h*q_stride_head + c,
+ * q_out contiguous [new][H_q][d].  Nothing that comes in may overlap what goes out.  cu_new: HOST [batch+1], cu_new[0] = 0,
+ * non-decreasing.  lens_out must be another array than lens.
+ */
+structkv_status structkv_paged_append(const structkv_paged* cache, const void* k_new, const void* v_new, int64_t new_stride_head,
+                                      int64_t new_stride_tok, const int64_t* cu_new, const structkv_rotary* rotary,
+                                      const int32_t* pos_new, int32_t n_q_heads, const void* q, int64_t q_stride_tok,
+                                      int64_t q_stride_head, void* q_out, int32_t* lens_out, void* stream);
+
+/*
+ * Attention of fresh tokens over the cache.  The T_b = cu_new[b+1] - cu_new[b] fresh tokens of sequence b (0 .. STRUCTKV_MAX_CHUNK, and
+ * T_b H_q / G below 2^18) have been appended: the last T_b slots in use, B_b = lens[b] - T_b the slots before them.  For row r = cu_new[b] + t,
+ * query head h, KV head g = h / (H_q/G):
+ *   y_s = scale * q[r][h] . k[g][s],  x_s = softcap > 0 ? softcap * tanh(y_s / softcap) : y_s      over s <= B_b + t in pages of the pool
+ *   out[r][h] = sum_s a_s v[g][s],  a = softmax_s(x),  lse_out[r][h] = ln sum_s e^{x_s}
+ * A row that sees nothing gets out 0 and lse_out -infinity.  What rows do not see, NaN among it, does not reach them; a row that sees a
+ * NaN gets NaN: throughout where it is a key's, or a value's in a fresh slot behind the first, in that component for other values.
+ * lambda in (0, 1] (only with T_b <= 1 everywhere): the weights are gathered, for table entries j < ceil(lens[b] / page_size) of sequences with T_b = 1
+ *   mass[b][j] = lambda * mass[b][j] + sum over the page's slots and all query heads of a_s     (0 for a dropped page)
+ * lambda = 0: mass stays as it is.
+ * q: element (r, h, c) at r*q_stride_tok + h*q_stride_head + c; out [new][H_q][d] contiguous; lse_out [new][H_q] fp32.
+ * scale, softcap: as in structkv_cache_attend.  A sequence with lens[b] < T_b or missed[b] != 0 is one whose rows see nothing, and
+ * whose mass stays as it is.  Deterministic: the same call on the same lengths and table gives the same bits.
+ */
+structkv_status structkv_paged_attend(const structkv_paged* cache, int32_t n_q_heads, float scale, float softcap, const void* q,
+                                      int64_t q_stride_tok, int64_t q_stride_head, const int64_t* cu_new, float lambda, void* out,
+                                      float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,6 +25,8 @@ STRUCTKV_DTYPE_BF16 = 1
 STRUCTKV_MAX_BATCH = 64
 STRUCTKV_STATIC_TOPK_MAX_TOKENS = 1048576
 STRUCTKV_MAX_DRAFTS = 64
+STRUCTKV_MAX_CHUNK = 4096
+STRUCTKV_ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
 
 EXPORTS = (
     "structkv_last_error", "structkv_version", "structkv_workspace_bytes", "structkv_score_layer",
@@ -36,6 +38,8 @@ EXPORTS = (
     "structkv_pivot_workspace_bytes", "structkv_pivot_metrics", "structkv_score_layer_pivot", "structkv_transition_scores",
     "structkv_cache_workspace_bytes", "structkv_cache_append", "structkv_cache_attend", "structkv_cache_accept",
     "structkv_cache_evict",
+    "structkv_rotary_turns", "structkv_rotate",
+    "structkv_paged_workspace_bytes", "structkv_paged_append", "structkv_paged_attend",
     "structkv_debug_probs", "structkv_debug_score_steps",
 )
 
@@ -52,6 +56,20 @@ class structkv_cache(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("planes", ctypes.c_int32),
                 ("mass", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("cu_slots", ctypes.c_void_p),
                 ("batch", ctypes.c_int32), ("missed", ctypes.c_void_p)]
+
+
+class structkv_rotary(ctypes.Structure):
+    """How rows are turned by their positions; make_rotary fills it in (and keeps the frequencies alive)."""
+    _fields_ = [("turns", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
+class structkv_paged(ctypes.Structure):
+    """A cache held in 8 bits, in pages; make_paged fills it in from tensors (and keeps those alive)."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("stride_page", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("batch", ctypes.c_int32), ("pages_stride", ctypes.c_int64),
+                ("pages", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("mass", ctypes.c_void_p), ("missed", ctypes.c_void_p)]
 
 
 class StructKVError(RuntimeError):
@@ -128,6 +146,19 @@ _lib.structkv_cache_accept.restype = _i32
 _lib.structkv_cache_accept.argtypes = [_cp, _i32, _f32, _f32, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp]
 _lib.structkv_cache_evict.restype = _i32
 _lib.structkv_cache_evict.argtypes = [_cp, _vp, _vp, _i32, _vp, _vp, _sz, _vp]
+
+_rp, _pp = ctypes.POINTER(structkv_rotary), ctypes.POINTER(structkv_paged)
+_f64 = ctypes.c_double
+_lib.structkv_rotary_turns.restype = _i32
+_lib.structkv_rotary_turns.argtypes = [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp]
+_lib.structkv_rotate.restype = _i32
+_lib.structkv_rotate.argtypes = [_rp, _vp, _i64, _i64, _i64, _i32, _i32, _i32, _vp, _i32, _vp, _i64, _i64, _vp]
+_lib.structkv_paged_workspace_bytes.restype = _sz
+_lib.structkv_paged_workspace_bytes.argtypes = [_pp, _i32, _i64]
+_lib.structkv_paged_append.restype = _i32
+_lib.structkv_paged_append.argtypes = [_pp, _vp, _vp, _i64, _i64, _vp, _rp, _vp, _i32, _vp, _i64, _i64, _vp, _vp, _vp]
+_lib.structkv_paged_attend.restype = _i32
+_lib.structkv_paged_attend.argtypes = [_pp, _i32, _f32, _f32, _vp, _i64, _i64, _vp, _f32, _vp, _vp, _vp, _sz, _vp]
 
 
 def make_shape(n_q_heads: int, n_kv_heads: int, head_dim: int, window: int, dtype: int,
@@ -440,8 +471,8 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, cu_slots: Sequence[int], lens: 
 _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _cache_call(fn, cache: structkv_cache, stream, *args) -> None:
-    """The call on the cache's GPU: on `stream`, or on the current one of that GPU."""
+def _cache_call(fn, cache, stream, *args) -> None:
+    """The call on the GPU of a handle (a cache's, or a rotation's): on `stream`, or on the current one of that GPU."""
     index = cache.index
     if stream is None:
         raw = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
@@ -541,3 +572,118 @@ def structkv_cache_evict(cache: structkv_cache, scores: Optional[torch.Tensor], 
     _vector(lens_out, torch.int32, cache.batch, cache.index, "lens_out")
     _cache_call(_lib.structkv_cache_evict, cache, stream, _ptr(scores), _host_i64(budget), keep_tail, lens_out.data_ptr(), workspace.data_ptr(),
                 _workspace(cache, workspace))
+
+
+# ---- rotary positions ----------------------------------------------------------------------------------------------------------
+
+def structkv_rotary_turns(rot_dim: int, base: float, scaling: str = "none", factor: float = 1.0, original: float = 0.0, low: float = 0.0,
+                          high: float = 0.0):
+    """(turns, magnitude): int64 [rot_dim / 2] in host memory, the bits of 64-bit fractions of a turn a position, and the factor of cosine
+    and sine.  scaling: "none", "linear", "ntk", "yarn" (low, high: 32 and 1 turns over `original` positions) or "bands" (1 and 4)."""
+    _require(scaling in STRUCTKV_ROTARY_SCALINGS, "scaling must be one of %s" % ", ".join(STRUCTKV_ROTARY_SCALINGS))
+    turns, magnitude = torch.empty(max(0, rot_dim // 2), dtype=torch.int64), ctypes.c_float()
+    _check(_lib.structkv_rotary_turns(rot_dim, base, STRUCTKV_ROTARY_SCALINGS[scaling], factor, original, low, high, _ptr(turns),
+                                      ctypes.byref(magnitude)))
+    return turns, float(magnitude.value)
+
+
+def make_rotary(turns: torch.Tensor, interleaved: bool = False, magnitude: float = 1.0) -> structkv_rotary:
+    """turns: int64 [rot_dim / 2] on the GPU, as structkv_rotary_turns gives them."""
+    index = turns.get_device()
+    _require(turns.dtype is torch.int64 and turns.dim() == 1 and turns.is_contiguous() and index >= 0,
+             "turns must be a contiguous int64 vector on a GPU")
+    r = structkv_rotary(_ptr(turns), 2 * turns.numel(), int(bool(interleaved)), float(magnitude))
+    r.tensors, r.device, r.index = turns, turns.device, index
+    return r
+
+
+_codes = {torch.float32: STRUCTKV_DTYPE_F32, torch.bfloat16: STRUCTKV_DTYPE_BF16}
+
+
+def structkv_rotate(rotary: structkv_rotary, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor, inverse: bool = False, stream=None) -> None:
+    """x, out: [tokens, heads, head_dim] views with contiguous components, float32 or bfloat16 (out may be x); pos: int32 [tokens].
+    inverse: turned back, which is the gradient."""
+    _require(x.dim() == 3 and out.shape == x.shape and x.dtype in _codes and out.dtype is x.dtype, "x and out must be [tokens, heads, head_dim] of one float type")
+    tokens, heads, d = x.shape
+    (xt, xh, xc), (ot, oh, oc) = x.stride(), out.stride()
+    _require((xc == 1 and oc == 1) or d == 1, "x and out must have contiguous components")
+    _require(x.get_device() == rotary.index and out.get_device() == rotary.index, "x and out must be on the rotation's GPU")
+    _vector(pos, torch.int32, tokens, rotary.index, "pos")
+    if heads == 0:
+        return
+    _cache_call(_lib.structkv_rotate, rotary, stream, x.data_ptr(), xt, xh, tokens, heads, d, _codes[x.dtype], pos.data_ptr(), int(inverse), out.data_ptr(), ot, oh)
+
+
+# ---- a cache held in 8 bits, in pages ------------------------------------------------------------------------------------------
+
+def make_paged(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor,
+               dtype: torch.dtype = torch.bfloat16, mass: Optional[torch.Tensor] = None, missed: Optional[torch.Tensor] = None) -> structkv_paged:
+    """k, v: [n_pages, G, page_size, d] views of float8_e4m3fn (or uint8) sharing strides, d contiguous; k_scale, v_scale: fp32 [n_pages, G];
+    pages: int32 [batch, max_pages]; lens: int32 [batch]; dtype: of new rows, queries and outputs; mass: fp32 [batch, max_pages]; missed:
+    int32 [batch], zeros.  The tensors are kept alive by the result; `lens` is read by the calls, whose lens_out is another tensor."""
+    _require(k.dim() == 4 and v.shape == k.shape and v.stride() == k.stride() and v.dtype == k.dtype,
+             "k and v must be [n_pages, G, page_size, d] views of one dtype that share shape and strides")
+    _require(k.dtype in (torch.float8_e4m3fn, torch.uint8), "k and v must be float8_e4m3fn (or its bytes, uint8)")
+    _require(dtype in _codes, "dtype must be float32 or bfloat16")
+    n_pages, G, page_size, d = k.shape
+    _require(G >= 1 and d >= 1 and (k.stride(3) == 1 or d == 1), "k and v need a KV head, and contiguous components")
+    _require(pages.dim() == 2 and pages.dtype is torch.int32, "pages must be int32 [batch, max_pages]")
+    batch, max_pages = pages.shape
+    index = k.get_device()
+    _require(index >= 0 and v.device == k.device, "the cache must be on one GPU")
+    _vector(k_scale, torch.float32, n_pages * G, index, "k_scale")
+    _vector(v_scale, torch.float32, n_pages * G, index, "v_scale")
+    _vector(lens, torch.int32, batch, index, "lens")
+    _vector(missed, torch.int32, batch, index, "missed")
+    _require(pages.get_device() == index and (max_pages <= 1 or pages.stride(1) == 1), "pages must be on the cache's GPU, its rows contiguous")
+    stride = pages.stride(0) if batch > 1 else max_pages
+    if mass is not None:
+        _require(mass.dtype is torch.float32 and mass.shape == pages.shape and mass.get_device() == index and
+                 (max_pages <= 1 or mass.stride(1) == 1) and (batch <= 1 or mass.stride(0) == stride), "mass must be fp32, laid out as pages")
+    sp, sh, st, _ = k.stride()
+    c = structkv_paged(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), sp, sh, st, G, d, _codes[dtype], page_size, n_pages, max_pages, batch,
+                       stride, _ptr(pages), _ptr(lens), _ptr(mass), _ptr(missed))
+    c.tensors = (k, v, k_scale, v_scale, pages, lens, mass, missed)
+    c.tensor_dtype, c.device, c.index = dtype, k.device, index
+    return c
+
+
+def structkv_paged_workspace_bytes(cache: structkv_paged, n_q_heads: int, new_tokens: int) -> int:
+    return int(_lib.structkv_paged_workspace_bytes(ctypes.byref(cache), n_q_heads, new_tokens))
+
+
+def structkv_paged_append(cache: structkv_paged, k_new: torch.Tensor, v_new: torch.Tensor, cu_new: Sequence[int], lens_out: torch.Tensor,
+                          rotary: Optional[structkv_rotary] = None, pos_new: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                          q_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k_new, v_new: [G, new, d] views sharing strides; q: [new, H_q, d] view, rotated into q_out [new, H_q, d]; pos_new: int32 [new], or None
+    for the slots' own numbers."""
+    _require(len(cu_new) == cache.batch + 1, "cu_new needs batch + 1 entries")
+    new = cu_new[cache.batch]
+    shape, strides = k_new.shape, k_new.stride()
+    _require(len(shape) == 3 and shape[0] == cache.n_kv_heads and shape[1] >= new and shape[2] == cache.head_dim and v_new.shape == shape and
+             v_new.stride() == strides and strides[2] == 1 and k_new.dtype is cache.tensor_dtype and
+             v_new.dtype is cache.tensor_dtype and k_new.get_device() == cache.index and v_new.get_device() == cache.index,
+             "k_new and v_new must be [G, new tokens, head_dim] views sharing strides, of the cache's dtype and GPU, with contiguous components")
+    _require(rotary is None or rotary.index == cache.index, "rotary belongs to another device than the cache")
+    _vector(pos_new, torch.int32, new, cache.index, "pos_new")
+    _vector(lens_out, torch.int32, cache.batch, cache.index, "lens_out")
+    heads = st = sh = 0
+    if q is not None:
+        _require(q.dim() == 3 and q_out is not None, "q must be [new tokens, n_q_heads, head_dim], and q_out given")
+        heads = q.shape[1]
+        st, sh = _query_strides(cache, heads, q, new)
+        _vector(q_out, cache.tensor_dtype, new * heads * cache.head_dim, cache.index, "q_out")
+    _cache_call(_lib.structkv_paged_append, cache, stream, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], _host_i64(cu_new),
+                None if rotary is None else ctypes.byref(rotary), _ptr(pos_new), heads, _ptr(q), st, sh, _ptr(q_out), lens_out.data_ptr())
+
+
+def structkv_paged_attend(cache: structkv_paged, n_q_heads: int, q: torch.Tensor, cu_new: Sequence[int], out: torch.Tensor, lse_out: torch.Tensor,
+                          workspace: torch.Tensor, scale: float = 0.0, softcap: float = 0.0, lam: float = 0.0, stream=None) -> None:
+    """q: [new, H_q, d] view with d contiguous; out [new, H_q, d] and lse_out fp32 [new, H_q] contiguous."""
+    _require(len(cu_new) == cache.batch + 1, "cu_new needs batch + 1 entries")
+    new = cu_new[cache.batch]
+    st, sh = _query_strides(cache, n_q_heads, q, new)
+    _vector(out, cache.tensor_dtype, new * n_q_heads * cache.head_dim, cache.index, "out")
+    _vector(lse_out, torch.float32, new * n_q_heads, cache.index, "lse_out")
+    _cache_call(_lib.structkv_paged_attend, cache, stream, n_q_heads, scale, softcap, q.data_ptr(), st, sh, _host_i64(cu_new), lam,
+                out.data_ptr(), lse_out.data_ptr(), workspace.data_ptr(), _workspace(cache, workspace))

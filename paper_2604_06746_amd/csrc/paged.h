@@ -1,0 +1,69 @@
+// Internal declarations of the operators on a cache held in 8 bits, in pages (paged_*.hip, paged_api.cpp).
+#pragma once
+#include "cache.h"
+#include "rotary.h"
+
+namespace skv {
+
+// The cache as kernels see it.
+struct PagedView {
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+  int64_t sp, sh, st;       // strides in elements, which are bytes
+  const int32_t* pages;
+  int64_t pst;
+  const int32_t* lens;
+  float* mass;
+  int32_t* missed;
+  int G, d, shift, n_pages, max_pages, batch;   // shift: log2 of the page size
+};
+
+constexpr int kBlock = 16;        // slots that share a page whatever its size: what the attend kernels go by
+constexpr float kTopCode = 448.f;
+constexpr float kLeastScale = 0x1p-64f, kMostScale = 0x1p64f;
+
+// Fresh tokens of the sequences, by value in the kernel arguments.
+template <int N>
+struct FreshTab {
+  int32_t cu_new[N + 1];
+  int32_t batch;
+};
+template <class F>
+void with_fresh_table(const CacheTable& s, F f) {
+  auto take = [&](auto t) {
+    constexpr int n = sizeof(t.cu_new) / sizeof(int32_t);
+    for (int i = 0; i < n; ++i) t.cu_new[i] = s.cu_new[i];
+    t.batch = s.batch;
+    f(t);
+  };
+  if (s.batch > 8) take(FreshTab<kMaxBatch>{}); else take(FreshTab<8>{});
+}
+
+struct PagedRows {
+  const void *k, *v;
+  int64_t sh, st;
+  const int32_t* pos;       // or NULL: positions are the slots'
+  RotaryView rotary;
+  const void* q;            // or NULL
+  int64_t qst, qsh;
+  void* q_out;
+  int H;
+  int32_t* lens_out;
+};
+hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const PagedRows& w, bool bf16, hipStream_t st);
+
+// An attend call is cut like one on a cache of slots (AttendPlan, AttendWork): x in AttendWork are here the weights of blocks of kBlock slots
+// in the log2 domain, head h, block i of sequence b at h xs + b blocks + i.
+hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const AttendPlan& p,
+                               const AttendWork& w, bool bf16, hipStream_t st);
+// the weights gathered: mass <- lambda mass + what the heads' blocks hold, for sequences with a fresh token
+hipError_t launch_paged_mass(const CacheTable& t, const PagedView& c, const AttendWork& w, hipStream_t st);
+
+#ifdef __HIPCC__
+// slots in use
+__device__ __forceinline__ int paged_len(const PagedView& c, int b) {
+  return (int)min((int64_t)max(c.lens[b], 0), (int64_t)c.max_pages << c.shift);
+}
+#endif
+
+}  // namespace skv

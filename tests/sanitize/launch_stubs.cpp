@@ -366,3 +366,32 @@ hipError_t launch_cache_evict(const CacheTable& t, const CacheView&, const Evict
 }
 
 }  // namespace skv
+
+// ---- rotary positions and the cache held in pages: their entry points, compiled here, and their launchers -------------------------
+#include "../../paper_2604_06746_amd/csrc/paged_api.cpp"
+
+namespace skv {
+
+hipError_t launch_rotate(const RotaryView& r, const void*, int64_t, int64_t, int64_t tokens, int heads, int d, bool, const int32_t*, void*,
+                         int64_t, int64_t, hipStream_t) {
+  ++g_launches;
+  return r.half >= 1 && 2 * r.half <= d && r.d == d && tokens > 0 && heads > 0 ? hipSuccess : hipErrorInvalidValue;
+}
+hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const PagedRows& w, bool, hipStream_t) {
+  ++g_launches;
+  return t.batch == c.batch && w.lens_out && w.rotary.d == c.d && (!w.q || w.rotary.half > 0) ? hipSuccess : hipErrorInvalidValue;
+}
+hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm&, const AttendPlan& p,
+                               const AttendWork& w, bool, hipStream_t) {
+  const int dp = c.d <= 64 ? 64 : c.d <= 128 ? 128 : 256;
+  const size_t parts = p.join ? (size_t)(p.units * c.G * p.rows) : 0;
+  const bool ok = v.G == c.G && v.slots == t.cu[t.batch] && p.off_x - p.off_o >= parts * dp * 4 && (p.gather != 0) == (w.x != nullptr) && (!p.gather || p.rows == 16) &&
+                  (!p.gather || p.total_bytes - p.off_x >= (size_t)w.H * (size_t)w.xs * 4);
+  return attend_fits(t, p, w, c.G) && ok ? hipSuccess : hipErrorInvalidValue;
+}
+hipError_t launch_paged_mass(const CacheTable&, const PagedView& c, const AttendWork& w, hipStream_t) {
+  ++g_launches;
+  return c.mass && w.x ? hipSuccess : hipErrorInvalidValue;
+}
+
+}  // namespace skv
