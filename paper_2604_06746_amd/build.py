@@ -12,7 +12,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libstructkv.so")
 SOURCES = ["api.cpp", "score_mfma_ring.hip", "score_mfma_wide.hip", "score_f32.hip", "score_short.hip", "score_combine.hip", "topk.hip", "gather.hip",
            "aggregate.hip", "pivot.hip", "cache_api.cpp", "cache_rows.hip", "cache_attend_f32.hip", "cache_attend_bf16.hip", "cache_attend_rows.hip",
-           "cache_combine.hip", "cache_weights_bf16.hip", "cache_evict.hip", "paged_api.cpp", "rotate.hip", "paged_append.hip", "paged_attend.hip"]
+           "cache_combine.hip", "cache_weights_bf16.hip", "cache_evict.hip", "paged_api.cpp", "rotate.hip", "paged_append.hip", "paged_attend.hip", "paged_join.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-x", "hip",
          # packed-fp32 instruction selection is switched off for all device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -56,8 +56,8 @@ hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const Pa
 // in the log2 domain, head h, block i of sequence b at h xs + b blocks + i.
 hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const AttendPlan& p,
                                const AttendWork& w, bool bf16, hipStream_t st);
-// the weights gathered: mass <- lambda mass + what the heads' blocks hold, for sequences with a fresh token
-hipError_t launch_paged_mass(const CacheTable& t, const PagedView& c, const AttendWork& w, hipStream_t st);
+// a plan that gathers the weights: the chunks joined, and mass <- lambda mass + what the heads' blocks hold
+hipError_t launch_paged_join(const CacheTable& t, const PagedView& c, const AttendWork& w, bool bf16, hipStream_t st);
 
 #ifdef __HIPCC__
 // slots in use

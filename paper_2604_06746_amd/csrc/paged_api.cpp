@@ -126,7 +126,8 @@ structkv_status plan_paged(const PagedView& v, int H, bool gather, CacheTable* t
   }
   const bool cut = p->rows == 16 && cap >= kCut;
   p->units = std::max(blocks, std::min(chunks, std::max(kUnits / G, cut ? 2 * blocks : 0)));
-  if (p->units * G >= ((int64_t)1 << 31)) return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
+  const int64_t gathers = gather ? v.batch * ceil_div(block_slots(v), 64) + (int64_t)t->cu_new[v.batch] * H : 0;
+  if (p->units * G >= ((int64_t)1 << 31) || gathers >= ((int64_t)1 << 31)) return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
   p->join = gather || p->units > blocks;
   const int64_t each = std::max<int64_t>(p->min_chunk, ceil_div(cap * blocks, std::max<int64_t>(1, p->units)));
   p->most_chunks = blocks > 0 ? ceil_div(cap, each) : 0;
@@ -321,12 +322,8 @@ structkv_status structkv_paged_attend(const structkv_paged* cache, int32_t n_q_h
                         (int)p.units, gs_reciprocal(gs), lambda, (int64_t)t.cu_new[cache->batch] * n_q_heads, (int64_t)cache->batch * block_slots(v)};
   const bool bf16 = cache->dtype == STRUCTKV_DTYPE_BF16;
   SKV_HIP_CHECK(launch_paged_attend(t, view, v, f, p, w, bf16, (hipStream_t)stream));
-  if (p.join) {
-    AttendPlan join = p;   // (the join of a cache of slots gathers its weights by slots)
-    join.gather = 0;
-    SKV_HIP_CHECK(launch_cache_combine(t, view, join, w, bf16, (hipStream_t)stream));
-  }
-  if (p.gather) SKV_HIP_CHECK(launch_paged_mass(t, v, w, (hipStream_t)stream));
+  if (p.gather) SKV_HIP_CHECK(launch_paged_join(t, v, w, bf16, (hipStream_t)stream));
+  else if (p.join) SKV_HIP_CHECK(launch_cache_combine(t, view, p, w, bf16, (hipStream_t)stream));
   return STRUCTKV_OK;
 }
 

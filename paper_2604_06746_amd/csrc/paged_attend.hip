@@ -338,26 +338,6 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void paged_attend_kernel(TAB 
   finish_blocks<T, DP, RB>(O, M, Z, buf, w, c.d, p.g, row0, rows, new0, p.nc);
 }
 
-// Table entry j of sequence blockIdx.y: its blocks' weights, brought to the row's norm, over all heads.
-template <class TAB>
-__global__ __launch_bounds__(256) void paged_mass_kernel(TAB tab, PagedView c, AttendWork w) {
-  const int b = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x, lb = c.shift - 4;
-  const int n = c.missed && c.missed[b] ? 0 : paged_len(c, b);
-  if (tab.cu_new[b + 1] - tab.cu_new[b] != 1 || (int64_t)j << c.shift >= n) return;
-  const float* lse = w.lse + (int64_t)tab.cu_new[b] * w.H;
-  const int64_t at = b * c.pst + j;
-  float sum = 0.f;
-  if ((uint32_t)c.pages[at] < (uint32_t)c.n_pages) {
-    const int blocks = min(1 << lb, (n - (j << c.shift) + kBlock - 1) / kBlock);
-    const float* x = w.x + (((int64_t)b * c.max_pages + j) << lb);
-    for (int h = 0; h < w.H; ++h) {
-      const float norm = lse[h] * kLog2e;
-      for (int i = 0; i < blocks; ++i) sum += __builtin_amdgcn_exp2f(x[h * w.xs + i] - norm);
-    }
-  }
-  c.mass[at] = w.lambda * c.mass[at] + sum;
-}
-
 template <class T, int DP>
 hipError_t attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const AttendPlan& p, const AttendWork& w, hipStream_t st) {
   const bool aligned = (((uintptr_t)w.q | (uintptr_t)((w.qst | w.qsh) * (int64_t)sizeof(T))) & 15) == 0;
@@ -389,13 +369,6 @@ hipError_t by_dim(const CacheTable& t, const CacheView& v, const PagedView& c, c
 hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const AttendPlan& p,
                                const AttendWork& w, bool bf16, hipStream_t st) {
   return bf16 ? by_dim<uint16_t>(t, v, c, f, p, w, st) : by_dim<float>(t, v, c, f, p, w, st);
-}
-
-hipError_t launch_paged_mass(const CacheTable& t, const PagedView& c, const AttendWork& w, hipStream_t st) {
-  with_fresh_table(t, [&](const auto& tab) {
-    paged_mass_kernel<<<dim3((unsigned)ceil_div(c.max_pages, 256), (unsigned)c.batch), 256, 0, st>>>(tab, c, w);
-  });
-  return hipGetLastError();
 }
 
 }  // namespace skv

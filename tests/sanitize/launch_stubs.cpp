@@ -389,9 +389,9 @@ hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const Pa
                   (!p.gather || p.total_bytes - p.off_x >= (size_t)w.H * (size_t)w.xs * 4);
   return attend_fits(t, p, w, c.G) && ok ? hipSuccess : hipErrorInvalidValue;
 }
-hipError_t launch_paged_mass(const CacheTable&, const PagedView& c, const AttendWork& w, hipStream_t) {
+hipError_t launch_paged_join(const CacheTable&, const PagedView& c, const AttendWork& w, bool, hipStream_t) {
   ++g_launches;
-  return c.mass && w.x ? hipSuccess : hipErrorInvalidValue;
+  return c.mass && w.x && w.shares ? hipSuccess : hipErrorInvalidValue;
 }
 
 }  // namespace skv
