@@ -107,7 +107,7 @@ constexpr int64_t kCut = 4096;
 
 int64_t block_slots(const PagedView& v) { return ((int64_t)v.max_pages << v.shift) / kBlock; }
 
-structkv_status plan_paged(const PagedView& v, int H, bool gather, CacheTable* t, AttendPlan* p) {
+structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, CacheTable* t, AttendPlan* p) {
   const int64_t G = v.G, gs = H / v.G, cap = (int64_t)v.max_pages << v.shift;
   memset(p, 0, sizeof(*p));
   p->mfma = 1;
@@ -115,8 +115,9 @@ structkv_status plan_paged(const PagedView& v, int H, bool gather, CacheTable* t
   int64_t most_rows = 0;
   for (int b = 0; b < v.batch; ++b) most_rows = std::max<int64_t>(most_rows, (int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs);
   if (most_rows >= (1 << 18)) return fail(STRUCTKV_ERR_UNSUPPORTED, "%lld query rows of a KV head in one sequence, they must stay below 2^18", (long long)most_rows);
-  p->rows = gather || most_rows <= 16 ? 16 : 32;
+  p->rows = gather || most_rows <= 16 || (!bf16 && v.d > 128) ? 16 : 32;   // (32 rows of 256 components in fp32: no registers for it)
   p->min_chunk = kAttendWaves * 32;
+  p->stream = most_rows <= p->rows;
   int64_t blocks = 0, chunks = 0;
   for (int b = 0; b < v.batch; ++b) {
     const int64_t rcs = ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, p->rows);
@@ -309,7 +310,7 @@ structkv_status structkv_paged_attend(const structkv_paged* cache, int32_t n_q_h
     for (int b = 0; b < cache->batch; ++b)
       if (t.cu_new[b + 1] - t.cu_new[b] > 1) return fail(STRUCTKV_ERR_INVALID_ARG, "sequence %d: lambda > 0 is for single tokens", b);
   AttendPlan p;
-  st = plan_paged(v, n_q_heads, lambda > 0.f, &t, &p);
+  st = plan_paged(v, n_q_heads, lambda > 0.f, cache->dtype == STRUCTKV_DTYPE_BF16, &t, &p);
   if (st != STRUCTKV_OK) return st;
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(STRUCTKV_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
   if (workspace_bytes < p.total_bytes) return fail(STRUCTKV_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", workspace_bytes, p.total_bytes);

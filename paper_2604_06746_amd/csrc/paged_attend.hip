@@ -24,15 +24,31 @@ typedef __attribute__((ext_vector_type(4))) uint32_t four;
 // Weights are at most 2^kTop (65504 is fp16's last number); when one would be more, the reference is raised so that the largest is some 2^kFresh.
 constexpr float kTop = 15.f, kFresh = 7.f;
 
-template <int N> __device__ __forceinline__ void load_bytes(uint32_t (&to)[N / 4], const uint8_t* p) {
+// ONCE: past the caches
+template <int N, bool ONCE> __device__ __forceinline__ void load_bytes(uint32_t (&to)[N / 4], const uint8_t* p) {
   typedef __attribute__((ext_vector_type(N / 4))) uint32_t vec;
-  if constexpr (N == 4) {
-    to[0] = *reinterpret_cast<const uint32_t*>(p);
-  } else {
-    const vec x = *reinterpret_cast<const vec*>(p);
+  const vec x = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const vec*>(p)) : *reinterpret_cast<const vec*>(p);
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) to[i] = x[i];
-  }
+  for (int i = 0; i < N / 4; ++i) to[i] = x[i];
+}
+// an offset that is widened where it is used, so that the load takes it beside a base in scalar registers (widened ahead of a loop it costs
+// an addition of 64 bits a load, and registers whose reuse waits for loads)
+__device__ __forceinline__ uint32_t in_place(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// over the four lanes that share a row
+__device__ __forceinline__ float row_total(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ float row_top(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, bool high) {
   return __builtin_bit_cast(uint32_t, high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
@@ -126,10 +142,23 @@ __device__ __forceinline__ void finish_blocks(const floatx4 (&O)[DP / 16][RB], c
   }
 }
 
-template <class TAB, class T, int DP, int RB, bool CAPPED, bool SAVE>
-__global__ __launch_bounds__(64 * kAttendWaves, 2) void paged_attend_kernel(TAB tab, CacheView view, PagedView c, ScoreForm f, AttendWork w, bool aligned) {
+// Two blocks on their way, or at work: their codes, and what all lanes know of them.
+template <int DP>
+struct Pair {
+  uint32_t k[2][DP / 64][4], v[2][4][DP / 64];
+  float kf[2], lv[2], iv[2];   // of the scores; log2 of the values' scale, and its inverse
+  int at[2];                   // their places in the batch of 64 that starts at block `base`
+  int base;
+  bool any, two;
+};
+
+template <class TAB, class T, int DP, int RB, bool CAPPED, bool SAVE, bool ONCE>
+__global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void paged_attend_kernel(TAB tab, CacheView view, PagedView c, ScoreForm f, AttendWork w, bool aligned) {
   constexpr bool F32 = std::is_same<T, float>::value;
   constexpr int QP = F32 ? 3 : 1, PP = F32 ? 2 : 1, KP = DP / 64, W = DP / 16;
+  constexpr bool AHEAD = DP <= 128 && (RB == 1 || !F32);   // (the others have no registers for it)
+  constexpr int kBatch = 64, kPitch = kBatch + 1;
+  static_assert(!SAVE || kAttendWaves * 16 * kPitch <= kAttendWaves * 16 * RB * (DP + 4), "the blocks' weights lie where the waves' sums come later");
   __shared__ __attribute__((aligned(16))) float buf[kFinishFloats<DP, RB>];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -165,168 +194,213 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void paged_attend_kernel(TAB 
   const int lb = c.shift - 4, first = p.s0 / kBlock, last = end > p.s0 ? (end + kBlock - 1) / kBlock : first;
   const int share = ((last - first + 2 * kAttendWaves - 1) / (2 * kAttendWaves)) * 2;
   const int mine0 = first + wave * share, mine1 = min(last, mine0 + share);
-  float* save = SAVE ? w.x + (int64_t)(p.g * w.gs + min(row0 + l16, rows - 1)) * w.xs + ((int64_t)p.b * c.max_pages << lb) : nullptr;
-  for (int base = mine0; base < mine1; base += 64) {
-    const int block = base + lane;
-    const int page = block < mine1 ? c.pages[p.b * c.pst + (block >> lb)] : -1;
-    const bool live = (uint32_t)page < (uint32_t)c.n_pages;
-    const float ks = live ? c.k_scale[(int64_t)page * c.G + p.g] : 1.f, vs = live ? c.v_scale[(int64_t)page * c.G + p.g] : 1.f;
-    const float kf = CAPPED ? ks : ks * f.c2;
-    const float vc = fminf(fmaxf(vs, kLeastScale), kMostScale);
-    const float lv = __builtin_amdgcn_logf(vc), iv = 1.f / vc;
-    const int64_t off = (int64_t)page * c.sp + (int64_t)((block & ((1 << lb) - 1)) * kBlock) * c.st;
-    uint64_t todo = __ballot(live);
-    while (todo) {
-      int at[2];
-      at[0] = __builtin_ctzll(todo);
-      todo &= todo - 1;
-      const bool two = todo != 0;
-      at[1] = two ? __builtin_ctzll(todo) : at[0];
-      todo &= todo - 1;
-      uint32_t kr[2][KP][4], vr[2][4][W / 4];
-      float kb_f[2], lvb[2], ivb[2];
-      int s0[2];
+  // A lane's block of the batch that is being fetched: place and scales
+  float kf = 0.f, lv = 0.f, iv = 0.f;
+  int64_t off = 0;
+  uint64_t todo = 0;
+  int next = mine0, base = mine0;
+  // What a lane reads of a block.  In the place of components behind the last one it reads the first: queries have zeros there, and nobody
+  // asks for those of the result.
+  uint32_t k_at[KP], v_at[4];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const int64_t o = (int64_t)(((uint64_t)from_lane((uint32_t)((uint64_t)off >> 32), at[kb]) << 32) | from_lane((uint32_t)off, at[kb])) + p.g * c.sh;
-        kb_f[kb] = lane_float(kf, at[kb]);
-        lvb[kb] = lane_float(lv, at[kb]);
-        ivb[kb] = lane_float(iv, at[kb]);
-        s0[kb] = (base + at[kb]) * kBlock;
-        const uint8_t *kp = c.k + o + l16 * c.st + 16 * q4, *vp = c.v + o + 4 * q4 * c.st + W * l16;
+  for (int i = 0; i < KP; ++i) k_at[i] = (uint32_t)(l16 * c.st) + (64 * i + 16 * q4 < c.d ? 64 * i + 16 * q4 : 0);
 #pragma unroll
-        for (int i = 0; i < KP; ++i) {
-          if (64 * i + 16 * q4 < c.d) load_bytes<16>(kr[kb][i], kp + 64 * i);
-          else kr[kb][i][0] = kr[kb][i][1] = kr[kb][i][2] = kr[kb][i][3] = 0u;
-        }
+  for (int i = 0; i < 4; ++i) v_at[i] = (uint32_t)((4 * q4 + i) * c.st) + (W * l16 < c.d ? W * l16 : 0);
+  auto fetch = [&](Pair<DP>& x) __attribute__((always_inline)) {
+    while (todo == 0 && next < mine1) {
+      base = next;
+      next += kBatch;
+      const int block = base + lane;
+      const int page = block < mine1 ? c.pages[p.b * c.pst + (block >> lb)] : -1;
+      const bool live = (uint32_t)page < (uint32_t)c.n_pages;
+      const float ks = live ? c.k_scale[(int64_t)page * c.G + p.g] : 1.f, vs = live ? c.v_scale[(int64_t)page * c.G + p.g] : 1.f;
+      kf = CAPPED ? ks : ks * f.c2;
+      const float vc = fminf(fmaxf(vs, kLeastScale), kMostScale);
+      lv = __builtin_amdgcn_logf(vc);
+      iv = 1.f / vc;
+      off = (int64_t)page * c.sp + (int64_t)((block & ((1 << lb) - 1)) * kBlock) * c.st;
+      todo = __ballot(live);
+    }
+    x.any = todo != 0;
+    x.base = base;
+    x.at[0] = x.any ? __builtin_ctzll(todo) : 0;
+    todo &= todo - 1;
+    x.two = todo != 0;
+    x.at[1] = x.two ? __builtin_ctzll(todo) : x.at[0];
+    todo &= todo - 1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (W * l16 < c.d) load_bytes<W>(vr[kb][i], vp + i * c.st);
-          else
+    for (int kb = 0; kb < 2; ++kb) {
+      const int at = x.at[kb];
+      // The loads are made past the last block too, for the waits to count them: all lanes read the pool's first bytes, then.
+      const bool there = kb ? x.two : x.any;
+      const uint32_t lo = from_lane((uint32_t)off, at), hi = from_lane((uint32_t)((uint64_t)off >> 32), at), mask = there ? ~0u : 0u;
+      const int64_t place = there ? (int64_t)((uint64_t)hi << 32 | lo) + p.g * c.sh : 0;
+      x.kf[kb] = lane_float(kf, at);
+      x.lv[kb] = lane_float(lv, at);
+      x.iv[kb] = lane_float(iv, at);
+      const uint8_t *kp = c.k + place, *vp = c.v + place;
 #pragma unroll
-            for (int j = 0; j < W / 4; ++j) vr[kb][i][j] = 0u;
-        }
-      }
-      floatx4 x[2][RB];
+      for (int i = 0; i < KP; ++i) load_bytes<16, ONCE>(x.k[kb][i], kp + in_place(k_at[i] & mask));
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int i = 0; i < 4; ++i) load_bytes<W, ONCE>(x.v[kb][i], vp + in_place(v_at[i] & mask));
+    }
+  };
+  // the blocks' weights of a batch, in LDS row by row, on their way to memory
+  float* held = buf + wave * 16 * kPitch;
+  int held_base = mine0;
+  auto put_held = [&]() __attribute__((always_inline)) {
+    float* to = w.x + (int64_t)(p.g * w.gs + row0) * w.xs + ((int64_t)p.b * c.max_pages << lb) + held_base + lane;
+    const int some = min(16, rows - row0);
+    for (int r = 0; r < some; ++r) {
+      const float x = held[r * kPitch + lane];
+      if (held_base + lane < mine1) to[r * w.xs] = x;
+    }
+  };
+  auto work = [&](Pair<DP>& x) __attribute__((always_inline)) {
+    const int s0[2] = {(x.base + x.at[0]) * kBlock, (x.base + x.at[1]) * kBlock};
+    floatx4 y[2][RB];
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) x[kb][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-        for (int i = 0; i < KP; ++i)
+      for (int rb = 0; rb < RB; ++rb) y[kb][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const bf16x8 k8 = eight_keys(kr[kb][i][2 * half], kr[kb][i][2 * half + 1]);
+      for (int i = 0; i < KP; ++i)
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-              for (int part = QP - 1; part >= 0; --part)
-                x[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, qf[rb][2 * i + half][part], x[kb][rb], 0, 0, 0);
-          }
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          float y[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = x[kb][rb][e] * kb_f[kb];
-          if (CAPPED) cap.apply(y);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[kb][rb][e] = y[e];
-        }
-      }
-      if (max(s0[0], s0[1]) + kBlock > edge || !two) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (s0[kb] + 4 * q4 + e >= limit[rb] || (kb && !two)) x[kb][rb][e] = -INFINITY;
-          // values of slots that are not in use count for nothing; what is not a number in fresh slots would reach rows that do not see them
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int s = s0[kb] + 4 * q4 + i;
-#pragma unroll
-            for (int j = 0; j < W / 4; ++j) {
-              const uint32_t nan = ((vr[kb][i][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-              if (s >= n) vr[kb][i][j] = 0u;
-              else if (s > h.base && nan) {
-                odd = min(odd, s);
-                vr[kb][i][j] &= ~((nan >> 7) * 0xFFu);
-              }
-            }
-          }
-        }
-      }
-      bool high = false;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-          high |= fmaxf(fmaxf(x[kb][rb][0], x[kb][rb][1]), fmaxf(x[kb][rb][2], x[kb][rb][3])) - (M[rb] - lvb[kb]) > kTop;
-      if (__any(high)) {
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          float top = -INFINITY;
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-            top = fmaxf(top, fmaxf(fmaxf(x[kb][rb][0], x[kb][rb][1]), fmaxf(x[kb][rb][2], x[kb][rb][3])) + lvb[kb]);
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float Mn = fmaxf(M[rb], ceilf(top) - kFresh), shrink = __builtin_amdgcn_exp2f(M[rb] - Mn);
-          M[rb] = Mn;
-          Z[rb] *= shrink;
-#pragma unroll
-          for (int j = 0; j < W; ++j) O[j][rb] *= shrink;
-        }
-      }
-      halfx8 weight[RB][PP];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          const float m = M[rb] - lvb[kb];
-          float z = 0.f;
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            const floatx2 pr = {__builtin_amdgcn_exp2f(x[kb][rb][e] - m), __builtin_amdgcn_exp2f(x[kb][rb][e + 1] - m)};
-            z += pr[0] + pr[1];
-            floatx2 rest = pr;
-#pragma unroll
-            for (int part = 0; part < PP; ++part) {
-              const halfx2 r = __builtin_convertvector(rest, halfx2);
-              weight[rb][part][kb * 4 + e] = r[0];
-              weight[rb][part][kb * 4 + e + 1] = r[1];
-              rest = floatx2{rest[0] - (float)r[0], rest[1] - (float)r[1]};
-            }
-          }
-          Z[rb] = fmaf(z, ivb[kb], Z[rb]);
-          if (SAVE) {
-            z += __shfl_xor(z, 16);
-            z += __shfl_xor(z, 32);
-            if (q4 == 0 && row0 + l16 < rows && (kb == 0 || two)) save[base + at[kb]] = m + __builtin_amdgcn_logf(z);
-          }
-        }
-#pragma unroll
-      for (int j4 = 0; j4 < W / 4; ++j4) {
-        four v[4];   // components 4 j4 .. +3 of the lane's: eight slots each
-#pragma unroll
-        for (int pair = 0; pair < 4; ++pair) {
-          const uint32_t even = vr[pair >> 1][2 * (pair & 1)][j4], uneven = vr[pair >> 1][2 * (pair & 1) + 1][j4];
-          const uint32_t lo = __builtin_amdgcn_perm(uneven, even, 0x05010400u), hi = __builtin_amdgcn_perm(uneven, even, 0x07030602u);
-          v[0][pair] = half_pair(lo, false);
-          v[1][pair] = half_pair(lo, true);
-          v[2][pair] = half_pair(hi, false);
-          v[3][pair] = half_pair(hi, true);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int half = 0; half < 2; ++half) {
+          const bf16x8 k8 = eight_keys(x.k[kb][i][2 * half], x.k[kb][i][2 * half + 1]);
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-            for (int part = PP - 1; part >= 0; --part)
-              O[4 * j4 + j][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, v[j]), weight[rb][part], O[4 * j4 + j][rb], 0, 0, 0);
+            for (int part = QP - 1; part >= 0; --part)
+              y[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, qf[rb][2 * i + half][part], y[kb][rb], 0, 0, 0);
+        }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float z[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = y[kb][rb][e] * x.kf[kb];
+        if (CAPPED) cap.apply(z);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[kb][rb][e] = z[e];
       }
     }
+    if (max(s0[0], s0[1]) + kBlock > edge || !x.two) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (s0[kb] + 4 * q4 + e >= limit[rb] || !(kb ? x.two : x.any)) y[kb][rb][e] = -INFINITY;
+        // values of slots that are not in use count for nothing; what is not a number in fresh slots would reach rows that do not see them
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int s = s0[kb] + 4 * q4 + i;
+#pragma unroll
+          for (int j = 0; j < W / 4; ++j) {
+            const uint32_t nan = ((x.v[kb][i][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+            if (s >= n || !(kb ? x.two : x.any)) x.v[kb][i][j] = 0u;
+            else if (s > h.base && nan) {
+              odd = min(odd, s);
+              x.v[kb][i][j] &= ~((nan >> 7) * 0xFFu);
+            }
+          }
+        }
+      }
+    }
+    bool high = false;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+        high |= fmaxf(fmaxf(y[kb][rb][0], y[kb][rb][1]), fmaxf(y[kb][rb][2], y[kb][rb][3])) - (M[rb] - x.lv[kb]) > kTop;
+    if (__any(high)) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+          top = fmaxf(top, fmaxf(fmaxf(y[kb][rb][0], y[kb][rb][1]), fmaxf(y[kb][rb][2], y[kb][rb][3])) + x.lv[kb]);
+        top = row_top(top);
+        const float Mn = fmaxf(M[rb], ceilf(top) - kFresh), shrink = __builtin_amdgcn_exp2f(M[rb] - Mn);
+        M[rb] = Mn;
+        Z[rb] *= shrink;
+#pragma unroll
+        for (int j = 0; j < W; ++j) O[j][rb] *= shrink;
+      }
+    }
+    if (SAVE && x.base != held_base) {
+      put_held();
+      held_base = x.base;
+    }
+    halfx8 weight[RB][PP];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float m = M[rb] - x.lv[kb];
+        float z = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const floatx2 pr = {__builtin_amdgcn_exp2f(y[kb][rb][e] - m), __builtin_amdgcn_exp2f(y[kb][rb][e + 1] - m)};
+          z += pr[0] + pr[1];
+          floatx2 rest = pr;
+#pragma unroll
+          for (int part = 0; part < PP; ++part) {
+            const halfx2 r = __builtin_convertvector(rest, halfx2);
+            weight[rb][part][kb * 4 + e] = r[0];
+            weight[rb][part][kb * 4 + e + 1] = r[1];
+            rest = floatx2{rest[0] - (float)r[0], rest[1] - (float)r[1]};
+          }
+        }
+        Z[rb] = fmaf(z, x.iv[kb], Z[rb]);
+        if (SAVE) {
+          z = row_total(z);
+          if (q4 == 0 && (kb ? x.two : x.any)) held[l16 * kPitch + x.at[kb]] = m + __builtin_amdgcn_logf(z);
+        }
+      }
+#pragma unroll
+    for (int j4 = 0; j4 < W / 4; ++j4) {
+      four v[4];   // components 4 j4 .. +3 of the lane's: eight slots each
+#pragma unroll
+      for (int pair = 0; pair < 4; ++pair) {
+        const uint32_t even = x.v[pair >> 1][2 * (pair & 1)][j4], uneven = x.v[pair >> 1][2 * (pair & 1) + 1][j4];
+        const uint32_t lo = __builtin_amdgcn_perm(uneven, even, 0x05010400u), hi = __builtin_amdgcn_perm(uneven, even, 0x07030602u);
+        v[0][pair] = half_pair(lo, false);
+        v[1][pair] = half_pair(lo, true);
+        v[2][pair] = half_pair(hi, false);
+        v[3][pair] = half_pair(hi, true);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int part = PP - 1; part >= 0; --part)
+            O[4 * j4 + j][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, v[j]), weight[rb][part], O[4 * j4 + j][rb], 0, 0, 0);
+    }
+  };
+  // two pairs in turns: one at work while the other is on its way
+  // (a pool without pages has no memory that the loads past the last block could read)
+  Pair<DP> a;
+  a.any = false;
+  if (c.n_pages > 0) fetch(a);
+  if (a.any) {
+    if constexpr (AHEAD) {
+      Pair<DP> b;
+      do {   // (one way out: a second one, between the halves, makes the waits for loads give up their counts)
+        fetch(b);
+        work(a);
+        fetch(a);
+        if (b.any) work(b);
+      } while (a.any);
+    } else {
+      do {
+        work(a);
+        fetch(a);
+      } while (a.any);
+    }
+    if (SAVE) put_held();
   }
   if (__any(odd != 0x7FFFFFFF)) {
     for (int m = 32; m; m >>= 1) odd = min(odd, __shfl_xor(odd, m));
@@ -347,12 +421,15 @@ hipError_t attend(const CacheTable& t, const CacheView& v, const PagedView& c, c
     auto go = [&](auto rb, auto save) {
       constexpr int RB = decltype(rb)::value;
       constexpr bool SAVE = decltype(save)::value;
-      if (f.softcap > 0.f) paged_attend_kernel<TAB, T, DP, RB, true, SAVE><<<grid, block, 0, st>>>(tab, v, c, f, w, aligned);
-      else paged_attend_kernel<TAB, T, DP, RB, false, SAVE><<<grid, block, 0, st>>>(tab, v, c, f, w, aligned);
+      auto form = [&](auto capped, auto once) {
+        paged_attend_kernel<TAB, T, DP, RB, decltype(capped)::value, SAVE, decltype(once)::value><<<grid, block, 0, st>>>(tab, v, c, f, w, aligned);
+      };
+      auto by_cap = [&](auto once) { f.softcap > 0.f ? form(std::true_type{}, once) : form(std::false_type{}, once); };
+      p.stream ? by_cap(std::true_type{}) : by_cap(std::false_type{});
     };
     if (w.x) go(std::integral_constant<int, 1>{}, std::true_type{});
     else if (p.rows == 16) go(std::integral_constant<int, 1>{}, std::false_type{});
-    else go(std::integral_constant<int, 2>{}, std::false_type{});
+    else if constexpr (DP <= 128 || sizeof(T) == 2) go(std::integral_constant<int, 2>{}, std::false_type{});
   });
   return hipGetLastError();
 }
