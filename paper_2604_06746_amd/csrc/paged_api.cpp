@@ -274,7 +274,9 @@ structkv_status structkv_paged_append(const structkv_paged* cache, const void* k
     int64_t most = 0;
     for (int b = 0; b < cache->batch; ++b) most = std::max<int64_t>(most, t.cu_new[b + 1] - t.cu_new[b]);
     const int64_t pages = (most + cache->page_size - 2) / cache->page_size + 1;
-    if ((q ? ceil_div(total * n_q_heads * upr, 256) : 0) + (int64_t)cache->batch * pages * 2 * cache->n_kv_heads >= ((int64_t)1 << 31) - 1)
+    // (the queries' workgroups: fewer than 2^24, unless a thread takes all heads of a token's unit)
+    if ((q && total * upr >= ((int64_t)1 << 31) - ((int64_t)1 << 24)) ||
+        ((int64_t)1 << 25) + (q ? total * upr / 64 : 0) + (int64_t)cache->batch * pages * 2 * cache->n_kv_heads >= ((int64_t)1 << 31))
       return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows for one launch");
   }
   const PagedRows w = {k_new, v_new, new_stride_head, new_stride_tok, pos_new, r, total > 0 ? q : nullptr, q_stride_tok, q_stride_head, q_out,

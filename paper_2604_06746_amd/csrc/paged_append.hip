@@ -46,35 +46,73 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int u, const RotaryVie
   }
 }
 
-template <class TAB, class T, bool VEC>
-__global__ __launch_bounds__(256) void paged_append_kernel(TAB tab, PagedView c, PagedRows w, int q_blocks, int touched) {
-  const int upr = c.d / kUnit;
-  if ((int)blockIdx.x < q_blocks) {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = e / upr;
-    const int u = (int)(e - row * upr), r = (int)(row / w.H), h = (int)(row - (int64_t)r * w.H);
-    if (r >= tab.cu_new[tab.batch]) return;
+// Which workgroup takes what: `pages` of them what comes into the touched pages, the others queries.
+struct AppendCut {
+  int touched;         // most pages that a sequence's rows go to
+  int pages;           // workgroups for them
+  uint32_t upr_recip;  // ceil(2^20 / units of a row): divides what a workgroup counts (256 rows at most)
+  int heads, groups;   // query heads that a thread takes, and how many such groups there are
+  uint32_t units;      // query units: tokens x groups x units of a row
+};
+
+// HOLD: units of a thread, kept in registers from the search for the largest magnitude on.  ONE: a single token at most, which goes to the
+// page of slot lens[b], so that its row is on its way before the length is known.
+template <class TAB, class T, bool VEC, int HOLD, bool ONE>
+__global__ __launch_bounds__(1024) void paged_append_kernel(TAB tab, PagedView c, PagedRows w, AppendCut cut) {
+  short_kernel_priority();
+  const int upr = c.d / kUnit, lane = threadIdx.x & 63;
+  if ((int)blockIdx.x >= cut.pages) {   // queries: the angles of a token's unit serve several heads
+    const uint32_t e = (blockIdx.x - (uint32_t)cut.pages) * blockDim.x + threadIdx.x;
+    if (e >= cut.units) return;
+    const uint32_t rest = e / (uint32_t)upr;
+    const int u = (int)(e - rest * upr), r = (int)(rest / (uint32_t)cut.groups), h0 = (int)(rest - (uint32_t)r * cut.groups) * cut.heads;
     int b = 0;
     while (b + 1 < tab.batch && r >= tab.cu_new[b + 1]) ++b;
     const int pos = w.pos ? w.pos[r] : paged_len(c, b) + r - tab.cu_new[b];
-    Unit x = load_unit<T, VEC>((const T*)w.q + r * w.qst + h * w.qsh, u, w.rotary);
-    turn(x, spin_unit(w.rotary, u, pos), u, w.rotary);
-    store_unit<T, VEC>((T*)w.q_out + row * c.d, u, w.rotary, x);
+    const Spin spin = spin_unit(w.rotary, u, pos);
+    const T* from = (const T*)w.q + r * w.qst;
+    T* to = (T*)w.q_out + (int64_t)r * w.H * c.d;
+    for (int h = h0; h < min(w.H, h0 + cut.heads); ++h) {
+      Unit x = load_unit<T, VEC>(from + h * w.qsh, u, w.rotary);
+      turn(x, spin, u, w.rotary);
+      store_unit<T, VEC>(to + (int64_t)h * c.d, u, w.rotary, x);
+    }
     return;
   }
-  __shared__ float tops[4];
-  int i = (int)blockIdx.x - q_blocks;
+  __shared__ float tops[16];
+  int i = (int)blockIdx.x;
   const int which = i % (2 * c.G);
   i /= 2 * c.G;
-  const int k = i % touched, b = i / touched, g = which >> 1;
+  const int k = ONE ? 0 : i % cut.touched, b = ONE ? i : i / cut.touched, g = which >> 1;
   const bool values = which & 1;
-  const int fresh = tab.cu_new[b + 1] - tab.cu_new[b], n = paged_len(c, b), lane = threadIdx.x & 63;
+  const int fresh = tab.cu_new[b + 1] - tab.cu_new[b];
+  RotaryView r = w.rotary;
+  if (values) { r.half = 0; r.interleaved = 1; }
+  const T* src = (const T*)(values ? w.v : w.k) + g * w.sh + (int64_t)tab.cu_new[b] * w.st;
+  Unit x[HOLD];
+  auto load = [&](int r0, int rows) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < HOLD; ++m) {
+      const int e = (int)(threadIdx.x + m * blockDim.x), row = (int)(((uint32_t)e * cut.upr_recip) >> 20), u = e - row * upr;
+      x[m] = Unit{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      if (row < rows) x[m] = load_unit<T, VEC>(src + (int64_t)(r0 + row) * w.st, u, r);
+    }
+  };
+  if (ONE) load(0, fresh);
+  const int n = paged_len(c, b);
   const int first = n >> c.shift, last = (int)(((int64_t)n + fresh - 1) >> c.shift);
   // whether the rows fit, and all their pages are there: every workgroup of the sequence sees the same
   bool fits = (int64_t)n + fresh <= (int64_t)c.max_pages << c.shift;
-  if (fits && fresh > 0)
-    for (int j = first + lane; j <= last; j += 64) fits &= (uint32_t)c.pages[b * c.pst + j] < (uint32_t)c.n_pages;
+  int page = -1;
+  if (fits && fresh > 0) {
+    for (int j = first + lane; j <= last; j += 64) {
+      const int id = c.pages[b * c.pst + j];
+      fits &= (uint32_t)id < (uint32_t)c.n_pages;
+      if (j == first + k) page = id;
+    }
+  }
   fits = __all(fits);
+  page = __builtin_amdgcn_readlane(page, k & 63);
   if (k == 0 && which == 0 && threadIdx.x == 0) {
     w.lens_out[b] = fits ? n + fresh : n;
     if (!fits && c.missed) c.missed[b] = 1;
@@ -83,39 +121,31 @@ __global__ __launch_bounds__(256) void paged_append_kernel(TAB tab, PagedView c,
   if (!fits || fresh == 0 || j > last) return;
   const int page0 = j << c.shift, ps = 1 << c.shift;
   const int old = max(0, n - page0), r0 = page0 + old - n, rows = min(page0 + ps, n + fresh) - max(page0, n);   // fresh rows r0 .. r0 + rows - 1
-  const int64_t page = c.pages[b * c.pst + j];
-  RotaryView r = w.rotary;
-  if (values) { r.half = 0; r.interleaved = 1; }
-  const T* src = (const T*)(values ? w.v : w.k) + g * w.sh + (int64_t)(tab.cu_new[b] + r0) * w.st;
   uint8_t* dst = (values ? c.v : c.k) + page * c.sp + g * c.sh;
-  float* scale = (values ? c.v_scale : c.k_scale) + page * c.G + g;
-  auto get = [&](int e, int& row, int& u) __attribute__((always_inline)) {
-    row = e / upr;
-    u = e - row * upr;
-    Unit x = load_unit<T, VEC>(src + row * w.st, u, r);
-    if (r.half) turn(x, spin_unit(r, u, w.pos ? w.pos[tab.cu_new[b] + r0 + row] : n + r0 + row), u, r);
-    return x;
-  };
+  float* scale = (values ? c.v_scale : c.k_scale) + (int64_t)page * c.G + g;
+  if (!ONE) load(r0, rows);
+  const float before = old > 0 ? *scale : 0.f;
   float top = 0.f;
-  for (int e = threadIdx.x; e < rows * upr; e += 256) {
-    int row, u;
-    const Unit x = get(e, row, u);
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      top = storable(x.a[m]) ? fmaxf(top, fabsf(x.a[m])) : top;
-      top = storable(x.b[m]) ? fmaxf(top, fabsf(x.b[m])) : top;
+  for (int m = 0; m < HOLD; ++m) {
+    const int e = (int)(threadIdx.x + m * blockDim.x), row = (int)(((uint32_t)e * cut.upr_recip) >> 20), u = e - row * upr;
+    if (r.half && row < rows) turn(x[m], spin_unit(r, u, w.pos ? w.pos[tab.cu_new[b] + r0 + row] : n + r0 + row), u, r);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      top = storable(x[m].a[q]) ? fmaxf(top, fabsf(x[m].a[q])) : top;
+      top = storable(x[m].b[q]) ? fmaxf(top, fabsf(x[m].b[q])) : top;
     }
   }
   for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-  if (lane == 0) tops[threadIdx.x >> 6] = top;
-  const float before = old > 0 ? *scale : 0.f;
-  __syncthreads();
-  const float come = scale_for(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
-  const float now = fmaxf(come, before), inv = inverse(now);
-  if (threadIdx.x == 0) *scale = now;
+  if (blockDim.x > 64) {
+    if (lane == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int m = 0; m < (int)blockDim.x >> 6; ++m) top = fmaxf(top, tops[m]);
+  }
+  const float come = scale_for(top), now = fmaxf(come, before), inv = inverse(now);
   if (old > 0 && now > before) {   // the earlier rows' codes in the new scale
     const float ratio = before * inv;
-    for (int e = threadIdx.x; e < old * (c.d / 4); e += 256) {
+    for (int e = threadIdx.x; e < old * (c.d / 4); e += blockDim.x) {
       const int row = e / (c.d / 4);
       uint32_t* at = reinterpret_cast<uint32_t*>(dst + row * c.st + (e - row * (c.d / 4)) * 4);
       typedef __attribute__((ext_vector_type(2))) float floatx2;
@@ -123,15 +153,17 @@ __global__ __launch_bounds__(256) void paged_append_kernel(TAB tab, PagedView c,
       *at = four_codes(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
     }
   }
-  for (int e = threadIdx.x; e < rows * upr; e += 256) {
-    int row, u;
-    Unit x = get(e, row, u);
+  if (threadIdx.x == 0) *scale = now;   // (every thread has read it: the largest of all has been exchanged)
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      x.a[m] = storable(x.a[m]) ? x.a[m] * inv : NAN;
-      x.b[m] = storable(x.b[m]) ? x.b[m] * inv : NAN;
+  for (int m = 0; m < HOLD; ++m) {
+    const int e = (int)(threadIdx.x + m * blockDim.x), row = (int)(((uint32_t)e * cut.upr_recip) >> 20), u = e - row * upr;
+    if (row >= rows) continue;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      x[m].a[q] = storable(x[m].a[q]) ? x[m].a[q] * inv : NAN;
+      x[m].b[q] = storable(x[m].b[q]) ? x[m].b[q] * inv : NAN;
     }
-    store_codes<VEC>(dst + (old + row) * c.st, u, r, x);
+    store_codes<VEC>(dst + (old + row) * c.st, u, r, x[m]);
   }
 }
 
@@ -144,16 +176,34 @@ hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const Pa
   const bool vec = bits % 16 == 0 && whole_units(w.rotary);
   int64_t most = 0;
   for (int b = 0; b < t.batch; ++b) most = std::max<int64_t>(most, t.cu_new[b + 1] - t.cu_new[b]);
-  const int64_t ps = (int64_t)1 << c.shift, touched = std::max<int64_t>(1, most > 0 ? (most + ps - 2) / ps + 1 : 1);
-  const int64_t q_blocks = w.q ? ceil_div((int64_t)t.cu_new[t.batch] * w.H * upr, 256) : 0;
-  const int64_t blocks = q_blocks + (int64_t)t.batch * touched * 2 * c.G;
+  const int ps = 1 << c.shift;
+  AppendCut cut;
+  cut.touched = (int)(most > 0 ? (most + ps - 2) / ps + 1 : 1);
+  cut.pages = t.batch * cut.touched * 2 * c.G;
+  cut.upr_recip = (uint32_t)(((1u << 20) + upr - 1) / upr);
+  // threads: four units each, from a wave to sixteen
+  const int units = (int)std::min<int64_t>(std::max<int64_t>(1, most), ps) * upr;
+  int threads = 64;
+  while (threads < 1024 && threads * 4 < units) threads *= 2;
+  // query heads of a thread: as many as leave the chip filled
+  const int64_t tokens = w.q ? t.cu_new[t.batch] : 0;
+  cut.heads = w.q ? (int)std::min<int64_t>(w.H, std::max<int64_t>(1, tokens * upr * w.H / (1 << 18))) : 1;
+  cut.groups = w.q ? (int)ceil_div(w.H, cut.heads) : 1;
+  cut.units = (uint32_t)(tokens * cut.groups * upr);
+  const int64_t blocks = cut.pages + ceil_div((int64_t)cut.units, threads);
   with_fresh_table(t, [&](const auto& tab) {
     using TAB = std::decay_t<decltype(tab)>;
-    auto go = [&](auto elem, auto v) {
-      paged_append_kernel<TAB, decltype(elem), decltype(v)::value><<<(unsigned)blocks, 256, 0, st>>>(tab, c, w, (int)q_blocks, (int)touched);
+    auto go = [&](auto elem, auto v, auto hold, auto one) {
+      paged_append_kernel<TAB, decltype(elem), decltype(v)::value, decltype(hold)::value, decltype(one)::value>
+          <<<(unsigned)blocks, threads, 0, st>>>(tab, c, w, cut);
     };
-    if (bf16) vec ? go(uint16_t{}, std::true_type{}) : go(uint16_t{}, std::false_type{});
-    else vec ? go(float{}, std::true_type{}) : go(float{}, std::false_type{});
+    auto by_size = [&](auto elem, auto v) {
+      if (most <= 1) go(elem, v, std::integral_constant<int, 1>{}, std::true_type{});
+      else if (units <= 4 * threads) go(elem, v, std::integral_constant<int, 4>{}, std::false_type{});
+      else go(elem, v, std::integral_constant<int, 8>{}, std::false_type{});
+    };
+    if (bf16) vec ? by_size(uint16_t{}, std::true_type{}) : by_size(uint16_t{}, std::false_type{});
+    else vec ? by_size(float{}, std::true_type{}) : by_size(float{}, std::false_type{});
   });
   return hipGetLastError();
 }
