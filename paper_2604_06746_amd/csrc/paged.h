@@ -60,6 +60,15 @@ hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const Pa
 hipError_t launch_paged_join(const CacheTable& t, const PagedView& c, const AttendWork& w, bool bf16, hipStream_t st);
 
 #ifdef __HIPCC__
+// The sequence of packed row r, which grows by little over the lanes: the count of those that end at or before the first lane's row, by a
+// look of each lane at one end (one behind the other they cost 64 sequences 3 us), and on from there.
+template <class TAB>
+__device__ __forceinline__ int sequence_of(const TAB& t, int r) {
+  const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane(r);
+  int b = __popcll(__ballot(lane < t.batch && t.cu_new[min(lane, t.batch - 1) + 1] <= first));
+  while (b + 1 < t.batch && r >= t.cu_new[b + 1]) ++b;
+  return b;
+}
 // slots in use
 __device__ __forceinline__ int paged_len(const PagedView& c, int b) {
   return (int)min((int64_t)max(c.lens[b], 0), (int64_t)c.max_pages << c.shift);

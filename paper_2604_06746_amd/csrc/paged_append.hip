@@ -66,8 +66,7 @@ __global__ __launch_bounds__(1024) void paged_append_kernel(TAB tab, PagedView c
     if (e >= cut.units) return;
     const uint32_t rest = e / (uint32_t)upr;
     const int u = (int)(e - rest * upr), r = (int)(rest / (uint32_t)cut.groups), h0 = (int)(rest - (uint32_t)r * cut.groups) * cut.heads;
-    int b = 0;
-    while (b + 1 < tab.batch && r >= tab.cu_new[b + 1]) ++b;
+    const int b = sequence_of(tab, r);
     const int pos = w.pos ? w.pos[r] : paged_len(c, b) + r - tab.cu_new[b];
     const Spin spin = spin_unit(w.rotary, u, pos);
     const T* from = (const T*)w.q + r * w.qst;

@@ -195,7 +195,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
   const int share = ((last - first + 2 * kAttendWaves - 1) / (2 * kAttendWaves)) * 2;
   const int mine0 = first + wave * share, mine1 = min(last, mine0 + share);
   // A lane's block of the batch that is being fetched: place and scales
-  float kf = 0.f, lv = 0.f, iv = 0.f;
+  float ks = 1.f, vs = 1.f, kf = 0.f, lv = 0.f, iv = 0.f;
   int64_t off = 0;
   uint64_t todo = 0;
   int next = mine0, base = mine0;
@@ -207,17 +207,17 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
 #pragma unroll
   for (int i = 0; i < 4; ++i) v_at[i] = (uint32_t)((4 * q4 + i) * c.st) + (W * l16 < c.d ? W * l16 : 0);
   auto fetch = [&](Pair<DP>& x) __attribute__((always_inline)) {
+    bool turned = false;   // to another batch
     while (todo == 0 && next < mine1) {
+      turned = true;
       base = next;
       next += kBatch;
       const int block = base + lane;
       const int page = block < mine1 ? c.pages[p.b * c.pst + (block >> lb)] : -1;
       const bool live = (uint32_t)page < (uint32_t)c.n_pages;
-      const float ks = live ? c.k_scale[(int64_t)page * c.G + p.g] : 1.f, vs = live ? c.v_scale[(int64_t)page * c.G + p.g] : 1.f;
-      kf = CAPPED ? ks : ks * f.c2;
-      const float vc = fminf(fmaxf(vs, kLeastScale), kMostScale);
-      lv = __builtin_amdgcn_logf(vc);
-      iv = 1.f / vc;
+      const int64_t at = (int64_t)(live ? page : 0) * c.G + p.g;
+      ks = c.k_scale[at];
+      vs = c.v_scale[at];
       off = (int64_t)page * c.sp + (int64_t)((block & ((1 << lb) - 1)) * kBlock) * c.st;
       todo = __ballot(live);
     }
@@ -235,14 +235,23 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
       const bool there = kb ? x.two : x.any;
       const uint32_t lo = from_lane((uint32_t)off, at), hi = from_lane((uint32_t)((uint64_t)off >> 32), at), mask = there ? ~0u : 0u;
       const int64_t place = there ? (int64_t)((uint64_t)hi << 32 | lo) + p.g * c.sh : 0;
-      x.kf[kb] = lane_float(kf, at);
-      x.lv[kb] = lane_float(lv, at);
-      x.iv[kb] = lane_float(iv, at);
       const uint8_t *kp = c.k + place, *vp = c.v + place;
 #pragma unroll
       for (int i = 0; i < KP; ++i) load_bytes<16, ONCE>(x.k[kb][i], kp + in_place(k_at[i] & mask));
 #pragma unroll
       for (int i = 0; i < 4; ++i) load_bytes<W, ONCE>(x.v[kb][i], vp + in_place(v_at[i] & mask));
+    }
+    if (turned) {   // (the scales come while the codes are on their way)
+      kf = CAPPED ? ks : ks * f.c2;
+      const float vc = fminf(fmaxf(vs, kLeastScale), kMostScale);
+      lv = __builtin_amdgcn_logf(vc);
+      iv = 1.f / vc;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      x.kf[kb] = lane_float(kf, x.at[kb]);
+      x.lv[kb] = lane_float(lv, x.at[kb]);
+      x.iv[kb] = lane_float(iv, x.at[kb]);
     }
   };
   // the blocks' weights of a batch, in LDS row by row, on their way to memory
@@ -388,12 +397,13 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
   if (a.any) {
     if constexpr (AHEAD) {
       Pair<DP> b;
-      do {   // (one way out: a second one, between the halves, makes the waits for loads give up their counts)
+      while (todo != 0 || next < mine1) {   // (one way out: a second one, between the halves, makes the waits for loads give up their counts)
         fetch(b);
         work(a);
         fetch(a);
         if (b.any) work(b);
-      } while (a.any);
+      }
+      if (a.any) work(a);
     } else {
       do {
         work(a);

@@ -49,8 +49,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, A
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int)blockIdx.x < row_blocks) {   // a row: lane groups on shares of its chunks
     const int r = (int)(blockIdx.x / (uint32_t)w.H), head = (int)blockIdx.x - r * w.H;
-    int b = 0;
-    while (b + 1 < tab.batch && r >= tab.cu_new[b + 1]) ++b;
+    const int b = sequence_of(tab, r);
     const int4 share = w.shares[b];
     const int g = token_of(w, head), mine = head - g * w.gs;   // (a single token's rows are its heads)
     const int64_t part0 = ((int64_t)(share.x + mine / 16) * c.G + g) * 16 + mine % 16, step = (int64_t)(tab.units[b + 1] - tab.units[b]) * c.G * 16;
