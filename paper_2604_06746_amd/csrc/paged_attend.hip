@@ -283,16 +283,22 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
             for (int part = QP - 1; part >= 0; --part)
               y[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, qf[rb][2 * i + half][part], y[kb][rb], 0, 0, 0);
         }
+      if (CAPPED) {
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        float z[4];
+        for (int rb = 0; rb < RB; ++rb) {
+          float z[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = y[kb][rb][e] * x.kf[kb];
-        if (CAPPED) cap.apply(z);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[kb][rb][e] = z[e];
+          for (int e = 0; e < 4; ++e) z[e] = y[kb][rb][e] * x.kf[kb];
+          cap.apply(z);
+          y[kb][rb] = floatx4{z[0], z[1], z[2], z[3]};
+        }
       }
     }
+    // (capped scores are in the log2 domain; the others are still to be multiplied)
+    const float f2[2] = {CAPPED ? 1.f : x.kf[0], CAPPED ? 1.f : x.kf[1]};
+    auto best = [&](int kb, int rb) __attribute__((always_inline)) {
+      return fmaxf(fmaxf(y[kb][rb][0], y[kb][rb][1]), fmaxf(y[kb][rb][2], y[kb][rb][3]));
+    };
     if (max(s0[0], s0[1]) + kBlock > edge || !x.two) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
@@ -322,14 +328,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
-        high |= fmaxf(fmaxf(y[kb][rb][0], y[kb][rb][1]), fmaxf(y[kb][rb][2], y[kb][rb][3])) - (M[rb] - x.lv[kb]) > kTop;
+        high |= fmaf(best(kb, rb), f2[kb], x.lv[kb] - M[rb]) > kTop;
     if (__any(high)) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         float top = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
-          top = fmaxf(top, fmaxf(fmaxf(y[kb][rb][0], y[kb][rb][1]), fmaxf(y[kb][rb][2], y[kb][rb][3])) + x.lv[kb]);
+          top = fmaxf(top, fmaf(best(kb, rb), f2[kb], x.lv[kb]));
         top = row_top(top);
         const float Mn = fmaxf(M[rb], ceilf(top) - kFresh), shrink = __builtin_amdgcn_exp2f(M[rb] - Mn);
         M[rb] = Mn;
@@ -347,11 +353,11 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const float m = M[rb] - x.lv[kb];
+        const float m = x.lv[kb] - M[rb];
         float z = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; e += 2) {
-          const floatx2 pr = {__builtin_amdgcn_exp2f(y[kb][rb][e] - m), __builtin_amdgcn_exp2f(y[kb][rb][e + 1] - m)};
+          const floatx2 pr = {__builtin_amdgcn_exp2f(fmaf(y[kb][rb][e], f2[kb], m)), __builtin_amdgcn_exp2f(fmaf(y[kb][rb][e + 1], f2[kb], m))};
           z += pr[0] + pr[1];
           floatx2 rest = pr;
 #pragma unroll
@@ -365,7 +371,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
         Z[rb] = fmaf(z, x.iv[kb], Z[rb]);
         if (SAVE) {
           z = row_total(z);
-          if (q4 == 0 && (kb ? x.two : x.any)) held[l16 * kPitch + x.at[kb]] = m + __builtin_amdgcn_logf(z);
+          if (q4 == 0 && (kb ? x.two : x.any)) held[l16 * kPitch + x.at[kb]] = __builtin_amdgcn_logf(z) - m;
         }
       }
 #pragma unroll
