@@ -95,50 +95,49 @@ __device__ __forceinline__ void load_query(bf16x8 (&q)[QP], const T* row, int c,
   }
 }
 
-// What the waves of a workgroup leave, added up in their order through LDS and written out by all threads (leave).  A lane holds components
-// 4 W q4 + W e + j of its rows in O[j][rb][e].
+// What the waves of a workgroup leave, added up in their order through LDS and written out by all threads (leave), 16 rows at a time.  A lane
+// holds components 4 W q4 + W e + j of its rows in O[j][rb][e].
+template <int DP>
+constexpr int kFinishBlocks = kAttendWaves * 16 * (DP + 4 + 2);
 template <class T, int DP, int RB>
 __device__ __forceinline__ void finish_blocks(const floatx4 (&O)[DP / 16][RB], const float (&M)[RB], const float (&Zl)[RB], float* buf,
                                               const AttendWork& w, int d, int g, int row0, int rows, int new0, int nc) {
-  constexpr int ROWS = 16 * RB, PITCH = DP + 4, W = DP / 16;
+  constexpr int PITCH = DP + 4, W = DP / 16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q4 = lane >> 4;
-  float* ml = buf + kAttendWaves * ROWS * PITCH;   // [wave][row][2]
+  float* ml = buf + kAttendWaves * 16 * PITCH;   // [wave][row][2]
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    float z = Zl[rb] + __shfl_xor(Zl[rb], 16);
-    z += __shfl_xor(z, 32);
+    if (row0 + rb * 16 >= rows) break;
+    const float z = row_total(Zl[rb]);
+    if (rb > 0) __syncthreads();
     if (q4 == 0) {
-      ml[(wave * ROWS + rb * 16 + l16) * 2] = M[rb];
-      ml[(wave * ROWS + rb * 16 + l16) * 2 + 1] = z;
+      ml[(wave * 16 + l16) * 2] = M[rb];
+      ml[(wave * 16 + l16) * 2 + 1] = z;
     }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int row = rb * 16 + l16;
-    float top = ml[row * 2];
-    for (int i = 1; i < kAttendWaves; ++i) top = fmaxf(top, ml[(i * ROWS + row) * 2]);
+    __syncthreads();
+    float top = ml[l16 * 2];
+    for (int i = 1; i < kAttendWaves; ++i) top = fmaxf(top, ml[(i * 16 + l16) * 2]);
     const float f = __builtin_amdgcn_exp2f(M[rb] - top);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int j = 0; j < W; j += 4)
-        *reinterpret_cast<floatx4*>(buf + (wave * ROWS + row) * PITCH + W * (4 * q4 + e) + j) =
+        *reinterpret_cast<floatx4*>(buf + (wave * 16 + l16) * PITCH + W * (4 * q4 + e) + j) =
             floatx4{O[j][rb][e], O[j + 1][rb][e], O[j + 2][rb][e], O[j + 3][rb][e]} * f;
-  }
-  __syncthreads();
-  for (int e = threadIdx.x; e < ROWS * (DP / 4); e += 64 * kAttendWaves) {
-    const int row = e / (DP / 4), c = e % (DP / 4) * 4;
-    if (row0 + row >= rows || c >= d) continue;
-    float top = ml[row * 2];
-    for (int i = 1; i < kAttendWaves; ++i) top = fmaxf(top, ml[(i * ROWS + row) * 2]);
-    float z = 0.f;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < kAttendWaves; ++i) {
-      z += ml[(i * ROWS + row) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(i * ROWS + row) * 2] - top);
-      o += *reinterpret_cast<const floatx4*>(buf + (i * ROWS + row) * PITCH + c);
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * (DP / 4); e += 64 * kAttendWaves) {
+      const int row = e / (DP / 4), c = e % (DP / 4) * 4;
+      if (row0 + rb * 16 + row >= rows || c >= d) continue;
+      float best = ml[row * 2];
+      for (int i = 1; i < kAttendWaves; ++i) best = fmaxf(best, ml[(i * 16 + row) * 2]);
+      float sum = 0.f;
+      floatx4 o = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < kAttendWaves; ++i) {
+        sum += ml[(i * 16 + row) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(i * 16 + row) * 2] - best);
+        o += *reinterpret_cast<const floatx4*>(buf + (i * 16 + row) * PITCH + c);
+      }
+      leave<T, DP>(w, d, g, row0 + rb * 16 + row, c, best, sum, o, new0, (int64_t)blockIdx.x * 16 * RB + rb * 16 + row, nc);
     }
-    leave<T, DP>(w, d, g, row0 + row, c, top, z, o, new0, (int64_t)blockIdx.x * ROWS + row, nc);
   }
 }
 
@@ -158,8 +157,8 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
   constexpr int QP = F32 ? 3 : 1, PP = F32 ? 2 : 1, KP = DP / 64, W = DP / 16;
   constexpr bool AHEAD = DP <= 128 && (RB == 1 || !F32);   // (the others have no registers for it)
   constexpr int kBatch = 64, kPitch = kBatch + 1;
-  static_assert(!SAVE || kAttendWaves * 16 * kPitch <= kAttendWaves * 16 * RB * (DP + 4), "the blocks' weights lie where the waves' sums come later");
-  __shared__ __attribute__((aligned(16))) float buf[kFinishFloats<DP, RB>];
+  static_assert(!SAVE || kAttendWaves * 16 * kPitch <= kAttendWaves * 16 * (DP + 4), "the blocks' weights lie where the waves' sums come later");
+  __shared__ __attribute__((aligned(16))) float buf[kFinishBlocks<DP>];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const AttendPlace p = attend_place(tab, view, w);
