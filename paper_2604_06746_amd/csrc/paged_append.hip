@@ -31,10 +31,11 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int u, const RotaryVie
     a = four_codes(x.a[0], x.b[0], x.a[1], x.b[1]);
     b = four_codes(x.a[2], x.b[2], x.a[3], x.b[3]);
   }
-  if (VEC) {
-    const bool split = unit_split(r, u);
-    *reinterpret_cast<uint32_t*>(row + (split ? 4 * u : 8 * u)) = a;
-    *reinterpret_cast<uint32_t*>(row + (split ? 4 * u + r.half : 8 * u + 4)) = b;
+  if (VEC && unit_split(r, u)) {
+    *reinterpret_cast<uint32_t*>(row + 4 * u) = a;
+    *reinterpret_cast<uint32_t*>(row + 4 * u + r.half) = b;
+  } else if (VEC) {
+    *reinterpret_cast<uint64_t*>(row + 8 * u) = (uint64_t)b << 32 | a;
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -52,13 +53,16 @@ struct AppendCut {
   int pages;           // workgroups for them
   uint32_t upr_recip;  // ceil(2^20 / units of a row): divides what a workgroup counts (256 rows at most)
   int heads, groups;   // query heads that a thread takes, and how many such groups there are
+  int once;            // 1: queries go past the caches
+  int keys;            // KV heads whose keys a workgroup takes one behind the other, for the angles serve all of them
   uint32_t units;      // query units: tokens x groups x units of a row
 };
 
 // HOLD: units of a thread, kept in registers from the search for the largest magnitude on.  ONE: a single token at most, which goes to the
 // page of slot lens[b], so that its row is on its way before the length is known.
-template <class TAB, class T, bool VEC, int HOLD, bool ONE>
-__global__ __launch_bounds__(1024) void paged_append_kernel(TAB tab, PagedView c, PagedRows w, AppendCut cut) {
+// SHARE: the workgroup (of 256 threads at most) takes several heads' keys, the next one's on their way.
+template <class TAB, class T, bool VEC, int HOLD, bool ONE, bool SHARE>
+__global__ __launch_bounds__(SHARE ? 256 : 1024) void paged_append_kernel(TAB tab, PagedView c, PagedRows w, AppendCut cut) {
   short_kernel_priority();
   const int upr = c.d / kUnit, lane = threadIdx.x & 63;
   if ((int)blockIdx.x >= cut.pages) {   // queries: the angles of a token's unit serve several heads
@@ -71,33 +75,38 @@ __global__ __launch_bounds__(1024) void paged_append_kernel(TAB tab, PagedView c
     const Spin spin = spin_unit(w.rotary, u, pos);
     const T* from = (const T*)w.q + r * w.qst;
     T* to = (T*)w.q_out + (int64_t)r * w.H * c.d;
-    for (int h = h0; h < min(w.H, h0 + cut.heads); ++h) {
-      Unit x = load_unit<T, VEC>(from + h * w.qsh, u, w.rotary);
-      turn(x, spin, u, w.rotary);
-      store_unit<T, VEC>(to + (int64_t)h * c.d, u, w.rotary, x);
-    }
+    if (cut.once) turn_heads<T, VEC, true, 4>(from, w.qsh, to, (int64_t)c.d, h0, min(w.H, h0 + cut.heads), u, w.rotary, spin);
+    else turn_heads<T, VEC, false, 4>(from, w.qsh, to, (int64_t)c.d, h0, min(w.H, h0 + cut.heads), u, w.rotary, spin);
     return;
   }
-  __shared__ float tops[16];
+  __shared__ float tops[2][16];
+  const int key_groups = (c.G + cut.keys - 1) / cut.keys;
   int i = (int)blockIdx.x;
-  const int which = i % (2 * c.G);
-  i /= 2 * c.G;
-  const int k = ONE ? 0 : i % cut.touched, b = ONE ? i : i / cut.touched, g = which >> 1;
-  const bool values = which & 1;
+  const int which = i % (key_groups + c.G);
+  i /= key_groups + c.G;
+  const int k = ONE ? 0 : i % cut.touched, b = ONE ? i : i / cut.touched;
+  const bool values = which >= key_groups;
+  const int g0 = values ? which - key_groups : which * cut.keys, g1 = SHARE && !values ? min(c.G, g0 + cut.keys) : g0 + 1;
   const int fresh = tab.cu_new[b + 1] - tab.cu_new[b];
   RotaryView r = w.rotary;
   if (values) { r.half = 0; r.interleaved = 1; }
-  const T* src = (const T*)(values ? w.v : w.k) + g * w.sh + (int64_t)tab.cu_new[b] * w.st;
+  const T* src = (const T*)(values ? w.v : w.k) + (int64_t)tab.cu_new[b] * w.st;
+  int row[HOLD], unit[HOLD];
+#pragma unroll
+  for (int m = 0; m < HOLD; ++m) {
+    const int e = (int)(threadIdx.x + m * blockDim.x);
+    row[m] = (int)(((uint32_t)e * cut.upr_recip) >> 20);
+    unit[m] = e - row[m] * upr;
+  }
   Unit x[HOLD];
-  auto load = [&](int r0, int rows) __attribute__((always_inline)) {
+  auto load = [&](int g, int r0, int rows) __attribute__((always_inline)) {
 #pragma unroll
     for (int m = 0; m < HOLD; ++m) {
-      const int e = (int)(threadIdx.x + m * blockDim.x), row = (int)(((uint32_t)e * cut.upr_recip) >> 20), u = e - row * upr;
       x[m] = Unit{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-      if (row < rows) x[m] = load_unit<T, VEC>(src + (int64_t)(r0 + row) * w.st, u, r);
+      if (row[m] < rows) x[m] = load_unit<T, VEC>(src + g * w.sh + (int64_t)(r0 + row[m]) * w.st, unit[m], r);
     }
   };
-  if (ONE) load(0, fresh);
+  if (ONE) load(g0, 0, fresh);
   const int n = paged_len(c, b);
   const int first = n >> c.shift, last = (int)(((int64_t)n + fresh - 1) >> c.shift);
   // whether the rows fit, and all their pages are there: every workgroup of the sequence sees the same
@@ -120,49 +129,65 @@ __global__ __launch_bounds__(1024) void paged_append_kernel(TAB tab, PagedView c
   if (!fits || fresh == 0 || j > last) return;
   const int page0 = j << c.shift, ps = 1 << c.shift;
   const int old = max(0, n - page0), r0 = page0 + old - n, rows = min(page0 + ps, n + fresh) - max(page0, n);   // fresh rows r0 .. r0 + rows - 1
-  uint8_t* dst = (values ? c.v : c.k) + page * c.sp + g * c.sh;
-  float* scale = (values ? c.v_scale : c.k_scale) + (int64_t)page * c.G + g;
-  if (!ONE) load(r0, rows);
-  const float before = old > 0 ? *scale : 0.f;
-  float top = 0.f;
+  if (!ONE) load(g0, r0, rows);
+  auto spin_of = [&](int m) __attribute__((always_inline)) { return spin_unit(r, unit[m], w.pos ? w.pos[tab.cu_new[b] + r0 + row[m]] : n + r0 + row[m]); };
+  Spin spin[SHARE ? HOLD : 1];
+  if (SHARE && r.half) {
 #pragma unroll
-  for (int m = 0; m < HOLD; ++m) {
-    const int e = (int)(threadIdx.x + m * blockDim.x), row = (int)(((uint32_t)e * cut.upr_recip) >> 20), u = e - row * upr;
-    if (r.half && row < rows) turn(x[m], spin_unit(r, u, w.pos ? w.pos[tab.cu_new[b] + r0 + row] : n + r0 + row), u, r);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      top = storable(x[m].a[q]) ? fmaxf(top, fabsf(x[m].a[q])) : top;
-      top = storable(x[m].b[q]) ? fmaxf(top, fabsf(x[m].b[q])) : top;
-    }
+    for (int m = 0; m < HOLD; ++m)
+      if (row[m] < rows) spin[m] = spin_of(m);
   }
-  for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-  if (blockDim.x > 64) {
-    if (lane == 0) tops[threadIdx.x >> 6] = top;
-    __syncthreads();
-    for (int m = 0; m < (int)blockDim.x >> 6; ++m) top = fmaxf(top, tops[m]);
-  }
-  const float come = scale_for(top), now = fmaxf(come, before), inv = inverse(now);
-  if (old > 0 && now > before) {   // the earlier rows' codes in the new scale
-    const float ratio = before * inv;
-    for (int e = threadIdx.x; e < old * (c.d / 4); e += blockDim.x) {
-      const int row = e / (c.d / 4);
-      uint32_t* at = reinterpret_cast<uint32_t*>(dst + row * c.st + (e - row * (c.d / 4)) * 4);
-      typedef __attribute__((ext_vector_type(2))) float floatx2;
-      const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(*at, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(*at, true);
-      *at = four_codes(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
-    }
-  }
-  if (threadIdx.x == 0) *scale = now;   // (every thread has read it: the largest of all has been exchanged)
+  for (int g = g0; g < g1; ++g) {
+    uint8_t* dst = (values ? c.v : c.k) + page * c.sp + g * c.sh;
+    float* scale = (values ? c.v_scale : c.k_scale) + (int64_t)page * c.G + g;
+    const float before = old > 0 ? *scale : 0.f;
+    float top = 0.f;
 #pragma unroll
-  for (int m = 0; m < HOLD; ++m) {
-    const int e = (int)(threadIdx.x + m * blockDim.x), row = (int)(((uint32_t)e * cut.upr_recip) >> 20), u = e - row * upr;
-    if (row >= rows) continue;
+    for (int m = 0; m < HOLD; ++m) {
+      if (r.half && row[m] < rows) turn(x[m], SHARE ? spin[SHARE ? m : 0] : spin_of(m), unit[m], r);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      x[m].a[q] = storable(x[m].a[q]) ? x[m].a[q] * inv : NAN;
-      x[m].b[q] = storable(x[m].b[q]) ? x[m].b[q] * inv : NAN;
+      for (int q = 0; q < 4; ++q) {
+        top = storable(x[m].a[q]) ? fmaxf(top, fabsf(x[m].a[q])) : top;
+        top = storable(x[m].b[q]) ? fmaxf(top, fabsf(x[m].b[q])) : top;
+      }
     }
-    store_codes<VEC>(dst + (old + row) * c.st, u, r, x[m]);
+    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if (blockDim.x > 64) {   // (two places in turns: a wave is at most one barrier ahead)
+      float* place = tops[(g - g0) & 1];
+      if (lane == 0) place[threadIdx.x >> 6] = top;
+      __syncthreads();
+      for (int m = 0; m < (int)blockDim.x >> 6; ++m) top = fmaxf(top, place[m]);
+    }
+    const float come = scale_for(top), now = fmaxf(come, before), inv = inverse(now);
+    if (old > 0 && now > before) {   // the earlier rows' codes in the new scale
+      const float ratio = before * inv;
+      for (int e = threadIdx.x; e < old * (c.d / 4); e += blockDim.x) {
+        const int at_row = e / (c.d / 4);
+        uint32_t* at = reinterpret_cast<uint32_t*>(dst + at_row * c.st + (e - at_row * (c.d / 4)) * 4);
+        typedef __attribute__((ext_vector_type(2))) float floatx2;
+        const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(*at, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(*at, true);
+        *at = four_codes(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
+      }
+    }
+    if (threadIdx.x == 0) *scale = now;   // (every thread has read it: the largest of all has been exchanged)
+    Unit coded[SHARE ? HOLD : 1];
+    auto code = [&](int m, Unit& to) __attribute__((always_inline)) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        to.a[q] = storable(x[m].a[q]) ? x[m].a[q] * inv : NAN;
+        to.b[q] = storable(x[m].b[q]) ? x[m].b[q] * inv : NAN;
+      }
+    };
+    if constexpr (SHARE) {   // (the next head's rows come while these are stored)
+#pragma unroll
+      for (int m = 0; m < HOLD; ++m) code(m, coded[m]);
+      if (g + 1 < g1) load(g + 1, r0, rows);
+    }
+#pragma unroll
+    for (int m = 0; m < HOLD; ++m) {
+      if (!SHARE) code(m, coded[0]);
+      if (row[m] < rows) store_codes<VEC>(dst + (old + row[m]) * c.st, unit[m], r, coded[SHARE ? m : 0]);
+    }
   }
 }
 
@@ -178,28 +203,35 @@ hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const Pa
   const int ps = 1 << c.shift;
   AppendCut cut;
   cut.touched = (int)(most > 0 ? (most + ps - 2) / ps + 1 : 1);
-  cut.pages = t.batch * cut.touched * 2 * c.G;
-  cut.upr_recip = (uint32_t)(((1u << 20) + upr - 1) / upr);
   // threads: four units each, from a wave to sixteen
   const int units = (int)std::min<int64_t>(std::max<int64_t>(1, most), ps) * upr;
   int threads = 64;
   while (threads < 1024 && threads * 4 < units) threads *= 2;
+  // (one head a workgroup where there are few, or units fill its registers)
+  cut.keys = 1;
+  while (w.rotary.half && most > 1 && threads <= 256 && cut.keys < 4 && 2 * cut.keys <= c.G && (int64_t)t.batch * cut.touched * (c.G / (2 * cut.keys)) >= 512) cut.keys *= 2;
+  cut.pages = t.batch * cut.touched * ((int)ceil_div(c.G, cut.keys) + c.G);
+  cut.upr_recip = (uint32_t)(((1u << 20) + upr - 1) / upr);
   // query heads of a thread: as many as leave the chip filled
   const int64_t tokens = w.q ? t.cu_new[t.batch] : 0;
   cut.heads = w.q ? (int)std::min<int64_t>(w.H, std::max<int64_t>(1, tokens * upr * w.H / (1 << 18))) : 1;
   cut.groups = w.q ? (int)ceil_div(w.H, cut.heads) : 1;
+  cut.once = 2 * tokens * w.H * c.d * e >= kOnceBytes;
   cut.units = (uint32_t)(tokens * cut.groups * upr);
   const int64_t blocks = cut.pages + ceil_div((int64_t)cut.units, threads);
   with_fresh_table(t, [&](const auto& tab) {
     using TAB = std::decay_t<decltype(tab)>;
-    auto go = [&](auto elem, auto v, auto hold, auto one) {
-      paged_append_kernel<TAB, decltype(elem), decltype(v)::value, decltype(hold)::value, decltype(one)::value>
+    auto go = [&](auto elem, auto v, auto hold, auto one, auto share) {
+      paged_append_kernel<TAB, decltype(elem), decltype(v)::value, decltype(hold)::value, decltype(one)::value, decltype(share)::value>
           <<<(unsigned)blocks, threads, 0, st>>>(tab, c, w, cut);
     };
     auto by_size = [&](auto elem, auto v) {
-      if (most <= 1) go(elem, v, std::integral_constant<int, 1>{}, std::true_type{});
-      else if (units <= 4 * threads) go(elem, v, std::integral_constant<int, 4>{}, std::false_type{});
-      else go(elem, v, std::integral_constant<int, 8>{}, std::false_type{});
+      const std::integral_constant<int, 1> h1; const std::integral_constant<int, 4> h4; const std::integral_constant<int, 8> h8;
+      const std::true_type yes; const std::false_type no;
+      if (most <= 1) go(elem, v, h1, yes, no);
+      else if (cut.keys > 1) go(elem, v, h4, no, yes);
+      else if (units <= 4 * threads) go(elem, v, h4, no, no);
+      else go(elem, v, h8, no, no);
     };
     if (bf16) vec ? by_size(uint16_t{}, std::true_type{}) : by_size(uint16_t{}, std::false_type{});
     else vec ? by_size(float{}, std::true_type{}) : by_size(float{}, std::false_type{});
