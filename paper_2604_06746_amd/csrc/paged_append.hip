@@ -98,6 +98,15 @@ __global__ __launch_bounds__(SHARE ? 256 : 1024) void paged_append_kernel(TAB ta
     row[m] = (int)(((uint32_t)e * cut.upr_recip) >> 20);
     unit[m] = e - row[m] * upr;
   }
+  auto exchanged = [&](float top, float* place) __attribute__((always_inline)) {   // the largest of all threads'
+    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if (blockDim.x > 64) {
+      if (lane == 0) place[threadIdx.x >> 6] = top;
+      __syncthreads();
+      for (int m = 0; m < (int)blockDim.x >> 6; ++m) top = fmaxf(top, place[m]);
+    }
+    return top;
+  };
   Unit x[HOLD];
   auto load = [&](int g, int r0, int rows) __attribute__((always_inline)) {
 #pragma unroll
@@ -146,17 +155,24 @@ __global__ __launch_bounds__(SHARE ? 256 : 1024) void paged_append_kernel(TAB ta
     for (int m = 0; m < HOLD; ++m) {
       if (r.half && row[m] < rows) turn(x[m], SHARE ? spin[SHARE ? m : 0] : spin_of(m), unit[m], r);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        top = storable(x[m].a[q]) ? fmaxf(top, fabsf(x[m].a[q])) : top;
-        top = storable(x[m].b[q]) ? fmaxf(top, fabsf(x[m].b[q])) : top;
-      }
+      for (int q = 0; q < 4; ++q) top = fmaxf(top, fmaxf(fabsf(x[m].a[q]), fabsf(x[m].b[q])));   // (NaN does not count)
     }
-    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if (blockDim.x > 64) {   // (two places in turns: a wave is at most one barrier ahead)
-      float* place = tops[(g - g0) & 1];
-      if (lane == 0) place[threadIdx.x >> 6] = top;
+    top = exchanged(top, tops[(g - g0) & 1]);   // (two places in turns: a wave is at most one barrier ahead)
+    // What cannot be stored is rare: the conversion makes NaN of NaN, and larger values are looked for only where there are some.
+    const bool odd = !(top <= kTopCode * kMostScale);
+    if (odd) {
+      top = 0.f;
+#pragma unroll
+      for (int m = 0; m < HOLD; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          x[m].a[q] = storable(x[m].a[q]) ? x[m].a[q] : NAN;
+          x[m].b[q] = storable(x[m].b[q]) ? x[m].b[q] : NAN;
+          top = fmaxf(top, fmaxf(fabsf(x[m].a[q]), fabsf(x[m].b[q])));
+        }
       __syncthreads();
-      for (int m = 0; m < (int)blockDim.x >> 6; ++m) top = fmaxf(top, place[m]);
+      top = exchanged(top, tops[(g - g0) & 1]);
+      __syncthreads();
     }
     const float come = scale_for(top), now = fmaxf(come, before), inv = inverse(now);
     if (old > 0 && now > before) {   // the earlier rows' codes in the new scale
@@ -174,8 +190,8 @@ __global__ __launch_bounds__(SHARE ? 256 : 1024) void paged_append_kernel(TAB ta
     auto code = [&](int m, Unit& to) __attribute__((always_inline)) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        to.a[q] = storable(x[m].a[q]) ? x[m].a[q] * inv : NAN;
-        to.b[q] = storable(x[m].b[q]) ? x[m].b[q] * inv : NAN;
+        to.a[q] = x[m].a[q] * inv;
+        to.b[q] = x[m].b[q] * inv;
       }
     };
     if constexpr (SHARE) {   // (the next head's rows come while these are stored)
@@ -209,7 +225,7 @@ hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const Pa
   while (threads < 1024 && threads * 4 < units) threads *= 2;
   // (one head a workgroup where there are few, or units fill its registers)
   cut.keys = 1;
-  while (w.rotary.half && most > 1 && threads <= 256 && cut.keys < 4 && 2 * cut.keys <= c.G && (int64_t)t.batch * cut.touched * (c.G / (2 * cut.keys)) >= 512) cut.keys *= 2;
+  while (w.rotary.half && most > 1 && threads <= 256 && cut.keys < 8 && 2 * cut.keys <= c.G && (int64_t)t.batch * cut.touched * (c.G / (2 * cut.keys)) >= 512) cut.keys *= 2;
   cut.pages = t.batch * cut.touched * ((int)ceil_div(c.G, cut.keys) + c.G);
   cut.upr_recip = (uint32_t)(((1u << 20) + upr - 1) / upr);
   // query heads of a thread: as many as leave the chip filled

@@ -540,3 +540,40 @@ def test_pool_beyond_2_31(B):
     B.structkv_paged_append(handle, new.cuda(), new.cuda(), [0, 2], lens_out)
     s = ks[far[3]].cpu().double()
     assert torch.equal(R.decode(k[far[3], :, 8:10].cpu()), R.decode(R.encode(new.double() / s[:, None, None])))
+
+
+@pytest.mark.parametrize("page_size,d,G,tokens,interleaved", [(64, 128, 8, 4200, False), (16, 64, 6, 1100, True), (256, 256, 2, 700, False), (128, 80, 3, 500, False)])
+def test_append_large_batches_like_single_sequences(B, page_size, d, G, tokens, interleaved):
+    """Calls that fill the chip, whose workgroups take several heads' keys, against one for each sequence, bit for bit: pages begun and
+    ended anywhere, scales that grow, rows that cannot be stored, queries of large calls."""
+    batch, H = 8, 2 * G
+    lens = [0, 5, 63, 64, 130, 1, 200, 17]
+    per = -(-(tokens + 200) // page_size)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    total = batch * tokens
+    k, v, q = normal(total, G, d).transpose(0, 1), normal(total, G, d).transpose(0, 1), normal(total, H, d)
+    k[:, ::37] *= 300
+    v[:, ::41] /= 1000
+    k[1, 100, 3], k[0, tokens + 7, 0], v[1, 50, 9], v[0, 3 * tokens, 1] = math.nan, math.inf, 3e38, -math.inf
+    n = batch * per
+    codes = torch.randint(0, 126, (n, G, page_size, d), generator=g, device="cuda").to(torch.uint8)
+    pages = torch.randperm(n, generator=g, device="cuda").int().view(batch, per)
+    plan = rotary(B, d, ("bands", 8.0, 8192.0, 1.0, 4.0), interleaved)[0]
+    res = []
+    for single in (False, True):
+        kc, vc, ks, vs = codes.clone(), codes.clone(), torch.full((n, G), 2.0 ** -7, device="cuda"), torch.full((n, G), 2.0 ** -9, device="cuda")
+        lens_gpu, lens_out, missed = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lens, [-1] * batch, [0] * batch))
+        q_out = torch.empty_like(q)
+        if single:
+            for b in range(batch):
+                s = slice(b * tokens, (b + 1) * tokens)
+                one = B.make_paged(kc, vc, ks, vs, pages[b:b + 1], lens_gpu[b:b + 1], missed=missed[b:b + 1])
+                B.structkv_paged_append(one, k[:, s], v[:, s], [0, tokens], lens_out[b:b + 1], plan, q=q[s], q_out=q_out[s])
+        else:
+            every = B.make_paged(kc, vc, ks, vs, pages, lens_gpu, missed=missed)
+            B.structkv_paged_append(every, k, v, cut([tokens] * batch), lens_out, plan, q=q, q_out=q_out)
+        res.append((kc, vc, ks, vs, q_out, lens_out, missed))
+    assert res[0][5].tolist() == [x + tokens for x in lens] and res[0][6].tolist() == [0] * batch
+    for x, y in zip(*res):
+        assert torch.equal(x.view(torch.int16) if x.dtype == torch.bfloat16 else x, y.view(torch.int16) if y.dtype == torch.bfloat16 else y)

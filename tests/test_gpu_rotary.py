@@ -210,3 +210,25 @@ def test_refusals(B):
         assert e.value.status == B.STRUCTKV_ERR_INVALID_ARG
     B.structkv_rotate(plan, x[:0], pos[:0], x[:0])
     B.structkv_rotate(plan, x[:, :0], pos, x[:, :0])
+
+
+@pytest.mark.parametrize("tokens,heads,d,dtype,interleaved", [(40000, 32, 128, torch.bfloat16, False), (40000, 32, 128, torch.bfloat16, True),
+                                                              (150000, 8, 128, torch.bfloat16, False), (20000, 20, 128, torch.float32, False),
+                                                              (30001, 19, 80, torch.bfloat16, False)])
+def test_large_calls_like_small_ones(B, tokens, heads, d, dtype, interleaved):
+    """Calls past the caches, of many heads a thread, against calls of 1000 tokens, bit for bit."""
+    turns, _ = B.structkv_rotary_turns(d, 500000.0)
+    plan = B.make_rotary(turns.cuda(), interleaved=interleaved)
+    x = torch.randn(tokens, heads, d, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
+    pos = torch.arange(tokens, dtype=torch.int32, device="cuda") * 3
+    large, small = torch.empty_like(x), torch.empty_like(x)
+    B.structkv_rotate(plan, x, pos, large)
+    for i in range(0, tokens, 1000):
+        s = slice(i, min(tokens, i + 1000))
+        B.structkv_rotate(plan, x[s], pos[s], small[s])
+    assert torch.equal(large, small)
+    if heads == 8:     # the same by head
+        by_head = x.transpose(0, 1).contiguous().transpose(0, 1)
+        out = torch.empty_like(by_head)
+        B.structkv_rotate(plan, by_head, pos, out)
+        assert torch.equal(out, large)
