@@ -52,9 +52,14 @@ struct PagedRows {
 };
 hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const PagedRows& w, bool bf16, hipStream_t st);
 
+// Waves of a workgroup that takes a whole short sequence's slots, so that nothing has to be joined.
+constexpr int kShortWaves = 8;
 // An attend call is cut like one on a cache of slots (AttendPlan, AttendWork): x in AttendWork are here the weights of blocks of kBlock slots
 // in the log2 domain, head h, block i of sequence b at h xs + b blocks + i.
-hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const AttendPlan& p,
+struct PagedPlan : AttendPlan {
+  int waves;   // of a workgroup: kAttendWaves, or kShortWaves (16 rows, nothing to join)
+};
+hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const PagedPlan& p,
                                const AttendWork& w, bool bf16, hipStream_t st);
 // a plan that gathers the weights: the chunks joined, and mass <- lambda mass + what the heads' blocks hold
 hipError_t launch_paged_join(const CacheTable& t, const PagedView& c, const AttendWork& w, bool bf16, hipStream_t st);

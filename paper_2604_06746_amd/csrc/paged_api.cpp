@@ -105,9 +105,13 @@ constexpr int64_t kUnits = 512, kLeast = 128;
 // Mean slots of a block of rows from which on it is cut in two even where the blocks fill the chip.
 constexpr int64_t kCut = 4096;
 
+// Capacity up to which a workgroup of kShortWaves takes all slots of a sequence where there would be chunks to join: a token over 256 slots 9.3 ->
+// 6.5 us, over 512 9.3 -> 8.5, over 1031 9.7 -> 11.5.
+constexpr int64_t kWhole = 512;
+
 int64_t block_slots(const PagedView& v) { return ((int64_t)v.max_pages << v.shift) / kBlock; }
 
-structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, CacheTable* t, AttendPlan* p) {
+structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, CacheTable* t, PagedPlan* p) {
   const int64_t G = v.G, gs = H / v.G, cap = (int64_t)v.max_pages << v.shift;
   memset(p, 0, sizeof(*p));
   p->mfma = 1;
@@ -126,7 +130,9 @@ structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, Ca
     t->units[b + 1] = (int32_t)blocks;
   }
   const bool cut = p->rows == 16 && cap >= kCut;
-  p->units = std::max(blocks, std::min(chunks, std::max(kUnits / G, cut ? 2 * blocks : 0)));
+  const bool whole = !gather && p->rows == 16 && cap <= kWhole && blocks < std::min(chunks, kUnits / G);
+  p->waves = whole ? kShortWaves : kAttendWaves;
+  p->units = whole ? blocks : std::max(blocks, std::min(chunks, std::max(kUnits / G, cut ? 2 * blocks : 0)));
   const int64_t gathers = gather ? v.batch * ceil_div(block_slots(v), 64) + (int64_t)t->cu_new[v.batch] * H : 0;
   if (p->units * G >= ((int64_t)1 << 31) || gathers >= ((int64_t)1 << 31)) return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
   p->join = gather || p->units > blocks;
@@ -311,7 +317,7 @@ structkv_status structkv_paged_attend(const structkv_paged* cache, int32_t n_q_h
   if (lambda > 0.f)
     for (int b = 0; b < cache->batch; ++b)
       if (t.cu_new[b + 1] - t.cu_new[b] > 1) return fail(STRUCTKV_ERR_INVALID_ARG, "sequence %d: lambda > 0 is for single tokens", b);
-  AttendPlan p;
+  PagedPlan p;
   st = plan_paged(v, n_q_heads, lambda > 0.f, cache->dtype == STRUCTKV_DTYPE_BF16, &t, &p);
   if (st != STRUCTKV_OK) return st;
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(STRUCTKV_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");

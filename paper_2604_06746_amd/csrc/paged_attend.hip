@@ -97,14 +97,14 @@ __device__ __forceinline__ void load_query(bf16x8 (&q)[QP], const T* row, int c,
 
 // What the waves of a workgroup leave, added up in their order through LDS and written out by all threads (leave), 16 rows at a time.  A lane
 // holds components 4 W q4 + W e + j of its rows in O[j][rb][e].
-template <int DP>
-constexpr int kFinishBlocks = kAttendWaves * 16 * (DP + 4 + 2);
-template <class T, int DP, int RB>
+template <int DP, int WAVES>
+constexpr int kFinishBlocks = WAVES * 16 * (DP + 4 + 2);
+template <class T, int DP, int RB, int WAVES>
 __device__ __forceinline__ void finish_blocks(const floatx4 (&O)[DP / 16][RB], const float (&M)[RB], const float (&Zl)[RB], float* buf,
                                               const AttendWork& w, int d, int g, int row0, int rows, int new0, int nc) {
   constexpr int PITCH = DP + 4, W = DP / 16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q4 = lane >> 4;
-  float* ml = buf + kAttendWaves * 16 * PITCH;   // [wave][row][2]
+  float* ml = buf + WAVES * 16 * PITCH;   // [wave][row][2]
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     if (row0 + rb * 16 >= rows) break;
@@ -116,7 +116,7 @@ __device__ __forceinline__ void finish_blocks(const floatx4 (&O)[DP / 16][RB], c
     }
     __syncthreads();
     float top = ml[l16 * 2];
-    for (int i = 1; i < kAttendWaves; ++i) top = fmaxf(top, ml[(i * 16 + l16) * 2]);
+    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, ml[(i * 16 + l16) * 2]);
     const float f = __builtin_amdgcn_exp2f(M[rb] - top);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -125,14 +125,14 @@ __device__ __forceinline__ void finish_blocks(const floatx4 (&O)[DP / 16][RB], c
         *reinterpret_cast<floatx4*>(buf + (wave * 16 + l16) * PITCH + W * (4 * q4 + e) + j) =
             floatx4{O[j][rb][e], O[j + 1][rb][e], O[j + 2][rb][e], O[j + 3][rb][e]} * f;
     __syncthreads();
-    for (int e = threadIdx.x; e < 16 * (DP / 4); e += 64 * kAttendWaves) {
+    for (int e = threadIdx.x; e < 16 * (DP / 4); e += 64 * WAVES) {
       const int row = e / (DP / 4), c = e % (DP / 4) * 4;
       if (row0 + rb * 16 + row >= rows || c >= d) continue;
       float best = ml[row * 2];
-      for (int i = 1; i < kAttendWaves; ++i) best = fmaxf(best, ml[(i * 16 + row) * 2]);
+      for (int i = 1; i < WAVES; ++i) best = fmaxf(best, ml[(i * 16 + row) * 2]);
       float sum = 0.f;
       floatx4 o = {0.f, 0.f, 0.f, 0.f};
-      for (int i = 0; i < kAttendWaves; ++i) {
+      for (int i = 0; i < WAVES; ++i) {
         sum += ml[(i * 16 + row) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(i * 16 + row) * 2] - best);
         o += *reinterpret_cast<const floatx4*>(buf + (i * 16 + row) * PITCH + c);
       }
@@ -151,14 +151,14 @@ struct Pair {
   bool any, two;
 };
 
-template <class TAB, class T, int DP, int RB, bool CAPPED, bool SAVE, bool ONCE>
-__global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void paged_attend_kernel(TAB tab, CacheView view, PagedView c, ScoreForm f, AttendWork w, bool aligned) {
+template <class TAB, class T, int DP, int RB, bool CAPPED, bool SAVE, bool ONCE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, RB * DP > 256 || WAVES > 8 ? 1 : 2) void paged_attend_kernel(TAB tab, CacheView view, PagedView c, ScoreForm f, AttendWork w, bool aligned) {
   constexpr bool F32 = std::is_same<T, float>::value;
   constexpr int QP = F32 ? 3 : 1, PP = F32 ? 2 : 1, KP = DP / 64, W = DP / 16;
   constexpr bool AHEAD = DP <= 128 && (RB == 1 || !F32);   // (the others have no registers for it)
   constexpr int kBatch = 64, kPitch = kBatch + 1;
-  static_assert(!SAVE || kAttendWaves * 16 * kPitch <= kAttendWaves * 16 * (DP + 4), "the blocks' weights lie where the waves' sums come later");
-  __shared__ __attribute__((aligned(16))) float buf[kFinishBlocks<DP>];
+  static_assert(!SAVE || kPitch <= DP + 4, "the blocks' weights lie where the waves' sums come later");
+  __shared__ __attribute__((aligned(16))) float buf[kFinishBlocks<DP, WAVES>];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const AttendPlace p = attend_place(tab, view, w);
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
   int odd = 0x7FFFFFFF;   // the first fresh slot behind the first one whose values are not all numbers
 
   const int lb = c.shift - 4, first = p.s0 / kBlock, last = end > p.s0 ? (end + kBlock - 1) / kBlock : first;
-  const int share = ((last - first + 2 * kAttendWaves - 1) / (2 * kAttendWaves)) * 2;
+  const int share = ((last - first + 2 * WAVES - 1) / (2 * WAVES)) * 2;
   const int mine0 = first + wave * share, mine1 = min(last, mine0 + share);
   // A lane's block of the batch that is being fetched: place and scales
   float ks = 1.f, vs = 1.f, kf = 0.f, lv = 0.f, iv = 0.f;
@@ -424,33 +424,37 @@ __global__ __launch_bounds__(64 * kAttendWaves, RB * DP > 256 ? 1 : 2) void page
 #pragma unroll
       for (int j = 0; j < W; ++j) O[j][rb] *= limit[rb] > odd ? NAN : 1.f;
   }
-  finish_blocks<T, DP, RB>(O, M, Z, buf, w, c.d, p.g, row0, rows, new0, p.nc);
+  finish_blocks<T, DP, RB, WAVES>(O, M, Z, buf, w, c.d, p.g, row0, rows, new0, p.nc);
 }
 
 template <class T, int DP>
-hipError_t attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const AttendPlan& p, const AttendWork& w, hipStream_t st) {
+hipError_t attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const PagedPlan& p, const AttendWork& w, hipStream_t st) {
   const bool aligned = (((uintptr_t)w.q | (uintptr_t)((w.qst | w.qsh) * (int64_t)sizeof(T))) & 15) == 0;
   with_cache_table(t, [&](const auto& tab) {
     using TAB = std::decay_t<decltype(tab)>;
-    const dim3 grid((unsigned)(p.units * c.G)), block(64 * kAttendWaves);
-    auto go = [&](auto rb, auto save) {
-      constexpr int RB = decltype(rb)::value;
+    auto go = [&](auto rb, auto save, auto waves) {
+      constexpr int RB = decltype(rb)::value, WAVES = decltype(waves)::value;
       constexpr bool SAVE = decltype(save)::value;
       auto form = [&](auto capped, auto once) {
-        paged_attend_kernel<TAB, T, DP, RB, decltype(capped)::value, SAVE, decltype(once)::value><<<grid, block, 0, st>>>(tab, v, c, f, w, aligned);
+        paged_attend_kernel<TAB, T, DP, RB, decltype(capped)::value, SAVE, decltype(once)::value, WAVES>
+            <<<(unsigned)(p.units * c.G), 64 * WAVES, 0, st>>>(tab, v, c, f, w, aligned);
       };
       auto by_cap = [&](auto once) { f.softcap > 0.f ? form(std::true_type{}, once) : form(std::false_type{}, once); };
       p.stream ? by_cap(std::true_type{}) : by_cap(std::false_type{});
     };
-    if (w.x) go(std::integral_constant<int, 1>{}, std::true_type{});
-    else if (p.rows == 16) go(std::integral_constant<int, 1>{}, std::false_type{});
-    else if constexpr (DP <= 128 || sizeof(T) == 2) go(std::integral_constant<int, 2>{}, std::false_type{});
+    const std::integral_constant<int, kAttendWaves> four;
+    const std::integral_constant<int, kShortWaves> more;
+    const std::integral_constant<int, 1> one;
+    if (w.x) go(one, std::true_type{}, four);
+    else if (p.rows == 16 && p.waves == kAttendWaves) go(one, std::false_type{}, four);
+    else if (p.rows == 16) go(one, std::false_type{}, more);
+    else if constexpr (DP <= 128 || sizeof(T) == 2) go(std::integral_constant<int, 2>{}, std::false_type{}, four);
   });
   return hipGetLastError();
 }
 
 template <class T>
-hipError_t by_dim(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const AttendPlan& p, const AttendWork& w, hipStream_t st) {
+hipError_t by_dim(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const PagedPlan& p, const AttendWork& w, hipStream_t st) {
   if (c.d <= 64) return attend<T, 64>(t, v, c, f, p, w, st);
   if (c.d <= 128) return attend<T, 128>(t, v, c, f, p, w, st);
   return attend<T, 256>(t, v, c, f, p, w, st);
@@ -458,7 +462,7 @@ hipError_t by_dim(const CacheTable& t, const CacheView& v, const PagedView& c, c
 
 }  // namespace
 
-hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const AttendPlan& p,
+hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const PagedPlan& p,
                                const AttendWork& w, bool bf16, hipStream_t st) {
   return bf16 ? by_dim<uint16_t>(t, v, c, f, p, w, st) : by_dim<float>(t, v, c, f, p, w, st);
 }

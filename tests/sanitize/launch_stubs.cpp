@@ -381,13 +381,13 @@ hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const Pa
   ++g_launches;
   return t.batch == c.batch && w.lens_out && w.rotary.d == c.d && (!w.q || w.rotary.half > 0) ? hipSuccess : hipErrorInvalidValue;
 }
-hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm&, const AttendPlan& p,
+hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm&, const PagedPlan& p,
                                const AttendWork& w, bool, hipStream_t) {
   const int dp = c.d <= 64 ? 64 : c.d <= 128 ? 128 : 256;
   const size_t parts = p.join ? (size_t)(p.units * c.G * p.rows) : 0;
   const bool ok = v.G == c.G && v.slots == t.cu[t.batch] && p.off_x - p.off_o >= parts * dp * 4 && (p.gather != 0) == (w.x != nullptr) && (!p.gather || p.rows == 16) &&
                   (!p.gather || p.total_bytes - p.off_x >= (size_t)w.H * (size_t)w.xs * 4);
-  return attend_fits(t, p, w, c.G) && ok ? hipSuccess : hipErrorInvalidValue;
+  return attend_fits(t, p, w, c.G) && ok && (p.waves == kAttendWaves || (p.waves == kShortWaves && p.rows == 16 && !p.join)) ? hipSuccess : hipErrorInvalidValue;
 }
 hipError_t launch_paged_join(const CacheTable&, const PagedView& c, const AttendWork& w, bool, hipStream_t) {
   ++g_launches;
