@@ -541,8 +541,8 @@ structkv_status structkv_paged_append(const structkv_paged* cache, const void* k
  * NaN gets NaN: throughout where it is a key's, or a value's in a fresh slot behind the first, in that component for other values.
  * lambda in (0, 1] (only with T_b <= 1 everywhere): the weights are gathered, for table entries j < ceil(lens[b] / page_size) of sequences with T_b = 1
  *   mass[b][j] = lambda * mass[b][j] + sum over the page's slots and all query heads of a_s     (0 for a dropped page)
- * lambda = 0: mass stays as it is.
- * q: element (r, h, c) at r*q_stride_tok + h*q_stride_head + c; out [new][H_q][d] contiguous; lse_out [new][H_q] fp32.
+ * lambda = 0: mass stays as it is.  A row whose norm is NaN makes the mass of the pages that it sees NaN.
+ * q: element (r, h, c) at r*q_stride_tok + h*q_stride_head + c; out [new][H_q][d] contiguous, and not overlapping q; lse_out [new][H_q] fp32.
  * scale, softcap: as in structkv_cache_attend.  A sequence with lens[b] < T_b or missed[b] != 0 is one whose rows see nothing, and
  * whose mass stays as it is.  Deterministic: the same call on the same lengths and table gives the same bits.
  */

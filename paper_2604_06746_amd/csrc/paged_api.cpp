@@ -231,7 +231,8 @@ structkv_status structkv_rotate(const structkv_rotary* rotary, const void* x, in
   if (!lie_apart(head_dim, tokens, out_stride_tok, n_heads, out_stride_head, 1, 0)) return fail(STRUCTKV_ERR_INVALID_ARG, "rows of out overlap");
   if (x == out && ((x_stride_tok != out_stride_tok && tokens > 1) || (x_stride_head != out_stride_head && n_heads > 1)))
     return fail(STRUCTKV_ERR_INVALID_ARG, "out is x, but its strides are others");
-  if (ceil_div(tokens * ceil_div(head_dim, kUnit), 256) >= ((int64_t)1 << 31) || tokens >= ((int64_t)1 << 40) || n_heads > 65535)
+  // (units of four components at least)
+  if (tokens >= ((int64_t)1 << 40) || ceil_div(tokens * ceil_div(head_dim, 4), 256) >= ((int64_t)1 << 31) || n_heads > 65535)
     return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows for one launch");
   SKV_HIP_CHECK(launch_rotate(r, x, x_stride_tok, x_stride_head, tokens, n_heads, head_dim, dtype == STRUCTKV_DTYPE_BF16, pos, out,
                               out_stride_tok, out_stride_head, (hipStream_t)stream));

@@ -17,7 +17,6 @@ __device__ __forceinline__ float scale_for(float a) {
   const uint32_t up = __float_as_uint(a) + 0x1FFFFFu;   // the exponent carries where the mantissa is beyond 1.75
   return fmaxf(__uint_as_float((up & 0x7F800000u) > (8u << 23) ? (up & 0x7F800000u) - (8u << 23) : 0u), kLeastScale);
 }
-__device__ __forceinline__ float inverse(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }   // of a power of two
 __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
@@ -174,7 +173,7 @@ __global__ __launch_bounds__(SHARE ? 256 : 1024) void paged_append_kernel(TAB ta
       top = exchanged(top, tops[(g - g0) & 1]);
       __syncthreads();
     }
-    const float come = scale_for(top), now = fmaxf(come, before), inv = inverse(now);
+    const float come = scale_for(top), now = fmaxf(come, before), inv = 1.f / now;   // (exact: powers of two)
     if (old > 0 && now > before) {   // the earlier rows' codes in the new scale
       const float ratio = before * inv;
       for (int e = threadIdx.x; e < old * (c.d / 4); e += blockDim.x) {

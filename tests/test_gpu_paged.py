@@ -577,3 +577,36 @@ def test_append_large_batches_like_single_sequences(B, page_size, d, G, tokens, 
     assert res[0][5].tolist() == [x + tokens for x in lens] and res[0][6].tolist() == [0] * batch
     for x, y in zip(*res):
         assert torch.equal(x.view(torch.int16) if x.dtype == torch.bfloat16 else x, y.view(torch.int16) if y.dtype == torch.bfloat16 else y)
+
+
+def test_attend_mass_of_rows_that_are_not_numbers(B):
+    """A key that is NaN: the mass of the pages that the sequence's token sees becomes NaN; other sequences, dropped pages and entries behind
+    the last one keep theirs."""
+    lens = [50, 50]
+    c = R.make_pool(2, 64, 16, 12, [[1, 2, 3, 4], [5, -1, 6, 7]], lens, torch.bfloat16, 3, capacity=6)
+    c.k[6, 1, 3, 7] = 127
+    on = OnGpu(B, c)
+    q, q_gpu = queries(2, 8, 64, torch.bfloat16, 1)
+    out, lse = torch.empty(2, 8, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(2, 8, device="cuda")
+    B.structkv_paged_attend(on.handle, 8, q_gpu, [0, 1, 2], out, lse, on.workspace(B, 8, 2), lam=0.5)
+    assert bool(out[1, 4:].isnan().all()) and bool(out[1, :4].isfinite().all()) and bool(out[0].isfinite().all())
+    mass = on.mass.cpu()
+    assert mass[1, [0, 2, 3]].isnan().all() and bool(mass[0].isfinite().all())
+    assert float(mass[1, 1]) == float(c.mass[1, 1]) * 0.5 and torch.equal(mass[:, 4:], c.mass[:, 4:])
+
+
+def test_attend_workspace_is_as_large_as_it_says(B):
+    """Nothing behind the bytes that a call of so many tokens needs is written, nor behind out and lse."""
+    for lens, fresh, H, d, dtype, lam in (([3000, 60], [1, 1], 8, 128, torch.bfloat16, 0.9), ([700, 300], [40, 9], 8, 64, torch.float32, 0.0),
+                                          ([9000], [1], 32, 64, torch.bfloat16, 0.0)):
+        pages, n = table(lens, 16, np.random.default_rng(1), spare=1)
+        c = R.make_pool(2, d, 16, n, pages, lens, dtype, 1)
+        on, new = OnGpu(B, c), sum(fresh)
+        size = B.structkv_paged_workspace_bytes(on.handle, H, new)
+        ws = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        room = torch.full((new * H * d + 512,), 7.0, dtype=dtype, device="cuda")
+        norms = torch.full((new * H + 64,), 7.0, device="cuda")
+        q, q_gpu = queries(new, H, d, dtype, 1)
+        B.structkv_paged_attend(on.handle, H, q_gpu, cut(fresh), room[:new * H * d], norms[:new * H], ws[:size], lam=lam)
+        assert bool((ws[size:] == 0xA5).all()) and bool((room[new * H * d:] == 7).all()) and bool((norms[new * H:] == 7).all())
+        assert bool(room[:new * H * d].isfinite().all())

@@ -115,7 +115,7 @@ def test_rotate_refusals(B):
                 dict(out=None), dict(pos=None), dict(x=P + 1), dict(out=Q + 1), dict(pos=P + 2), dict(inverse=2), dict(ot=63), dict(ot=0), dict(heads=2, oh=32),
                 dict(out=P, xt=128), dict(heads=2, xh=128, xt=64, oh=256, out=P)):
         assert call(**bad) == 1, (bad, B.structkv_last_error())
-    assert call(dtype=2) == 2 and call(d=70000, ot=70000) == 2 and call(heads=65536, oh=64, ot=1 << 23) == 2 and call(tokens=1 << 40) == 2
+    assert call(dtype=2) == 2 and call(d=70000, ot=70000) == 2 and call(heads=65536, oh=64, ot=1 << 23) == 2 and call(tokens=1 << 40) == 2 and call(tokens=1 << 35) == 2
     assert call(tokens=0, x=None, out=None, pos=None) == 0
 
 
