@@ -151,13 +151,15 @@ struct Pair {
   bool any, two;
 };
 
-template <class TAB, class T, int DP, int RB, bool CAPPED, bool SAVE, bool ONCE, int WAVES>
+// HELD: batches of 64 blocks whose weights stay in LDS until they go to memory, for 16 / HELD rows of a KV head at most; 0: nobody wants them.
+template <class TAB, class T, int DP, int RB, bool CAPPED, int HELD, bool ONCE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 || WAVES > 8 ? 1 : 2) void paged_attend_kernel(TAB tab, CacheView view, PagedView c, ScoreForm f, AttendWork w, bool aligned) {
   constexpr bool F32 = std::is_same<T, float>::value;
   constexpr int QP = F32 ? 3 : 1, PP = F32 ? 2 : 1, KP = DP / 64, W = DP / 16;
   constexpr bool AHEAD = DP <= 128 && (RB == 1 || !F32);   // (the others have no registers for it)
-  constexpr int kBatch = 64, kPitch = kBatch + 1;
-  static_assert(!SAVE || kPitch <= DP + 4, "the blocks' weights lie where the waves' sums come later");
+  constexpr bool SAVE = HELD > 0;
+  constexpr int kBatch = 64, kPitch = HELD * kBatch + 1;
+  static_assert(!SAVE || (16 / (SAVE ? HELD : 1)) * kPitch <= 16 * (DP + 4), "the blocks' weights lie where the waves' sums come later");
   __shared__ __attribute__((aligned(16))) float buf[kFinishBlocks<DP, WAVES>];
   const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -253,16 +255,23 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 || WAVES > 8 ? 1 : 2) voi
       x.iv[kb] = lane_float(iv, x.at[kb]);
     }
   };
-  // the blocks' weights of a batch, in LDS row by row, on their way to memory
-  float* held = buf + wave * 16 * kPitch;
+  // The blocks' weights, in LDS row by row, on their way to memory: a store among the loads holds up those behind it until it has reached
+  // memory, so as many batches at once as there is room for (one at a time: a token over eight caches of 64K to 128K 288 us, four: 279).
+  const int some = min(16, rows - row0);
+  float* held = buf + wave * (16 / (SAVE ? HELD : 1)) * kPitch;
   int held_base = mine0;
   auto put_held = [&]() __attribute__((always_inline)) {
-    float* to = w.x + (int64_t)(p.g * w.gs + row0) * w.xs + ((int64_t)p.b * c.max_pages << lb) + held_base + lane;
-    const int some = min(16, rows - row0);
-    for (int r = 0; r < some; ++r) {
-      const float x = held[r * kPitch + lane];
-      if (held_base + lane < mine1) to[r * w.xs] = x;
-    }
+    float* to = w.x + (int64_t)(p.g * w.gs + row0) * w.xs + ((int64_t)p.b * c.max_pages << lb);
+    const int until = min(mine1, held_base + HELD * kBatch);
+    for (int j = held_base + lane; j < until; j += kBatch)
+      for (int r = 0; r < some; r += 4) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = held[(r + i) * kPitch + j - held_base];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (r + i < some) to[(r + i) * w.xs + j] = x[i];
+      }
   };
   auto work = [&](Pair<DP>& x) __attribute__((always_inline)) {
     const int s0[2] = {(x.base + x.at[0]) * kBlock, (x.base + x.at[1]) * kBlock};
@@ -343,7 +352,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 || WAVES > 8 ? 1 : 2) voi
         for (int j = 0; j < W; ++j) O[j][rb] *= shrink;
       }
     }
-    if (SAVE && x.base != held_base) {
+    if (SAVE && x.base - held_base >= HELD * kBatch) {
       put_held();
       held_base = x.base;
     }
@@ -370,7 +379,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 || WAVES > 8 ? 1 : 2) voi
         Z[rb] = fmaf(z, x.iv[kb], Z[rb]);
         if (SAVE) {
           z = row_total(z);
-          if (q4 == 0 && (kb ? x.two : x.any)) held[l16 * kPitch + x.at[kb]] = __builtin_amdgcn_logf(z) - m;
+          if (lane < some && (kb ? x.two : x.any)) held[l16 * kPitch + x.base - held_base + x.at[kb]] = __builtin_amdgcn_logf(z) - m;
         }
       }
 #pragma unroll
@@ -433,10 +442,9 @@ hipError_t attend(const CacheTable& t, const CacheView& v, const PagedView& c, c
   with_cache_table(t, [&](const auto& tab) {
     using TAB = std::decay_t<decltype(tab)>;
     auto go = [&](auto rb, auto save, auto waves) {
-      constexpr int RB = decltype(rb)::value, WAVES = decltype(waves)::value;
-      constexpr bool SAVE = decltype(save)::value;
+      constexpr int RB = decltype(rb)::value, WAVES = decltype(waves)::value, HELD = decltype(save)::value;
       auto form = [&](auto capped, auto once) {
-        paged_attend_kernel<TAB, T, DP, RB, decltype(capped)::value, SAVE, decltype(once)::value, WAVES>
+        paged_attend_kernel<TAB, T, DP, RB, decltype(capped)::value, HELD, decltype(once)::value, WAVES>
             <<<(unsigned)(p.units * c.G), 64 * WAVES, 0, st>>>(tab, v, c, f, w, aligned);
       };
       auto by_cap = [&](auto once) { f.softcap > 0.f ? form(std::true_type{}, once) : form(std::false_type{}, once); };
@@ -445,10 +453,12 @@ hipError_t attend(const CacheTable& t, const CacheView& v, const PagedView& c, c
     const std::integral_constant<int, kAttendWaves> four;
     const std::integral_constant<int, kShortWaves> more;
     const std::integral_constant<int, 1> one;
-    if (w.x) go(one, std::true_type{}, four);
-    else if (p.rows == 16 && p.waves == kAttendWaves) go(one, std::false_type{}, four);
-    else if (p.rows == 16) go(one, std::false_type{}, more);
-    else if constexpr (DP <= 128 || sizeof(T) == 2) go(std::integral_constant<int, 2>{}, std::false_type{}, four);
+    const std::integral_constant<int, 0> none;
+    if (w.x && w.gs <= 4) go(one, four, four);
+    else if (w.x) go(one, one, four);
+    else if (p.rows == 16 && p.waves == kAttendWaves) go(one, none, four);
+    else if (p.rows == 16) go(one, none, more);
+    else if constexpr (DP <= 128 || sizeof(T) == 2) go(std::integral_constant<int, 2>{}, none, four);
   });
   return hipGetLastError();
 }

@@ -610,3 +610,10 @@ def test_attend_workspace_is_as_large_as_it_says(B):
         B.structkv_paged_attend(on.handle, H, q_gpu, cut(fresh), room[:new * H * d], norms[:new * H], ws[:size], lam=lam)
         assert bool((ws[size:] == 0xA5).all()) and bool((room[new * H * d:] == 7).all()) and bool((norms[new * H:] == 7).all())
         assert bool(room[:new * H * d].isfinite().all())
+
+
+@pytest.mark.parametrize("G,H,n", [(128, 128, 70000), (64, 512, 36000)])
+def test_attend_weights_of_long_shares(B, G, H, n):
+    """Waves that see more blocks than have room for their weights at once."""
+    pages, total = table([n], 64, np.random.default_rng(3), dropped=0.2, fresh=[1])
+    check_attend(B, R.make_pool(G, 16, 64, total, pages, [n], torch.bfloat16, 3, capacity=len(pages[0])), H, [1], lam=0.9)
