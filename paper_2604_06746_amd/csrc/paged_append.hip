@@ -4,6 +4,10 @@
 // page's scale grows, its earlier codes move by exponents: only those that become subnormal lose bits.
 // A workgroup takes what comes into one page for one KV head's keys or values: the largest magnitude first, then the codes, so no two
 // workgroups share a scale.  Queries that come with the rows are other workgroups of the same launch.
+// Prompts are bound by memory, three quarters of it the queries': eight of 5715 tokens (1.03 GB) 229 us.  Rows that are read again for the
+// codes 391 us; kept in registers, with the queries' angles shared by heads, 257; wide pieces, past the caches 240; checks for values that cannot be
+// stored out of the way 235; keys' angles for eight heads 229 (for none of them 253).  A token of each of 64 sequences 4.8 us: a chain of
+// length, table and scale, beside which its row is on its way.
 #include "paged.h"
 
 #include <algorithm>

@@ -3,7 +3,7 @@
 // Chunk i of a row left (M_i, Z_i, O_i); with M = max M_i: Z = sum 2^(M_i - M) Z_i, out = sum 2^(M_i - M) O_i / Z, lse = ln 2 (M + log2 Z).
 // The first launch also left each row's weight of each block of 16 slots, in the log2 domain: a page's mass takes 2^(x - lse2) of its
 // blocks and all heads.  Few bytes, so what counts is the chain of loads; the workgroups that gather form the rows' norms themselves, beside
-// those that join the rows, and have the blocks' weights on their way meanwhile.
+// those that join the rows, and have the blocks' weights on their way meanwhile.  2081 slots 6.0 us (by two launches 4.3 + 11.2), eight of 64K to 128K 11.
 #include "paged.h"
 
 namespace skv {
