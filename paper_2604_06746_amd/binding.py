@@ -8,6 +8,7 @@ from __future__ import annotations
 import array
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -180,6 +181,14 @@ def _host_i64(values: Sequence[int]):
         return (_i64 * len(values))(*values)
     except TypeError:   # (numbers of other kinds)
         return (_i64 * len(values))(*[int(v) for v in values])
+
+
+def _packed_i64(values: Sequence[int]) -> bytes:
+    """Offsets for the length of a call (65: 0.35 us against 1.0)."""
+    try:
+        return struct.pack("%dq" % len(values), *values)
+    except struct.error:   # (numbers of other kinds)
+        return struct.pack("%dq" % len(values), *[int(v) for v in values])
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -673,7 +682,7 @@ def structkv_paged_append(cache: structkv_paged, k_new: torch.Tensor, v_new: tor
         heads = q.shape[1]
         st, sh = _query_strides(cache, heads, q, new)
         _vector(q_out, cache.tensor_dtype, new * heads * cache.head_dim, cache.index, "q_out")
-    _cache_call(_lib.structkv_paged_append, cache, stream, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], _host_i64(cu_new),
+    _cache_call(_lib.structkv_paged_append, cache, stream, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], _packed_i64(cu_new),
                 None if rotary is None else ctypes.byref(rotary), _ptr(pos_new), heads, _ptr(q), st, sh, _ptr(q_out), lens_out.data_ptr())
 
 
@@ -685,5 +694,5 @@ def structkv_paged_attend(cache: structkv_paged, n_q_heads: int, q: torch.Tensor
     st, sh = _query_strides(cache, n_q_heads, q, new)
     _vector(out, cache.tensor_dtype, new * n_q_heads * cache.head_dim, cache.index, "out")
     _vector(lse_out, torch.float32, new * n_q_heads, cache.index, "lse_out")
-    _cache_call(_lib.structkv_paged_attend, cache, stream, n_q_heads, scale, softcap, q.data_ptr(), st, sh, _host_i64(cu_new), lam,
+    _cache_call(_lib.structkv_paged_attend, cache, stream, n_q_heads, scale, softcap, q.data_ptr(), st, sh, _packed_i64(cu_new), lam,
                 out.data_ptr(), lse_out.data_ptr(), workspace.data_ptr(), _workspace(cache, workspace))

@@ -158,7 +158,7 @@ struct Pair {
 
 // HELD: batches of 64 blocks whose weights stay in LDS until they go to memory, for 16 / HELD rows of a KV head at most; 0: nobody wants them.
 template <class TAB, class T, int DP, int RB, bool CAPPED, int HELD, bool ONCE, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, RB * DP > 256 || WAVES > 8 ? 1 : 2) void paged_attend_kernel(TAB tab, CacheView view, PagedView c, ScoreForm f, AttendWork w, bool aligned) {
+__global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_attend_kernel(TAB tab, CacheView view, PagedView c, ScoreForm f, AttendWork w, bool aligned) {
   constexpr bool F32 = std::is_same<T, float>::value;
   constexpr int QP = F32 ? 3 : 1, PP = F32 ? 2 : 1, KP = DP / 64, W = DP / 16;
   constexpr bool AHEAD = DP <= 128 && (RB == 1 || !F32);   // (the others have no registers for it)
