@@ -103,6 +103,9 @@ structkv_status check_query_heads(const structkv_paged* c, int32_t H) {
 // Workgroups: two a CU, chunks of at least kLeast slots.  (Sixteen caches of 1K to 6.6K slots: 512 32.7 us, 768 33.0, 1024 35.2; four of 8K to 16.5K, 32 rows:
 // 512 31 us, 1024 39.)
 constexpr int64_t kUnits = 512, kLeast = 128;
+// ... of 256 where a workgroup has 32 rows, whose partial results cost more to join: chains of 64 over 1000 slots 17.3 -> 14.2 us, of 13 over 4000
+// 16.2 -> 13.7, of 13 over 1000 12.4 -> 13.4 (512: 14.4, 14.3 and 14.9).
+constexpr int64_t kLeastRows = 256;
 // Mean slots of a block of rows from which on it is cut in two even where the blocks fill the chip.
 constexpr int64_t kCut = 4096;
 
@@ -121,13 +124,14 @@ structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, Ca
   for (int b = 0; b < v.batch; ++b) most_rows = std::max<int64_t>(most_rows, (int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs);
   if (most_rows >= (1 << 18)) return fail(STRUCTKV_ERR_UNSUPPORTED, "%lld query rows of a KV head in one sequence, they must stay below 2^18", (long long)most_rows);
   p->rows = gather || most_rows <= 16 || (!bf16 && v.d > 128) ? 16 : 32;   // (32 rows of 256 components in fp32: no registers for it)
-  p->min_chunk = kAttendWaves * 32;
+  const int64_t least = p->rows == 16 ? kLeast : kLeastRows;
+  p->min_chunk = (int)least;
   p->stream = most_rows <= p->rows;   // nobody else reads the codes: past the caches (eight of 64K to 128K 304 -> 289 us, 64 of 2K 67 -> 61, four of 16K by 32 rows 31.4 -> 31.8)
   int64_t blocks = 0, chunks = 0;
   for (int b = 0; b < v.batch; ++b) {
     const int64_t rcs = ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, p->rows);
     blocks += rcs;
-    chunks += rcs * std::max<int64_t>(1, ceil_div(cap, kLeast));
+    chunks += rcs * std::max<int64_t>(1, ceil_div(cap, least));
     t->units[b + 1] = (int32_t)blocks;
   }
   const bool cut = p->rows == 16 && cap >= kCut;
