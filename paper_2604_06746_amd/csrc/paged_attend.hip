@@ -441,6 +441,9 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
   finish_blocks<T, DP, RB, WAVES>(O, M, Z, buf, w, c.d, p.g, row0, rows, new0, p.nc);
 }
 
+}  // namespace
+
+// Compiled in six parts, one object each with SKV_PAGED_PART = 0 .. 5 (in one they take minutes); part 0 also holds the dispatch.
 template <class T, int DP>
 hipError_t attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const PagedPlan& p, const AttendWork& w, hipStream_t st) {
   const bool aligned = (((uintptr_t)w.q | (uintptr_t)((w.qst | w.qsh) * (int64_t)sizeof(T))) & 15) == 0;
@@ -468,6 +471,16 @@ hipError_t attend(const CacheTable& t, const CacheView& v, const PagedView& c, c
   return hipGetLastError();
 }
 
+#define SKV_PAGED_INST(T, DP) \
+  template hipError_t attend<T, DP>(const CacheTable&, const CacheView&, const PagedView&, const ScoreForm&, const PagedPlan&, const AttendWork&, hipStream_t)
+#if SKV_PAGED_PART == 0
+SKV_PAGED_INST(uint16_t, 64);
+extern SKV_PAGED_INST(uint16_t, 128);
+extern SKV_PAGED_INST(uint16_t, 256);
+extern SKV_PAGED_INST(float, 64);
+extern SKV_PAGED_INST(float, 128);
+extern SKV_PAGED_INST(float, 256);
+
 template <class T>
 hipError_t by_dim(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const PagedPlan& p, const AttendWork& w, hipStream_t st) {
   if (c.d <= 64) return attend<T, 64>(t, v, c, f, p, w, st);
@@ -475,11 +488,20 @@ hipError_t by_dim(const CacheTable& t, const CacheView& v, const PagedView& c, c
   return attend<T, 256>(t, v, c, f, p, w, st);
 }
 
-}  // namespace
-
 hipError_t launch_paged_attend(const CacheTable& t, const CacheView& v, const PagedView& c, const ScoreForm& f, const PagedPlan& p,
                                const AttendWork& w, bool bf16, hipStream_t st) {
   return bf16 ? by_dim<uint16_t>(t, v, c, f, p, w, st) : by_dim<float>(t, v, c, f, p, w, st);
 }
+#elif SKV_PAGED_PART == 1
+SKV_PAGED_INST(uint16_t, 128);
+#elif SKV_PAGED_PART == 2
+SKV_PAGED_INST(uint16_t, 256);
+#elif SKV_PAGED_PART == 3
+SKV_PAGED_INST(float, 64);
+#elif SKV_PAGED_PART == 4
+SKV_PAGED_INST(float, 128);
+#else
+SKV_PAGED_INST(float, 256);
+#endif
 
 }  // namespace skv
