@@ -3,6 +3,8 @@
 #include "cache.h"
 #include "rotary.h"
 
+#include <cmath>
+
 namespace skv {
 
 // The cache as kernels see it.
@@ -55,7 +57,12 @@ hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const Pa
 // Waves of a workgroup that takes a whole short sequence's slots, so that nothing has to be joined.
 constexpr int kShortWaves = 8;
 // An attend call is cut like one on a cache of slots (AttendPlan, AttendWork): x in AttendWork are here the weights of blocks of kBlock slots
-// in the log2 domain, head h, block i of sequence b at h xs + b blocks + i.
+// as their log2, head h, block i of sequence b at h xs + b blocks + i.  Weights in units of 2^u that are not small are kApart there, and the pair
+// (u, log2 in those units) lies at twice that place behind all of them.
+constexpr float kSmallUnit = 1024.f, kApart = INFINITY;
+struct PagedUnit {
+  float unit, weight;
+};
 struct PagedPlan : AttendPlan {
   int waves;   // of a workgroup: kAttendWaves, or kShortWaves (16 rows, nothing to join)
 };

@@ -149,7 +149,7 @@ structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, Ca
   p->off_shares = off; off += p->join ? align_up(sizeof(int4) * (size_t)v.batch, 256) : 0;
   p->off_ml = off; off += align_up((size_t)part * 2 * sizeof(float), 256);
   p->off_o = off;  off += align_up((size_t)part * dp * sizeof(float), 256);
-  p->off_x = off;  off += gather ? align_up((size_t)H * v.batch * block_slots(v) * sizeof(float), 256) : 0;
+  p->off_x = off;  off += gather ? align_up((size_t)H * v.batch * block_slots(v) * 3 * sizeof(float), 256) : 0;
   p->total_bytes = off;
   return STRUCTKV_OK;
 }
@@ -162,7 +162,7 @@ size_t most_paged_bytes(const PagedView& v, int H, int64_t new_tokens) {
   const int64_t blocks16 = with_tokens * ceil_div(gs, 16) + new_tokens * gs / 16;
   const size_t part = (size_t)std::max<int64_t>(32 * kUnits, 2 * blocks16 * 16 * v.G);
   return align_up(sizeof(int4) * (size_t)v.batch, 256) + align_up(part * 2 * sizeof(float), 256) + align_up(part * dp * sizeof(float), 256) +
-         (v.mass ? align_up((size_t)H * v.batch * block_slots(v) * sizeof(float), 256) : 0);
+         (v.mass ? align_up((size_t)H * v.batch * block_slots(v) * 3 * sizeof(float), 256) : 0);
 }
 
 uint32_t gs_reciprocal(int gs) { return gs > 1 ? (uint32_t)(((uint64_t)1 << 32) / gs) + 1u : 0u; }

@@ -28,6 +28,10 @@ typedef __attribute__((ext_vector_type(4))) uint32_t four;
 
 // Weights are at most 2^kTop (65504 is fp16's last number); when one would be more, the reference is raised so that the largest is some 2^kFresh.
 constexpr float kTop = 15.f, kFresh = 7.f;
+// From references of this size on, whole numbers only just, the fma takes a product and its row's reference apart by the latter's rounding, in the end by
+// more than an exponent bears.  The wave then takes its blocks once more (CARE), by scores rounded once and references in two parts: N, the highest score,
+// and L, a small number that has the values' scales: w = 2^((y - N) + (log2 s_v - L)).
+constexpr float kHuge = 8388608.f;
 
 // ONCE: past the caches
 template <int N, bool ONCE> __device__ __forceinline__ void load_bytes(uint32_t (&to)[N / 4], const uint8_t* p) {
@@ -101,11 +105,12 @@ __device__ __forceinline__ void load_query(bf16x8 (&q)[QP], const T* row, int c,
 }
 
 // What the waves of a workgroup leave, added up in their order through LDS and written out by all threads (leave), 16 rows at a time.  A lane
-// holds components 4 W q4 + W e + j of its rows in O[j][rb][e].
+// holds components 4 W q4 + W e + j of its rows in O[j][rb][e].  What a wave puts there has its weights' sum
+// between 1/2 and 1, the power of two taken to M; with references in two parts (apart), relative to N.
 template <int DP, int WAVES>
 constexpr int kFinishBlocks = WAVES * 16 * (DP + 4 + 2);
 template <class T, int DP, int RB, int WAVES>
-__device__ __forceinline__ void finish_blocks(const floatx4 (&O)[DP / 16][RB], const float (&M)[RB], const float (&Zl)[RB], float* buf,
+__device__ __forceinline__ void finish_blocks(const floatx4 (&O)[DP / 16][RB], const float (&Ml)[RB], const float (&Zl)[RB], const float (*apart)[2], float* buf,
                                               const AttendWork& w, int d, int g, int row0, int rows, int new0, int nc) {
   constexpr int PITCH = DP + 4, W = DP / 16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q4 = lane >> 4;
@@ -113,16 +118,24 @@ __device__ __forceinline__ void finish_blocks(const floatx4 (&O)[DP / 16][RB], c
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     if (row0 + rb * 16 >= rows) break;
-    const float z = row_total(Zl[rb]);
+    float z = row_total(Zl[rb]), M = Ml[rb];
+    int shift = M > kNothingSeen ? -__builtin_amdgcn_frexp_expf(z) : 0;   // (0 for 0 and NaN)
+    if (apart) {
+      M = apart[rb * 16 + l16][0];
+      shift = (int)apart[rb * 16 + l16][1];
+    } else {
+      M -= (float)shift;
+    }
+    z = ldexpf(z, shift);
     if (rb > 0) __syncthreads();
     if (q4 == 0) {
-      ml[(wave * 16 + l16) * 2] = M[rb];
+      ml[(wave * 16 + l16) * 2] = M;
       ml[(wave * 16 + l16) * 2 + 1] = z;
     }
     __syncthreads();
     float top = ml[l16 * 2];
     for (int i = 1; i < WAVES; ++i) top = fmaxf(top, ml[(i * 16 + l16) * 2]);
-    const float f = __builtin_amdgcn_exp2f(M[rb] - top);
+    const float f = ldexpf(__builtin_amdgcn_exp2f(M - top), shift);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -166,6 +179,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
   constexpr int kBatch = 64, kPitch = HELD * kBatch + 1;
   static_assert(!SAVE || (16 / (SAVE ? HELD : 1)) * kPitch <= 16 * (DP + 4), "the blocks' weights lie where the waves' sums come later");
   __shared__ __attribute__((aligned(16))) float buf[kFinishBlocks<DP, WAVES>];
+  __shared__ float parts[WAVES][16 * RB][2];   // (N, L) of the waves' rows, where huge
   const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const AttendPlace p = attend_place(tab, view, w);
@@ -195,6 +209,8 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
     for (int j = 0; j < W; ++j) O[j][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
   const Cap cap(f, CAPPED ? kLog2e : 1.f);
+  bool again = false;   // the blocks are to be taken with care
+  bool huge = false;    // the references are in `parts`, and M is 0
   int odd = 0x7FFFFFFF;   // the first fresh slot behind the first one whose values are not all numbers
 
   const int lb = c.shift - 4, first = p.s0 / kBlock, last = end > p.s0 ? (end + kBlock - 1) / kBlock : first;
@@ -262,23 +278,91 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
   };
   // The blocks' weights, in LDS row by row, on their way to memory: a store among the loads holds up those behind it until it has reached
   // memory, so as many batches at once as there is room for (one at a time: a token over eight caches of 64K to 128K 288 us, four: 279).
+  // They are held as the log2 of their sums; with CARE, since a large reference would take their bits, in units of it, and what leaves for rows whose
+  // reference is no small number is kApart, the reference and they behind the others.  (So for all rows: 289 us.)
   const int some = min(16, rows - row0);
   float* held = buf + wave * (16 / (SAVE ? HELD : 1)) * kPitch;
   int held_base = mine0;
-  auto put_held = [&]() __attribute__((always_inline)) {
+  auto put_held = [&](auto care) __attribute__((always_inline)) {
     float* to = w.x + (int64_t)(p.g * w.gs + row0) * w.xs + ((int64_t)p.b * c.max_pages << lb);
     const int until = min(mine1, held_base + HELD * kBatch);
-    for (int j = held_base + lane; j < until; j += kBatch)
-      for (int r = 0; r < some; r += 4) {
-        float x[4];
+    if constexpr (!decltype(care)::value) {
+      for (int j = held_base + lane; j < until; j += kBatch)
+        for (int r = 0; r < some; r += 4) {
+          float x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = held[(r + i) * kPitch + j - held_base];
+          for (int i = 0; i < 4; ++i) x[i] = held[(r + i) * kPitch + j - held_base];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (r + i < some) to[(r + i) * w.xs + j] = x[i];
+          for (int i = 0; i < 4; ++i)
+            if (r + i < some) to[(r + i) * w.xs + j] = x[i];
+        }
+    } else {
+      PagedUnit* pairs = reinterpret_cast<PagedUnit*>(w.x + w.H * w.xs) + (to - w.x);
+      const float N = huge ? parts[wave][l16][0] : M[0], L = huge ? parts[wave][l16][1] : 0.f;
+#pragma nounroll
+      for (int r = 0; r < some; ++r) {
+        const float n = lane_float(N, r), l = lane_float(L, r);
+        const bool small = fabsf(n) < kSmallUnit;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+          const int j = held_base + i * kBatch + lane;
+          if (j >= until) continue;
+          const float x = held[r * kPitch + i * kBatch + lane] + l;
+          to[r * w.xs + j] = small ? n + x : kApart;
+          if (!small) pairs[r * w.xs + j] = PagedUnit{n, x};
+        }
       }
+    }
   };
-  auto work = [&](Pair<DP>& x) __attribute__((always_inline)) {
+  // ... in units of 2^-by (all that there is room for: what is not held yet may be anything)
+  auto shift_held = [&](float by) __attribute__((always_inline)) {
+#pragma nounroll
+    for (int r = 0; r < some; ++r) {
+      const float x = lane_float(by, r);
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) held[r * kPitch + i * kBatch + lane] += x;
+    }
+  };
+  // Where huge: scores made the exponents of their weights, (y - N) + (log2 s_v - L), the references first moved, by -step, where one would be too large.
+  auto to_exponents = [&](floatx4 (&y)[2][RB], float (&f2)[2], float (&lv)[2], float (&step)[RB]) __attribute__((always_inline)) {
+#pragma clang fp contract(off)   // (scores are rounded before anything is subtracted)
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float N = parts[wave][rb * 16 + l16][0], L = parts[wave][rb * 16 + l16][1], top = -INFINITY, most = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        float best = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[kb][rb][e] = y[kb][rb][e] * f2[kb];
+          best = fmaxf(best, y[kb][rb][e]);
+        }
+        top = fmaxf(top, best);
+        most = fmaxf(most, (best - N) + (lv[kb] - L));
+      }
+      step[rb] = 0.f;
+      if (__any(top - N > kTop || most > kTop)) {
+        const float Nn = fmaxf(N, row_top(top));
+        most = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most = fmaxf(most, (y[kb][rb][e] - Nn) + lv[kb]);
+        const float Ln = fmaxf(ceilf(L + (N - Nn)), ceilf(row_top(most)) - kFresh);   // (whole: a shift in the end)
+        step[rb] = (N - Nn) + (L - Ln);
+        parts[wave][rb * 16 + l16][0] = N = Nn;
+        parts[wave][rb * 16 + l16][1] = L = Ln;
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[kb][rb][e] = (y[kb][rb][e] - N) + (lv[kb] - L);
+    }
+    f2[0] = f2[1] = 1.f;
+    lv[0] = lv[1] = 0.f;
+  };
+  auto work = [&](Pair<DP>& x, auto care) __attribute__((always_inline)) {
+    constexpr bool CARE = decltype(care)::value;
     const int s0[2] = {(x.base + x.at[0]) * kBlock, (x.base + x.at[1]) * kBlock};
     floatx4 y[2][RB];
 #pragma unroll
@@ -308,7 +392,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
       }
     }
     // (capped scores are in the log2 domain; the others are still to be multiplied)
-    const float f2[2] = {CAPPED ? 1.f : x.kf[0], CAPPED ? 1.f : x.kf[1]};
+    float f2[2] = {CAPPED ? 1.f : x.kf[0], CAPPED ? 1.f : x.kf[1]}, lv[2] = {x.lv[0], x.lv[1]};
     auto best = [&](int kb, int rb) __attribute__((always_inline)) {
       return fmaxf(fmaxf(y[kb][rb][0], y[kb][rb][1]), fmaxf(y[kb][rb][2], y[kb][rb][3]));
     };
@@ -336,29 +420,52 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
         }
       }
     }
-    bool high = false;
+    bool high = CARE && huge;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
-        high |= fmaf(best(kb, rb), f2[kb], x.lv[kb] - M[rb]) > kTop;
+        high |= fmaf(best(kb, rb), f2[kb], lv[kb] - M[rb]) > kTop;
     if (__any(high)) {
+      float step[RB];   // of the references, downwards
+      if (!CARE || !huge) {
+        float Mn[RB];
+        bool far = false;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const float top = row_top(fmaxf(fmaf(best(0, rb), f2[0], lv[0]), fmaf(best(1, rb), f2[1], lv[1])));
+          Mn[rb] = fmaxf(M[rb], ceilf(top) - kFresh);
+          far |= fabsf(Mn[rb]) >= (SAVE && !CARE ? kSmallUnit : kHuge) && Mn[rb] > kNothingSeen;
+          step[rb] = M[rb] - Mn[rb];
+        }
+        far = __any(far);
+        if (!CARE && far) {   // (what the usual loop still does comes to nothing)
+          again = true;
+          todo = 0;
+          next = mine1;
+        }
+        if (CARE) huge = far;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          if (CARE && huge) {
+            parts[wave][rb * 16 + l16][0] = M[rb];
+            parts[wave][rb * 16 + l16][1] = 0.f;
+          }
+          M[rb] = CARE && huge ? 0.f : Mn[rb];
+        }
+      }
+      if (CARE && huge) to_exponents(y, f2, lv, step);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-          top = fmaxf(top, fmaf(best(kb, rb), f2[kb], x.lv[kb]));
-        top = row_top(top);
-        const float Mn = fmaxf(M[rb], ceilf(top) - kFresh), shrink = __builtin_amdgcn_exp2f(M[rb] - Mn);
-        M[rb] = Mn;
+        const float shrink = __builtin_amdgcn_exp2f(step[rb]);
         Z[rb] *= shrink;
 #pragma unroll
         for (int j = 0; j < W; ++j) O[j][rb] *= shrink;
+        if (SAVE && CARE) shift_held(step[rb]);
       }
     }
     if (SAVE && x.base - held_base >= HELD * kBatch) {
-      put_held();
+      put_held(care);
       held_base = x.base;
     }
     halfx8 weight[RB][PP];
@@ -366,7 +473,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const float m = x.lv[kb] - M[rb];
+        const float m = lv[kb] - M[rb];
         float z = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; e += 2) {
@@ -383,8 +490,8 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
         }
         Z[rb] = fmaf(z, x.iv[kb], Z[rb]);
         if (SAVE) {
-          z = row_total(z);
-          if (lane < some && (kb ? x.two : x.any)) held[l16 * kPitch + x.base - held_base + x.at[kb]] = __builtin_amdgcn_logf(z) - m;
+          z = row_total(z * x.iv[kb]);
+          if (lane < some && (kb ? x.two : x.any)) held[l16 * kPitch + x.base - held_base + x.at[kb]] = __builtin_amdgcn_logf(z) + (CARE ? 0.f : M[0]);
         }
       }
 #pragma unroll
@@ -410,6 +517,8 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
   };
   // two pairs in turns: one at work while the other is on its way
   // (a pool without pages has no memory that the loads past the last block could read)
+  const std::false_type usual;
+  const std::true_type care;
   Pair<DP> a;
   a.any = false;
   if (c.n_pages > 0) fetch(a);
@@ -418,18 +527,35 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
       Pair<DP> b;
       while (todo != 0 || next < mine1) {   // (one way out: a second one, between the halves, makes the waits for loads give up their counts)
         fetch(b);
-        work(a);
+        work(a, usual);
         fetch(a);
-        if (b.any) work(b);
+        if (b.any) work(b, usual);
       }
-      if (a.any) work(a);
+      if (a.any) work(a, usual);
     } else {
       do {
-        work(a);
+        work(a, usual);
         fetch(a);
       } while (a.any);
     }
-    if (SAVE) put_held();
+    if (__builtin_expect(again, false)) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        M[rb] = kNothingSeen; Z[rb] = 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) O[j][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+      todo = 0;
+      next = base = held_base = mine0;
+      fetch(a);
+      do {
+        work(a, care);
+        fetch(a);
+      } while (a.any);
+      if (SAVE) put_held(care);
+    } else if (SAVE) {
+      put_held(usual);
+    }
   }
   if (__any(odd != 0x7FFFFFFF)) {
     for (int m = 32; m; m >>= 1) odd = min(odd, __shfl_xor(odd, m));
@@ -438,7 +564,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
 #pragma unroll
       for (int j = 0; j < W; ++j) O[j][rb] *= limit[rb] > odd ? NAN : 1.f;
   }
-  finish_blocks<T, DP, RB, WAVES>(O, M, Z, buf, w, c.d, p.g, row0, rows, new0, p.nc);
+  finish_blocks<T, DP, RB, WAVES>(O, M, Z, huge ? parts[wave] : nullptr, buf, w, c.d, p.g, row0, rows, new0, p.nc);
 }
 
 }  // namespace

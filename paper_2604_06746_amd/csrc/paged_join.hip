@@ -2,7 +2,7 @@
 //
 // Chunk i of a row left (M_i, Z_i, O_i); with M = max M_i: Z = sum 2^(M_i - M) Z_i, out = sum 2^(M_i - M) O_i / Z, lse = ln 2 (M + log2 Z).
 // The first launch also left each row's weight of each block of 16 slots, in the log2 domain: a page's mass takes 2^(x - lse2) of its
-// blocks and all heads.  Few bytes, so what counts is the chain of loads; the workgroups that gather form the rows' norms themselves, beside
+// blocks and all heads, or, of weights in units of 2^u, 2^((u - M) + (x - log2 Z)), large numbers and small ones apart.  Few bytes, so what counts is the chain of loads; the workgroups that gather form the rows' norms themselves, beside
 // those that join the rows, and have the blocks' weights on their way meanwhile.  2081 slots 6.0 us (by two launches 4.3 + 11.2), eight of 64K to 128K 11.
 #include "paged.h"
 
@@ -45,7 +45,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, A
   constexpr int LANES = DP / 4, PARTS = 256 / LANES;
   __shared__ __attribute__((aligned(16))) float sh[256 * 4];
   __shared__ float zs[4];
-  extern __shared__ float norms[];   // of the heads
+  extern __shared__ float norms[];   // of the heads: M + log2 Z, and behind them each apart
+  PagedUnit* apart_norms = reinterpret_cast<PagedUnit*>(norms + w.H);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int)blockIdx.x < row_blocks) {   // a row: lane groups on shares of its chunks
     const int r = (int)(blockIdx.x / (uint32_t)w.H), head = (int)blockIdx.x - r * w.H;
@@ -134,7 +135,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, A
     for (int j = 0; j < kAhead; ++j) {
       if (h0 + 4 * j >= w.H) break;
       const float top = wave_top(a[j][0]), z = wave_total(a[j][1] * __builtin_amdgcn_exp2f(a[j][0] - top));
-      if (lane == 0) norms[h0 + 4 * j] = z != 0.f ? top + __builtin_amdgcn_logf(z) : INFINITY;
+      if (lane == 0) {
+        const float log_z = z != 0.f ? __builtin_amdgcn_logf(z) : INFINITY;
+        norms[h0 + 4 * j] = top + log_z;
+        apart_norms[h0 + 4 * j] = PagedUnit{top, log_z};
+      }
     }
   }
   __syncthreads();   // (a wave reads its own heads' norms; the barrier is for the wave's own writes too)
@@ -148,9 +153,23 @@ __global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, A
       const int h = h0 + 4 * (kAhead + k);
       ahead[k] = there && h < w.H ? x[h * w.xs] : -INFINITY;
     }
+    float exponent[kAhead];
+    bool apart = false;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (h0 + 4 * k < w.H) sum += there ? __builtin_amdgcn_exp2f(now[k] - norms[h0 + 4 * k]) : 0.f;
+    for (int k = 0; k < kAhead; ++k) {
+      exponent[k] = h0 + 4 * k < w.H ? now[k] - norms[h0 + 4 * k] : -INFINITY;
+      apart |= now[k] == kApart;
+    }
+    if (__any(apart)) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (now[k] == kApart) {
+          const PagedUnit pair = reinterpret_cast<const PagedUnit*>(w.x + w.H * w.xs)[x - w.x + (h0 + 4 * k) * w.xs], norm = apart_norms[h0 + 4 * k];
+          exponent[k] = (pair.unit - norm.unit) + (pair.weight - norm.weight);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) sum += there ? __builtin_amdgcn_exp2f(exponent[k]) : 0.f;
   }
   sh[threadIdx.x] = sum;
   __syncthreads();
@@ -173,7 +192,7 @@ hipError_t launch_paged_join(const CacheTable& t, const PagedView& c, const Atte
     constexpr int DP = decltype(dp)::value;
     with_cache_table(t, [&](const auto& tab) {
       using TAB = std::decay_t<decltype(tab)>;
-      const size_t lds = sizeof(float) * w.H;
+      const size_t lds = (sizeof(float) + sizeof(PagedUnit)) * w.H;
       if (bf16) paged_join_kernel<TAB, uint16_t, DP><<<(unsigned)blocks, 256, lds, st>>>(tab, c, w, (int)w.rows);
       else paged_join_kernel<TAB, float, DP><<<(unsigned)blocks, 256, lds, st>>>(tab, c, w, (int)w.rows);
     });

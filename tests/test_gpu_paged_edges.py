@@ -1,0 +1,151 @@
+"""GPU tests of attention over a cache held in pages, beside test_gpu_paged.py: scores, scales and values at their limits.
+
+Tolerances as derived there, unless a test says otherwise."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_reference as R
+from test_gpu_paged import B, EPS, OnGpu, cut, table, within  # noqa: F401  (B is the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def run(B, c, H, q, fresh, *, scale=1.0, softcap=0.0, lam=0.0, on=None):  # noqa: F811
+    """(out, lse, mass) in host memory."""
+    on, new = on or OnGpu(B, c), sum(fresh)
+    out = torch.full((new, H, c.d), math.nan, dtype=c.dtype, device="cuda")
+    lse = torch.full((new, H), math.nan, device="cuda")
+    B.structkv_paged_attend(on.handle, H, q.cuda(), cut(fresh), out, lse, on.workspace(B, H, new), scale=scale, softcap=softcap, lam=lam)
+    return out.cpu(), lse.cpu(), on.mass.cpu()
+
+
+FORMS = [(torch.bfloat16, 128, 2, 8, 1), (torch.bfloat16, 64, 2, 8, 7), (torch.bfloat16, 128, 2, 8, 40), (torch.float32, 64, 2, 8, 7), (torch.float32, 128, 2, 40, 1),
+         (torch.bfloat16, 80, 2, 4, 1), (torch.float32, 256, 1, 4, 3), (torch.bfloat16, 256, 1, 4, 20)]
+
+
+@pytest.mark.parametrize("dtype,d,G,H,T", FORMS)
+@pytest.mark.parametrize("lens", [[1300, 700], [300, 90]])
+@pytest.mark.parametrize("score", [-2.0 ** 22, 2.0 ** 23, 2.0 ** 25, -2.0 ** 28, 2.0 ** 28, 2.0 ** 30, -2.0 ** 40, 2.0 ** 40, -2.0 ** 90, 2.0 ** 110, -2.0 ** 125])
+def test_scores_far_from_zero(B, dtype, d, G, H, T, lens, score):  # noqa: F811
+    """A row whose scores are huge attends to the highest: one slot's value as it is, lse its score (to log2 and back: a rounding each of score,
+    factor and product on both ways), mass of one for each head."""
+    best = [77 * lens[0] // 100, 0]
+    pages, n = table(lens, 16, np.random.default_rng(5), spare=1)
+    c = R.make_pool(G, d, 16, n, pages, lens, dtype, 41)
+    c.k[:], c.ks[:] = 0, 1.0
+    small, large = R.encode(torch.tensor([1.125, 2.0], dtype=torch.float64)) + (128 if score < 0 else 0)
+    c.k[:, :, :, 0] = large if score < 0 else small
+    for b in range(2):
+        c.k[pages[b][best[b] // 16], :, best[b] % 16, 0] = small if score < 0 else large
+    q = torch.zeros(2 * T, H, d, dtype=dtype)
+    q[:, :, 0] = 1.2890625 * abs(score)
+    want = 1.2890625 * abs(score) * (-1.125 if score < 0 else 2.0)
+    out, lse, mass = run(B, c, H, q, [T, T], lam=0.5 if T == 1 else 0.0)
+    for b in range(2):
+        p, r = pages[b][best[b] // 16], best[b] % 16
+        v = (R.decode(c.v[p, :, r]) * c.vs[p].double()[:, None]).repeat_interleave(H // G, 0)      # (exact in 16 bits)
+        assert torch.equal(out[b * T:(b + 1) * T].double(), v.expand(T, H, d))
+    assert torch.all((lse.double() / want - 1).abs() <= 6 * 2.0 ** -24)
+    if T == 1:
+        ref = c.mass.double()
+        for b in range(2):
+            ref[b, :len(pages[b]) - 1] *= 0.5
+            ref[b, best[b] // 16] += H
+        within(mass.double(), ref, H * 2.0 ** -19 * (ref > 0.0), "mass")     # (log2 of sums up to 2^16, to 2^-20 each)
+
+
+@pytest.mark.parametrize("dtype,d,G,H,T", FORMS)
+@pytest.mark.parametrize("score", [0.0, 5.0 * 2.0 ** 10, -5.0 * 2.0 ** 19, 5.0 * 2.0 ** 19, 5.0 * 2.0 ** 22, -5.0 * 2.0 ** 22, 5.0 * 2.0 ** 26, -5.0 * 2.0 ** 40, 5.0 * 2.0 ** 100])
+def test_equal_scores_share(B, dtype, d, G, H, T, score):  # noqa: F811
+    """Slots that share the highest score, in pages whose values have other scales, share the weight evenly whatever the score is; the others are
+    too far below to count, or there are none (score 0).  A weight is rounded to 11 bits (fp32 outputs: 22), its sum to fp32."""
+    lens = [1000, 333]
+    pages, n = table(lens, 16, np.random.default_rng(6), spare=1)
+    c = R.make_pool(G, d, 16, n, pages, lens, dtype, 42)
+    c.k[:], c.ks[:] = 0, 1.0
+    c.vs = torch.exp2(torch.randint(-9, 3, (n, G), generator=torch.Generator().manual_seed(1)).float())
+    one, two = R.encode(torch.tensor([1.0, 2.0], dtype=torch.float64)) + (128 if score < 0 else 0)
+    c.k[:, :, :, 0] = two if score < 0 else one
+    tops = [[0, 5, 16, 300, 301, 640, 900], [3, 100, 200]]
+    for b in range(2):
+        for s in tops[b]:
+            c.k[pages[b][s // 16], :, s % 16, 0] = one if score < 0 else two
+    if score == 0.0:
+        tops = [list(range(lens[b])) for b in range(2)]
+    q = torch.zeros(2 * T, H, d, dtype=dtype)
+    q[:, :, 0] = abs(score)
+    best = abs(score) * (-1.0 if score < 0 else 2.0)
+    out, lse, mass = run(B, c, H, q, [T, T], lam=0.5 if T == 1 else 0.0)
+    p_err = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -21
+    ref_mass = c.mass.double()
+    for b in range(2):
+        for t in range(T):
+            seen = [s for s in tops[b] if s <= lens[b] - T + t]
+            p = torch.tensor([pages[b][s // 16] for s in seen])
+            v = R.decode(c.v[p, :, torch.tensor([s % 16 for s in seen])]) * c.vs[p].double()[..., None]
+            ref, size = (x.mean(0).repeat_interleave(H // G, 0) for x in (v, v.abs()))
+            within(out[b * T + t].double(), ref, EPS[dtype] * ref.abs() + p_err * size + 2.0 ** -30 * v.abs().max(), "out of row %d" % t)
+            norm = best + math.log(len(seen))
+            assert torch.all((lse[b * T + t].double() - norm).abs() <= 6 * 2.0 ** -24 * abs(norm) + 2.0 ** -20), (t, lse[b * T + t], norm)
+        ref_mass[b, :len(pages[b]) - 1] *= 0.5
+        for s in seen:
+            ref_mass[b, s // 16] += H / len(seen)
+    if T == 1:
+        within(mass.double(), ref_mass, 2.0 ** -18 * ref_mass.abs(), "mass")     # (the same, and its sums' roundings)
+
+
+@pytest.mark.parametrize("dtype,d,G,H,T", FORMS)
+def test_rows_of_all_sizes_side_by_side(B, dtype, d, G, H, T):  # noqa: F811
+    """Heads whose scores are zero, some hundreds, thousands, 2^22, 2^30 and as far below zero share waves; each is what it is by itself.  Scores are exact
+    products, equal or far apart."""
+    lens = [700, 90]
+    pages, n = table(lens, 32, np.random.default_rng(9), spare=1)
+    c = R.make_pool(G, d, 32, n, pages, lens, dtype, 46)
+    used = c.k[..., 0] != 127
+    c.ks[:] = 1.0
+    c.k[:] = 0
+    c.k[..., 0] = R.encode((torch.rand(n, G, 32, generator=torch.Generator().manual_seed(1)) < 0.05).double() + 1.0)
+    c.k[~used] = 127
+    size = torch.tensor([0.0, 320.0, -320.0, 5120.0, -5120.0, 5.0 * 2 ** 22, -5.0 * 2 ** 22, 5.0 * 2 ** 30])
+    q = torch.zeros(2 * T, H, d, dtype=dtype)
+    q[:, :, 0] = (size[torch.arange(2 * T * H) % 8]).view(2 * T, H)
+    if dtype == torch.bfloat16:
+        assert torch.equal(q[:, :, 0].flatten()[:8].float(), size)
+    lam = 0.5 if T == 1 else 0.0
+    out, lse, mass = run(B, c, H, q, [T, T], lam=lam)
+    ref, ref_lse, ref_mass, size, top = R.attend(c, H, q, [0, T, 2 * T], 1.0, 0.0, lam)
+    p_err = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -21
+    within(out.double(), ref, EPS[dtype] * ref.abs() + p_err * size + 700 * 2.0 ** -31 * top, "out")
+    within(lse.double(), ref_lse, 6 * 2.0 ** -24 * ref_lse.abs() + 2.0 ** -20, "lse")
+    within(mass.double(), ref_mass, 2.0 ** -12 * ref_mass.abs(), "mass")      # (norms of up to 2^10 are taken off as one number: 2^-14 each, and log2's)
+
+
+@pytest.mark.parametrize("G,H,n", [(128, 128, 70000), (64, 512, 36000)])
+@pytest.mark.parametrize("score", [5.0 * 2.0 ** 11, -5.0 * 2.0 ** 26])
+def test_large_scores_of_long_shares(B, G, H, n, score):  # noqa: F811
+    """Waves that see more blocks than have room for their weights at once, the highest scores among the first, the last and some between."""
+    d, ps = 16, 64
+    per = -(-n // ps)
+    pages = np.random.default_rng(3).permutation(per + 2)[:per].tolist()
+    one, two = R.encode(torch.tensor([1.0, 2.0], dtype=torch.float64)) + (128 if score < 0 else 0)
+    k = torch.zeros(per + 2, G, ps, d, dtype=torch.uint8)
+    k[..., 0] = two if score < 0 else one
+    tops = [1, 2, 5000, 5001, 17777, 30000, n - 1]
+    c = R.make_pool(1, 16, 16, 1, [[0]], [0], torch.bfloat16, 1)
+    c.G, c.d, c.ps, c.n_pages, c.lens, c.pages = G, d, ps, per + 2, [n], torch.tensor([pages], dtype=torch.int32)
+    for s in tops:
+        k[pages[s // ps], :, s % ps, 0] = one if score < 0 else two
+    c.k, c.v = k, torch.full_like(k, int(one) & 127)
+    c.ks, c.vs, c.mass = torch.ones(per + 2, G), torch.exp2(torch.arange(per + 2) % 7 - 3.0)[:, None].repeat(1, G), torch.zeros(1, per)
+    q = torch.zeros(1, H, d, dtype=torch.bfloat16)
+    q[:, :, 0] = abs(score)
+    out, lse, mass = run(B, c, H, q, [1], lam=1.0)
+    want = float(np.mean([float(c.vs[pages[s // ps], 0]) for s in tops]))
+    assert torch.all((out.double() / want - 1).abs() <= 2.0 ** -8 + 2.0 ** -11)
+    ref = torch.zeros(1, per, dtype=torch.float64)
+    for s in tops:
+        ref[0, s // ps] += H / len(tops)
+    within(mass.double(), ref, 2.0 ** -18 * ref, "mass")
