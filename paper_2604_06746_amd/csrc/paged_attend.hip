@@ -32,6 +32,10 @@ constexpr float kTop = 15.f, kFresh = 7.f;
 // more than an exponent bears.  The wave then takes its blocks once more (CARE), by scores rounded once and references in two parts: N, the highest score,
 // and L, a small number that has the values' scales: w = 2^((y - N) + (log2 s_v - L)).
 constexpr float kHuge = 8388608.f;
+// A weight has its value's scale, and its share of the norm is taken without it again; beside values of 2^100 as much that is nothing for weights
+// that count.  So a wave that meets scales on both sides of these takes its blocks with care too, the norm's shares by exponents of their own.  (Within them what is
+// lost is below 2^-49 of the norm.)
+constexpr float kTinyScale = 0x1p-20f, kLargeScale = 0x1p12f;
 
 // ONCE: past the caches
 template <int N, bool ONCE> __device__ __forceinline__ void load_bytes(uint32_t (&to)[N / 4], const uint8_t* p) {
@@ -175,6 +179,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
   constexpr bool F32 = std::is_same<T, float>::value;
   constexpr int QP = F32 ? 3 : 1, PP = F32 ? 2 : 1, KP = DP / 64, W = DP / 16;
   constexpr bool AHEAD = DP <= 128 && (RB == 1 || !F32);   // (the others have no registers for it)
+  constexpr bool TIGHT = F32 && DP > 128;   // places are worked out where they are used, which takes fewer registers
   constexpr bool SAVE = HELD > 0;
   constexpr int kBatch = 64, kPitch = HELD * kBatch + 1;
   static_assert(!SAVE || (16 / (SAVE ? HELD : 1)) * kPitch <= 16 * (DP + 4), "the blocks' weights lie where the waves' sums come later");
@@ -210,6 +215,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
   }
   const Cap cap(f, CAPPED ? kLog2e : 1.f);
   bool again = false;   // the blocks are to be taken with care
+  bool tiny = false, large = false;
   bool huge = false;    // the references are in `parts`, and M is 0
   int odd = 0x7FFFFFFF;   // the first fresh slot behind the first one whose values are not all numbers
 
@@ -217,26 +223,33 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
   const int share = ((last - first + 2 * WAVES - 1) / (2 * WAVES)) * 2;
   const int mine0 = first + wave * share, mine1 = min(last, mine0 + share);
   // A lane's block of the batch that is being fetched: place and scales
-  float ks = 1.f, vs = 1.f, kf = 0.f, lv = 0.f, iv = 0.f;
+  float kf = 0.f, lv = 0.f, iv = 0.f;
   int64_t off = 0;
   uint64_t todo = 0;
   int next = mine0, base = mine0;
   // What a lane reads of a block.  In the place of components behind the last one it reads the first: queries have zeros there, and nobody
   // asks for those of the result.
+  auto key_at = [&](int i, uint32_t part) __attribute__((always_inline)) { return (uint32_t)(l16 * c.st) + (64 * i + part < (uint32_t)c.d ? 64 * i + part : 0); };
   uint32_t k_at[KP], v_at[4];
 #pragma unroll
-  for (int i = 0; i < KP; ++i) k_at[i] = (uint32_t)(l16 * c.st) + (64 * i + 16 * q4 < c.d ? 64 * i + 16 * q4 : 0);
+  for (int i = 0; i < KP; ++i) k_at[i] = key_at(i, 16 * q4);
 #pragma unroll
   for (int i = 0; i < 4; ++i) v_at[i] = (uint32_t)((4 * q4 + i) * c.st) + (W * l16 < c.d ? W * l16 : 0);
+  auto take_again = [&]() __attribute__((always_inline)) {   // (what the usual loop still does comes to nothing)
+    again = true;
+    todo = 0;
+    next = mine1;
+  };
   auto fetch = [&](Pair<DP>& x) __attribute__((always_inline)) {
-    bool turned = false;   // to another batch
+    bool turned = false, live = false;   // to another batch; the lane's block is there
+    float ks = 1.f, vs = 1.f;
     while (todo == 0 && next < mine1) {
       turned = true;
       base = next;
       next += kBatch;
       const int block = base + lane;
       const int page = block < mine1 ? c.pages[p.b * c.pst + (block >> lb)] : -1;
-      const bool live = (uint32_t)page < (uint32_t)c.n_pages;
+      live = (uint32_t)page < (uint32_t)c.n_pages;
       const int64_t at = (int64_t)(live ? page : 0) * c.G + p.g;
       ks = c.k_scale[at];
       vs = c.v_scale[at];
@@ -259,15 +272,18 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
       const int64_t place = there ? (int64_t)((uint64_t)hi << 32 | lo) + p.g * c.sh : 0;
       const uint8_t *kp = c.k + place, *vp = c.v + place;
 #pragma unroll
-      for (int i = 0; i < KP; ++i) load_bytes<16, ONCE>(x.k[kb][i], kp + in_place(k_at[i] & mask));
+      for (int i = 0; i < KP; ++i) load_bytes<16, ONCE>(x.k[kb][i], kp + in_place((TIGHT ? key_at(i, in_place(16 * q4)) : k_at[i]) & mask));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load_bytes<W, ONCE>(x.v[kb][i], vp + in_place(v_at[i] & mask));
+      for (int i = 0; i < 4; ++i) load_bytes<W, ONCE>(x.v[kb][i], vp + in_place((TIGHT ? in_place(v_at[0]) + i * (uint32_t)c.st : v_at[i]) & mask));
     }
     if (turned) {   // (the scales come while the codes are on their way)
       kf = CAPPED ? ks : ks * f.c2;
       const float vc = fminf(fmaxf(vs, kLeastScale), kMostScale);
       lv = __builtin_amdgcn_logf(vc);
       iv = 1.f / vc;
+      tiny |= __any(live && vc < kTinyScale);
+      large |= __any(live && vc > kLargeScale);
+      if (tiny && large && !again) take_again();
     }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -439,11 +455,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
           step[rb] = M[rb] - Mn[rb];
         }
         far = __any(far);
-        if (!CARE && far) {   // (what the usual loop still does comes to nothing)
-          again = true;
-          todo = 0;
-          next = mine1;
-        }
+        if (!CARE && far) take_again();
         if (CARE) huge = far;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -457,8 +469,8 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
       if (CARE && huge) to_exponents(y, f2, lv, step);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const float shrink = __builtin_amdgcn_exp2f(step[rb]);
-        Z[rb] *= shrink;
+        const float shrink = __builtin_amdgcn_exp2f(step[rb]), least = fmaxf(step[rb], -4096.f), whole = rintf(least);
+        Z[rb] = ldexpf(CARE ? Z[rb] * __builtin_amdgcn_exp2f(least - whole) : Z[rb], (int)whole);   // (may be far above the weights, whose own shrinks to nothing)
 #pragma unroll
         for (int j = 0; j < W; ++j) O[j][rb] *= shrink;
         if (SAVE && CARE) shift_held(step[rb]);
@@ -475,10 +487,14 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
       for (int rb = 0; rb < RB; ++rb) {
         const float m = lv[kb] - M[rb];
         float z = 0.f;
+        if (CARE) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z += __builtin_amdgcn_exp2f(fmaf(y[kb][rb][e], f2[kb], m - x.lv[kb]));
+        }
 #pragma unroll
         for (int e = 0; e < 4; e += 2) {
           const floatx2 pr = {__builtin_amdgcn_exp2f(fmaf(y[kb][rb][e], f2[kb], m)), __builtin_amdgcn_exp2f(fmaf(y[kb][rb][e + 1], f2[kb], m))};
-          z += pr[0] + pr[1];
+          if (!CARE) z += pr[0] + pr[1];
           floatx2 rest = pr;
 #pragma unroll
           for (int part = 0; part < PP; ++part) {
@@ -488,9 +504,9 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
             rest = floatx2{rest[0] - (float)r[0], rest[1] - (float)r[1]};
           }
         }
-        Z[rb] = fmaf(z, x.iv[kb], Z[rb]);
+        Z[rb] = CARE ? Z[rb] + z : fmaf(z, x.iv[kb], Z[rb]);
         if (SAVE) {
-          z = row_total(z * x.iv[kb]);
+          z = row_total(CARE ? z : z * x.iv[kb]);
           if (lane < some && (kb ? x.two : x.any)) held[l16 * kPitch + x.base - held_base + x.at[kb]] = __builtin_amdgcn_logf(z) + (CARE ? 0.f : M[0]);
         }
       }

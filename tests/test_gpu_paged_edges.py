@@ -149,3 +149,50 @@ def test_large_scores_of_long_shares(B, G, H, n, score):  # noqa: F811
     for s in tops:
         ref[0, s // ps] += H / len(tops)
     within(mass.double(), ref, 2.0 ** -18 * ref, "mass")
+
+
+@pytest.mark.parametrize("dtype,d,G,H,T", FORMS)
+@pytest.mark.parametrize("lens", [[1300, 700], [300, 90]])
+@pytest.mark.parametrize("high", [11, 12, 13, 40, 64])
+def test_value_scales_far_apart(B, dtype, d, G, H, T, lens, high):  # noqa: F811
+    """The weight of a page whose values are zeros (scale 2^-64, as they are stored) or tiny, beside pages of 2^11 to 2^64: lse and mass do not depend on
+    the values' scales at all, out is what the large ones make of their share.  Scores of a few units."""
+    pages, n = table(lens, 16, np.random.default_rng(7), spare=1)
+    for kind in ("zeros", "tiny", "few"):
+        c = R.make_pool(G, d, 16, n, pages, lens, dtype, 43)
+        g = torch.Generator().manual_seed(2)
+        small = torch.rand(n, G, generator=g) < (0.03 if kind == "few" else 0.5)
+        c.vs = torch.where(small, 2.0 ** -64, 2.0 ** high)
+        if kind == "zeros":
+            c.v[small & (c.v != 127).all(3).all(2)] = 0
+        flat = OnGpu(B, c)
+        flat.vs.fill_(2.0 ** -3)
+        q = torch.randn(2 * T, H, d, generator=g).to(dtype)
+        res = [run(B, c, H, q, [T, T], scale=0.0, lam=0.5 if T == 1 else 0.0, on=on) for on in (None, flat)]
+        (out, lse, mass), (_, want_lse, want_mass) = res
+        ref, _, _, size, top = R.attend(c, H, q, cut([T, T]))
+        # the same sums in other units: their roundings, and a log2 to 2^-20
+        within(lse.double(), want_lse.double(), 2.0 ** -18 + 2.0 ** -22 * want_lse.abs().double(), "lse")
+        within(mass.double(), want_mass.double(), 2.0 ** -18 * want_mass.abs().double(), "mass")
+        # scores of d terms of magnitude up to |q| |k|, as in test_gpu_paged.py; what tiny values add is below the last bits of the others'
+        keys = (R.decode(c.k).nan_to_num(0.0) * c.ks[:, :, None, None]).norm(dim=3).max()
+        a_err = 2 * float(d * keys * q.double().norm(dim=2).max() / math.sqrt(d) + 512) * 2.0 ** -24 + (max(lens) / 16 + 64) * 2.0 ** -24
+        p_err = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -22
+        within(out.double(), ref, EPS[dtype] * ref.abs() + (2 * a_err + p_err) * size + max(lens) * 2.0 ** -31 * top, "out")
+
+
+def test_a_page_of_zeros_weighs_what_it_weighs(B):  # noqa: F811
+    """Stored by append: zeros in the values of one page, 2^70 in another's, scores all equal: half the weight is each one's."""
+    dtype, d = torch.float32, 64
+    for order in (0, 1):
+        c = R.make_pool(1, d, 16, 4, [[1, 2]], [0], dtype, 1)
+        on = OnGpu(B, c)
+        v = torch.zeros(1, 32, d)
+        v[:, 16 * order:16 * order + 16] = 2.0 ** 70
+        B.structkv_paged_append(on.handle, torch.ones(1, 32, d).cuda(), v.cuda(), [0, 32], on.lens_out)
+        assert on.lens_out.tolist() == [32] and on.vs.cpu().flatten()[1 + (1 - order)] == 2.0 ** -64
+        on.handle = B.make_paged(on.k, on.v, on.ks, on.vs, on.pages, on.lens_out, dtype, on.mass, on.missed)
+        on.mass.zero_()
+        out, lse, mass = run(B, c, 1, torch.zeros(1, 1, d), [1], lam=1.0, on=on)
+        assert torch.all((out / 2.0 ** 69 - 1).abs() <= 2.0 ** -21), out       # (the mean: half of 2^70)
+        assert abs(float(lse) - math.log(32.0)) <= 2.0 ** -20 and torch.all((mass[0, :2] - 0.5).abs() <= 2.0 ** -19), (lse, mass)
