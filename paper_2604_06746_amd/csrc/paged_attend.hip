@@ -573,6 +573,31 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
       put_held(usual);
     }
   }
+  // Fresh slots behind the first that all rows see were not looked at: a NaN among their values has left one in the sums, and then it is looked for.
+  // (In each pair of blocks that holds some it would cost a sixth of a prompt's first chunk.)
+  const int seen0 = max(h.base + 1, mine0 * kBlock), seen1 = min(edge, mine1 * kBlock);
+  if (!SAVE && seen0 < seen1) {
+    float sum = 0.f;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum = fmaf(O[j][rb][e], 0.f, sum);
+    if (__any(sum != sum))
+      for (int block = seen0 / kBlock; block * kBlock < seen1; ++block) {
+        const int page = c.pages[p.b * c.pst + (block >> lb)];
+        if ((uint32_t)page >= (uint32_t)c.n_pages) continue;
+        const uint8_t* vp = c.v + page * c.sp + p.g * c.sh + (int64_t)((block & ((1 << lb) - 1)) * kBlock) * c.st;
+        for (int i = 0; i < 4; ++i) {
+          uint32_t v[W / 4];
+          load_bytes<W, false>(v, vp + (uint32_t)(v_at[0] + i * c.st));
+          const int s = block * kBlock + 4 * q4 + i;
+          for (int j = 0; j < W / 4; ++j)
+            if ((((v[j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) && s >= seen0 && s < seen1) odd = min(odd, s);
+        }
+      }
+  }
   if (__any(odd != 0x7FFFFFFF)) {
     for (int m = 32; m; m >>= 1) odd = min(odd, __shfl_xor(odd, m));
 #pragma unroll

@@ -196,3 +196,42 @@ def test_a_page_of_zeros_weighs_what_it_weighs(B):  # noqa: F811
         out, lse, mass = run(B, c, 1, torch.zeros(1, 1, d), [1], lam=1.0, on=on)
         assert torch.all((out / 2.0 ** 69 - 1).abs() <= 2.0 ** -21), out       # (the mean: half of 2^70)
         assert abs(float(lse) - math.log(32.0)) <= 2.0 ** -20 and torch.all((mass[0, :2] - 0.5).abs() <= 2.0 ** -19), (lse, mass)
+
+
+@pytest.mark.parametrize("dtype,d,G,H,lens,T", [(torch.bfloat16, 128, 2, 8, [70, 300], 64), (torch.bfloat16, 64, 1, 2, [100, 100], 100), (torch.float32, 128, 2, 4, [90, 700], 90),
+                                                (torch.float32, 256, 1, 8, [40, 77], 33), (torch.bfloat16, 128, 1, 16, [1300, 40], 40)])
+@pytest.mark.parametrize("at", [0, 1, 3, 17, 30])
+def test_values_that_are_not_numbers_in_a_chunk(B, dtype, d, G, H, lens, T, at):  # noqa: F811
+    """A fresh slot behind the first whose value has a NaN: every row that sees it gets NaN throughout, in whichever block of rows it is; the first
+    fresh slot's NaN (at = 0), and an older one's, stay in their component.  Rows that do not see it, and other KV heads' heads, are as without it."""
+    pages, n = table(lens, 16, np.random.default_rng(4), spare=1)
+    for b in range(2):
+        for s, fresh in ((lens[b] - T + at, at > 0), (3, False)):
+            if s == 3 and lens[b] - T <= 3:      # (that would be a fresh one)
+                continue
+            c, clean = (R.make_pool(G, d, 16, n, pages, lens, dtype, 4) for _ in range(2))
+            c.v[pages[b][s // 16], G - 1, s % 16, 5] = 127
+            q = torch.randn(2 * T, H, d, generator=torch.Generator().manual_seed(9)).to(dtype)
+            (out, lse, _), (want, want_lse, _) = (run(B, x, H, q, [T, T], scale=0.0) for x in (c, clean))
+            assert torch.equal(lse, want_lse)
+            sees = torch.zeros(2 * T, dtype=torch.bool)
+            sees[b * T + max(0, s - (lens[b] - T)):(b + 1) * T] = True
+            hit = torch.zeros_like(out, dtype=torch.bool)
+            heads = slice(H // G * (G - 1), H)
+            hit[sees, heads] = fresh
+            hit[sees, heads, 5] = True
+            assert torch.equal(out.isnan(), hit), (b, s)
+            assert torch.equal(out[~hit], want[~hit])
+
+
+def test_not_numbers_beside_dropped_pages(B):  # noqa: F811
+    """Two fresh NaN slots, one of them in a dropped page: that one reaches nobody."""
+    lens, T, d, H = [200], 60, 64, 4
+    pages, n = table(lens, 16, np.random.default_rng(4), spare=1)
+    c, clean = (R.make_pool(1, d, 16, n, pages, lens, torch.bfloat16, 4) for _ in range(2))
+    for s in (150, 180):
+        c.v[pages[0][s // 16], 0, s % 16, 7] = 127
+    c.pages[0, 150 // 16] = clean.pages[0, 150 // 16] = -1
+    q = torch.randn(T, H, d, generator=torch.Generator().manual_seed(9)).bfloat16()
+    (out, lse, _), (want, want_lse, _) = (run(B, x, H, q, [T], scale=0.0) for x in (c, clean))
+    assert torch.equal(lse, want_lse) and torch.equal(out[:40], want[:40]) and bool(out[40:].isnan().all())
