@@ -543,8 +543,8 @@ structkv_status structkv_paged_append(const structkv_paged* cache, const void* k
  *   mass[b][j] = lambda * mass[b][j] + sum over the page's slots and all query heads of a_s     (0 for a dropped page)
  * lambda = 0: mass stays as it is.  A row whose norm is NaN makes the mass of the pages that it sees NaN.
  * q: element (r, h, c) at r*q_stride_tok + h*q_stride_head + c; out [new][H_q][d] contiguous, and not overlapping q; lse_out [new][H_q] fp32.
- * scale, softcap: as in structkv_cache_attend.  A sequence with lens[b] < T_b or missed[b] != 0 is one whose rows see nothing, and
- * whose mass stays as it is.  Deterministic: the same call on the same lengths and table gives the same bits.
+ * scale, softcap: as in structkv_cache_attend; scale at most 2^62 without a softcap.  A sequence with lens[b] < T_b or missed[b] != 0 is
+ * one whose rows see nothing, and whose mass stays as it is.  Deterministic: the same call on the same lengths and table gives the same bits.
  */
 structkv_status structkv_paged_attend(const structkv_paged* cache, int32_t n_q_heads, float scale, float softcap, const void* q,
                                       int64_t q_stride_tok, int64_t q_stride_head, const int64_t* cu_new, float lambda, void* out,

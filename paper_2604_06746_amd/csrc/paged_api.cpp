@@ -10,6 +10,8 @@ namespace skv {
 namespace {
 
 constexpr int kMostHeads = 4096;
+// scale log2(e) is multiplied by a page's scale (2^64 at most) before it meets a product
+constexpr float kMostScoreScale = 0x1p62f;
 
 int bytes_of(int dtype) { return dtype == STRUCTKV_DTYPE_BF16 ? 2 : 4; }
 
@@ -312,6 +314,7 @@ structkv_status structkv_paged_attend(const structkv_paged* cache, int32_t n_q_h
   const float s = scale > 0.f ? scale : 1.0f / std::sqrt((float)cache->head_dim);
   if (softcap > 0.f && (!std::isfinite(1.f / softcap) || !std::isfinite(2.f * softcap) || !std::isfinite(s / softcap * 4.f) || !std::isnormal(s / softcap)))
     return fail(STRUCTKV_ERR_UNSUPPORTED, "softcap, 1 / softcap or scale / softcap leaves fp32's range");
+  if (softcap == 0.f && !(s <= kMostScoreScale)) return fail(STRUCTKV_ERR_UNSUPPORTED, "a scale beyond 2^62 leaves fp32's range where a page's largest comes to it");
   if (!(lambda >= 0.f && lambda <= 1.f)) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda must be in [0,1]");
   if (lambda > 0.f && !cache->mass) return fail(STRUCTKV_ERR_INVALID_ARG, "lambda > 0 needs the cache's mass");
   const uintptr_t e = bytes_of(cache->dtype);

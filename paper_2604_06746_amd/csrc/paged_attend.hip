@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_atten
       for (int i = 0; i < 4; ++i) load_bytes<W, ONCE>(x.v[kb][i], vp + in_place((TIGHT ? in_place(v_at[0]) + i * (uint32_t)c.st : v_at[i]) & mask));
     }
     if (turned) {   // (the scales come while the codes are on their way)
-      kf = CAPPED ? ks : ks * f.c2;
+      kf = CAPPED ? ks : fmaxf(ks * f.c2, 0x1p-149f);   // (not 0, which makes NaN of what is masked)
       const float vc = fminf(fmaxf(vs, kLeastScale), kMostScale);
       lv = __builtin_amdgcn_logf(vc);
       iv = 1.f / vc;

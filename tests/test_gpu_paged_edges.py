@@ -235,3 +235,32 @@ def test_not_numbers_beside_dropped_pages(B):  # noqa: F811
     q = torch.randn(T, H, d, generator=torch.Generator().manual_seed(9)).bfloat16()
     (out, lse, _), (want, want_lse, _) = (run(B, x, H, q, [T], scale=0.0) for x in (c, clean))
     assert torch.equal(lse, want_lse) and torch.equal(out[:40], want[:40]) and bool(out[40:].isnan().all())
+
+
+@pytest.mark.parametrize("dtype,d,G,H,T", FORMS)
+@pytest.mark.parametrize("scale,key_scale", [(1e-30, 2.0 ** -64), (1.2e-38, 1.0), (1e-44, 2.0 ** -20), (1e-18, 2.0 ** -64)])
+def test_scores_next_to_nothing(B, dtype, d, G, H, T, scale, key_scale):  # noqa: F811
+    """scale times a page's scale below fp32's least number: all scores are zero, so a row's result is the mean of the values that it sees."""
+    lens = [300, 41]
+    pages, n = table(lens, 16, np.random.default_rng(8), spare=1)
+    c = R.make_pool(G, d, 16, n, pages, lens, dtype, 44)
+    c.ks[:] = key_scale
+    q = torch.randn(2 * T, H, d, generator=torch.Generator().manual_seed(3)).to(dtype)
+    out, lse, mass = run(B, c, H, q, [min(T, 41), T], scale=scale, lam=0.5 if T == 1 else 0.0)
+    ref, ref_lse, ref_mass, size, top = R.attend(c, H, q, cut([min(T, 41), T]), scale, 0.0, 0.5 if T == 1 else 0.0)
+    p_err = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -22
+    within(lse.double(), ref_lse, 2.0 ** -20 + 0 * ref_lse, "lse")
+    within(out.double(), ref, EPS[dtype] * ref.abs() + (p_err + 2.0 ** -18) * size + 300 * 2.0 ** -31 * top, "out")
+    within(mass.double(), ref_mass, 2.0 ** -18 * ref_mass.abs(), "mass")
+
+
+def test_scale_beyond_fp32(B):  # noqa: F811
+    """A scale that leaves fp32's range where it meets a page's largest is refused; the largest that does not is taken."""
+    c = R.make_pool(1, 64, 16, 4, [[1]], [5], torch.float32, 1)
+    c.ks[:] = 2.0 ** 64
+    q = torch.zeros(1, 1, 64)
+    out, lse, _ = run(B, c, 1, q, [1], scale=2.0 ** 62)
+    assert abs(float(lse) - math.log(5.0)) <= 2.0 ** -20 and bool(out.isfinite().all())
+    with pytest.raises(B.StructKVError) as e:
+        run(B, c, 1, q, [1], scale=2.0 ** 63)
+    assert e.value.status == B.STRUCTKV_ERR_UNSUPPORTED
