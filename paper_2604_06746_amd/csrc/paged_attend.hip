@@ -101,8 +101,10 @@ __device__ __forceinline__ void load_query(bf16x8 (&q)[QP], const T* row, int c,
       float rest = x[i];
 #pragma unroll
       for (int part = 0; part < QP; ++part) {
-        q[part][i] = (__bf16)rest;
-        rest -= (float)q[part][i];
+        // (cut off: to the nearest, the largest numbers would become infinity)
+        const uint32_t bits = __float_as_uint(rest) & 0xFFFF0000u;
+        q[part][i] = __builtin_bit_cast(__bf16, (uint16_t)(bits >> 16));
+        rest -= __uint_as_float(bits);
       }
     }
   }

@@ -264,3 +264,24 @@ def test_scale_beyond_fp32(B):  # noqa: F811
     with pytest.raises(B.StructKVError) as e:
         run(B, c, 1, q, [1], scale=2.0 ** 63)
     assert e.value.status == B.STRUCTKV_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("value", [3.4028234e38, -3.4e38, 3.39e38, 2.0 ** 100 * 1.99999, 1.1754944e-38 * 3])
+def test_queries_at_the_ends_of_fp32(B, value):  # noqa: F811
+    """fp32 queries next to the largest number, which bf16 parts that are rounded to the nearest do not hold: scores of a few units."""
+    dtype, d, H, lens = torch.float32, 64, 4, [100, 33]
+    pages, n = table(lens, 16, np.random.default_rng(8), spare=1)
+    c = R.make_pool(1, d, 16, n, pages, lens, dtype, 45)
+    k = R.decode(c.k)
+    c.k = R.encode(torch.where(torch.arange(d) == 0, (k / 512).clamp(-0.7, 0.7), 0.0 * k).nan_to_num(0.0))      # (products that stay in range)
+    c.ks[:] = 2.0 ** -6
+    q = torch.zeros(2, H, d)
+    q[..., 0] = value * torch.tensor([1.0, 0.75, 0.9999999, 1.0])
+    scale = float(min(2.0 ** 62, 2.0 ** 8 / abs(value)))
+    out, lse, mass = run(B, c, H, q, [1, 1], scale=scale, lam=0.5)
+    ref, ref_lse, ref_mass, size, top = R.attend(c, H, q, [0, 1, 2], scale, 0.0, 0.5)
+    assert scale == 2.0 ** 62 or float(ref_lse.abs().max()) > 3.0
+    # one product a score: roundings of it, of its scale and of the sums
+    within(lse.double(), ref_lse, 2.0 ** -19 + 0 * ref_lse, "lse")
+    within(out.double(), ref, 2.0 ** -24 * ref.abs() + 2.0 ** -18 * size + 2.0 ** -24 * top, "out")
+    within(mass.double(), ref_mass, 2.0 ** -17 * ref_mass.abs(), "mass")
