@@ -141,8 +141,10 @@ structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, Ca
   p->waves = whole ? kShortWaves : kAttendWaves;
   p->units = whole ? blocks : std::max(blocks, std::min(chunks, std::max(kUnits / G, cut ? 2 * blocks : 0)));
   const int64_t gathers = gather ? v.batch * ceil_div(block_slots(v), 64) + (int64_t)t->cu_new[v.batch] * H : 0;
-  if (p->units * G >= ((int64_t)1 << 31) || gathers >= ((int64_t)1 << 31)) return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
   p->join = gather || p->units > blocks;
+  // (a launch takes fewer than 2^32 threads; the second one has a workgroup of 256 for each row at most, and for what it gathers)
+  const int64_t joins = p->join ? std::max(gathers, (int64_t)t->cu_new[v.batch] * H) : 0;
+  if (p->units * G * 64 * p->waves >> 32 || joins * 256 >> 32) return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
   const int64_t each = std::max<int64_t>(p->min_chunk, ceil_div(cap * blocks, std::max<int64_t>(1, p->units)));
   p->most_chunks = blocks > 0 ? ceil_div(cap, each) : 0;
   const int64_t part = p->join ? p->units * G * p->rows : 0;
@@ -238,9 +240,7 @@ structkv_status structkv_rotate(const structkv_rotary* rotary, const void* x, in
   if (!lie_apart(head_dim, tokens, out_stride_tok, n_heads, out_stride_head, 1, 0)) return fail(STRUCTKV_ERR_INVALID_ARG, "rows of out overlap");
   if (x == out && ((x_stride_tok != out_stride_tok && tokens > 1) || (x_stride_head != out_stride_head && n_heads > 1)))
     return fail(STRUCTKV_ERR_INVALID_ARG, "out is x, but its strides are others");
-  // (units of four components at least)
-  if (tokens >= ((int64_t)1 << 40) || ceil_div(tokens * ceil_div(head_dim, 4), 256) >= ((int64_t)1 << 31) || n_heads > 65535)
-    return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows for one launch");
+  if (tokens >= ((int64_t)1 << 35) || n_heads > 65535) return fail(STRUCTKV_ERR_UNSUPPORTED, "2^35 rows or more, or more than 65535 heads");
   SKV_HIP_CHECK(launch_rotate(r, x, x_stride_tok, x_stride_head, tokens, n_heads, head_dim, dtype == STRUCTKV_DTYPE_BF16, pos, out,
                               out_stride_tok, out_stride_head, (hipStream_t)stream));
   return STRUCTKV_OK;
@@ -288,14 +288,16 @@ structkv_status structkv_paged_append(const structkv_paged* cache, const void* k
     int64_t most = 0;
     for (int b = 0; b < cache->batch; ++b) most = std::max<int64_t>(most, t.cu_new[b + 1] - t.cu_new[b]);
     const int64_t pages = (most + cache->page_size - 2) / cache->page_size + 1;
-    // (the queries' workgroups: fewer than 2^24, unless a thread takes all heads of a token's unit)
+    // (numbers that fit what the launch counts them in, the queries' workgroups fewer than 2^24, unless a thread takes all heads of a token's unit)
     if ((q && total * upr >= ((int64_t)1 << 31) - ((int64_t)1 << 24)) ||
         ((int64_t)1 << 25) + (q ? total * upr / 64 : 0) + (int64_t)cache->batch * pages * 2 * cache->n_kv_heads >= ((int64_t)1 << 31))
       return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows for one launch");
   }
   const PagedRows w = {k_new, v_new, new_stride_head, new_stride_tok, pos_new, r, total > 0 ? q : nullptr, q_stride_tok, q_stride_head, q_out,
                        n_q_heads, lens_out};
-  SKV_HIP_CHECK(launch_paged_append(t, v, w, cache->dtype == STRUCTKV_DTYPE_BF16, (hipStream_t)stream));
+  const hipError_t launched = launch_paged_append(t, v, w, cache->dtype == STRUCTKV_DTYPE_BF16, (hipStream_t)stream);
+  if (launched == hipErrorInvalidConfiguration) return fail(STRUCTKV_ERR_UNSUPPORTED, "too many rows for one launch");
+  SKV_HIP_CHECK(launched);
   return STRUCTKV_OK;
 }
 

@@ -238,6 +238,30 @@ hipError_t launch_paged_append(const CacheTable& t, const PagedView& c, const Pa
   cut.once = 2 * tokens * w.H * c.d * e >= kOnceBytes;
   cut.units = (uint32_t)(tokens * cut.groups * upr);
   const int64_t blocks = cut.pages + ceil_div((int64_t)cut.units, threads);
+  if (blocks * threads >> 32) {   // a launch takes fewer than 2^32 threads: the sequences one by one, which leaves out what is there for the longest one's pages
+    if (t.batch == 1) return hipErrorInvalidConfiguration;
+    for (int b = 0; b < t.batch; ++b) {
+      const int64_t r = t.cu_new[b];
+      CacheTable one = {};
+      one.cu_new[1] = t.cu_new[b + 1] - t.cu_new[b];
+      one.batch = 1;
+      PagedView v = c;
+      v.pages += b * c.pst;
+      v.lens += b;
+      v.missed = c.missed ? c.missed + b : nullptr;
+      v.batch = 1;
+      PagedRows x = w;
+      x.k = (const uint8_t*)w.k + r * w.st * e;
+      x.v = (const uint8_t*)w.v + r * w.st * e;
+      x.pos = w.pos ? w.pos + r : nullptr;
+      x.q = w.q && one.cu_new[1] > 0 ? (const uint8_t*)w.q + r * w.qst * e : nullptr;
+      x.q_out = (uint8_t*)w.q_out + r * w.H * c.d * e;
+      x.lens_out = w.lens_out + b;
+      const hipError_t st1 = launch_paged_append(one, v, x, bf16, st);
+      if (st1 != hipSuccess) return st1;
+    }
+    return hipSuccess;
+  }
   with_fresh_table(t, [&](const auto& tab) {
     using TAB = std::decay_t<decltype(tab)>;
     auto go = [&](auto elem, auto v, auto hold, auto one, auto share) {

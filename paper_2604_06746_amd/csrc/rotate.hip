@@ -12,15 +12,16 @@ namespace {
 // A thread of many heads has four on their way at once: queries of 32 heads, 45720 tokens, 158 -> 140 us (5.4 TB/s); of eight heads it costs
 // (keys of 131072 tokens 92 -> 104 us), and in fp32 (8191 tokens of 32 heads of 80 components 38.2 -> 39.4).
 constexpr int kManyHeads = 16;
+constexpr int64_t kLaunchUnits = (int64_t)1 << 31;
 
 // P: pairs of a unit.  ONCE: past the caches.  AT: heads that are on their way at once.
 template <class T, bool VEC, bool ONCE, int P, int AT>
-__global__ __launch_bounds__(256) void rotate_kernel(RotaryView r, const T* x, int64_t xst, int64_t xsh, int64_t units, int heads, int upr, const int32_t* pos, T* out,
+__global__ __launch_bounds__(256) void rotate_kernel(RotaryView r, const T* x, int64_t xst, int64_t xsh, uint32_t units, int heads, int upr, const int32_t* pos, T* out,
                                                      int64_t ost, int64_t osh, int per) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t e = blockIdx.x * 256 + threadIdx.x;
   if (e >= units) return;
-  const int64_t t = units >> 32 ? e / upr : (int64_t)((uint32_t)e / (uint32_t)upr);
-  const int u = (int)(e - t * upr), h0 = blockIdx.y * per, h1 = min(heads, h0 + per);
+  const int64_t t = e / (uint32_t)upr;
+  const int u = (int)(e - (uint32_t)t * upr), h0 = blockIdx.y * per, h1 = min(heads, h0 + per);
   const Spins<P> w = spin_unit<P>(r, u, pos[t]);
   turn_heads<T, VEC, ONCE, AT, P>(x + t * xst, xsh, out + t * ost, osh, h0, h1, u, r, w);
 }
@@ -35,12 +36,15 @@ hipError_t launch_rotate(const RotaryView& r, const void* x, int64_t xst, int64_
     using T = decltype(elem);
     constexpr int P = decltype(pairs)::value;
     const int upr = (int)ceil_div(d, 2 * P);
-    const int64_t units = tokens * upr;
-    const int per = (int)std::min<int64_t>(heads, std::max<int64_t>(1, units * heads / (1 << 18)));
-    const dim3 grid((unsigned)ceil_div(units, 256), (unsigned)ceil_div(heads, per));
-    auto form = [&](auto at) {
-      rotate_kernel<T, decltype(v)::value, decltype(once)::value, P, decltype(at)::value>
-          <<<grid, 256, 0, st>>>(r, (const T*)x, xst, xsh, units, heads, upr, pos, (T*)out, ost, osh, per);
+    const int per = (int)std::min<int64_t>(heads, std::max<int64_t>(1, std::min(tokens * upr, kLaunchUnits) * heads / (1 << 18)));
+    auto form = [&](auto at) {   // (a launch takes fewer than 2^32 threads)
+      const int64_t most = kLaunchUnits / upr;
+      for (int64_t t = 0; t < tokens; t += most) {
+        const uint32_t units = (uint32_t)(std::min(most, tokens - t) * upr);
+        rotate_kernel<T, decltype(v)::value, decltype(once)::value, P, decltype(at)::value>
+            <<<dim3((unsigned)ceil_div((int64_t)units, 256), (unsigned)ceil_div(heads, per)), 256, 0, st>>>(r, (const T*)x + t * xst, xst, xsh, units, heads, upr, pos + t,
+                                                                                                           (T*)out + t * ost, ost, osh, per);
+      }
     };
     per >= kManyHeads && bf16 ? form(std::integral_constant<int, 4>{}) : form(std::integral_constant<int, 1>{});
   };

@@ -285,3 +285,55 @@ def test_queries_at_the_ends_of_fp32(B, value):  # noqa: F811
     within(lse.double(), ref_lse, 2.0 ** -19 + 0 * ref_lse, "lse")
     within(out.double(), ref, 2.0 ** -24 * ref.abs() + 2.0 ** -18 * size + 2.0 ** -24 * top, "out")
     within(mass.double(), ref_mass, 2.0 ** -17 * ref_mass.abs(), "mass")
+
+
+def test_rotation_of_more_than_one_launch(B):  # noqa: F811
+    """2^32 units of 16 bytes (64 GiB, in place): more threads than a launch may have."""
+    d, tokens, dtype = 65536, (1 << 32) // 8192 + 3, torch.bfloat16
+    row = torch.randn(d, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
+    x = torch.empty(tokens, 1, d, dtype=dtype, device="cuda")
+    x.copy_(row.expand_as(x))
+    pos = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    turns, _ = B.structkv_rotary_turns(64, 500000.0)
+    plan = B.make_rotary(turns.cuda())
+    B.structkv_rotate(plan, x, pos, x)
+    for t in (0, 1, 262143, 262144, 262145, 300001, 524287, 524288, tokens - 1):
+        want = torch.empty(1, 1, d, dtype=dtype, device="cuda")
+        B.structkv_rotate(plan, row[None, None], pos[t:t + 1], want)
+        assert torch.equal(x[t:t + 1], want), t
+    del x
+    torch.cuda.empty_cache()
+
+
+def test_append_of_more_than_one_launch(B):  # noqa: F811
+    """One long prompt among many short sequences: workgroups for as many pages of each would be more than a launch may have."""
+    G, d, ps, batch, long = 8, 16, 16, 64, (1 << 20) + 5
+    fresh = [3] * batch
+    fresh[1], fresh[5] = long, 0
+    total, cu = sum(fresh), cut(fresh)
+    per = -(-(long + 7) // ps)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    n = per + 2 * batch
+    codes = torch.zeros(n, G, ps, d, dtype=torch.uint8, device="cuda")
+    pages = torch.full((batch, per), -1, dtype=torch.int32, device="cuda")
+    pages[1] = torch.randperm(per, generator=g, device="cuda").int()
+    rest = [b for b in range(batch) if b != 1]
+    pages[rest, 0], pages[rest, 1] = (per + torch.arange(i, 2 * batch - 2, 2, device="cuda").int() for i in (0, 1))
+    k, v = (torch.randn(G, total, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(total, G, d, generator=g, device="cuda").bfloat16()
+    turns, _ = B.structkv_rotary_turns(d, 500000.0)
+    plan = B.make_rotary(turns.cuda())
+    lens = torch.tensor([7 + (b % 9) for b in range(batch)], dtype=torch.int32, device="cuda")
+    lens[1] = 2
+    res = []
+    for parts in ([list(range(batch))], [[b] for b in range(batch)]):
+        kc, vc, ks, vs = codes.clone(), codes.clone(), torch.ones(n, G, device="cuda"), torch.ones(n, G, device="cuda")
+        lens_out, missed, q_out = torch.full_like(lens, -1), torch.zeros_like(lens), torch.empty_like(q)
+        for part in parts:
+            s, b = slice(cu[part[0]], cu[part[-1] + 1]), slice(part[0], part[-1] + 1)
+            handle = B.make_paged(kc, vc, ks, vs, pages[b], lens[b], missed=missed[b])
+            B.structkv_paged_append(handle, k[:, s], v[:, s], [x - cu[part[0]] for x in cu[part[0]:part[-1] + 2]], lens_out[b], plan, q=q[s], q_out=q_out[s])
+        res.append((kc, vc, ks, vs, lens_out, missed, q_out.view(torch.int16)))
+    assert torch.equal(res[0][4], lens + torch.tensor(fresh, device="cuda").int()) and not res[0][5].any()
+    for x, y in zip(*res):
+        assert torch.equal(x, y)

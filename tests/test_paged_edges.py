@@ -10,3 +10,28 @@ def test_scales_that_leave_fp32(B):  # noqa: F811
         return B._lib.structkv_paged_attend(ctypes.byref(cache(B)), 8, scale, cap, P, 64, 64, cu, 0.0, P, P, ws, 1 << 40, None)
     assert call(2.0 ** 63) == 2 and "2^62" in B.structkv_last_error()
     assert call(2.0 ** 62) == 3 and call(1e-44) == 3 and call(2.0 ** 63, 2.0 ** 20) == 3     # (taken so far: the workspace is NULL)
+
+
+def test_more_threads_than_a_launch_has(B):  # noqa: F811
+    """Calls whose launches would have 2^32 threads or more are refused before anything touches a GPU."""
+    def append(tokens, **changes):
+        c = cache(B, page_size=16, batch=1, max_pages=1 << 26, pages_stride=1 << 26, **changes)
+        return B._lib.structkv_paged_append(ctypes.byref(c), P, P, 1 << 40, 16, i64(0, tokens), None, None, 0, None, 0, 0, None, Q, None)
+    like = dict(n_kv_heads=64, head_dim=16, stride_tok=16, stride_head=256, stride_page=64 * 256)
+    if not hasattr(B._lib, "structkv_stub_last_attend"):                                      # (the launcher's own check)
+        assert append(1 << 23, **like) == 2, B.structkv_last_error()                          # 2^19 pages, 128 workgroups of 64 threads each
+    c = cache(B, batch=64, head_dim=256, stride_tok=256, stride_head=32 * 256, stride_page=2 * 32 * 256, dtype=0, max_pages=1 << 8, pages_stride=1 << 8)
+    full = i64(*[4096 * b for b in range(65)])
+    def attend(H, cu=full, **changes):
+        for name, value in changes.items():
+            setattr(c, name, value)
+        return B._lib.structkv_paged_attend(ctypes.byref(c), H, 0.0, 0.0, P, H * 256, 256, cu, 0.9 if cu is not full else 0.0, P, P, P, 1 << 60, None)
+    assert attend(64) == 2, B.structkv_last_error()                                           # 2^24 rows to join
+    single = i64(*range(65))
+    assert attend(2, single, max_pages=1 << 24, pages_stride=1 << 24) == 2, B.structkv_last_error()   # 2^25 stretches whose weights are gathered
+
+
+def test_most_rows_of_a_rotation(B):  # noqa: F811
+    def call(tokens, d):
+        return B._lib.structkv_rotate(ctypes.byref(rotary(B, rot_dim=min(d, 64))), P, d, d, tokens, 1, d, 1, P, 0, Q, d, d, None)
+    assert call(1 << 35, 2) == 2 and call(1 << 35, 256) == 2
