@@ -110,6 +110,8 @@ constexpr int64_t kUnits = 512, kLeast = 128;
 constexpr int64_t kLeastRows = 256;
 // Mean slots of a block of rows from which on it is cut in two even where the blocks fill the chip.
 constexpr int64_t kCut = 4096;
+// ... while the rows, each of them a workgroup of 256 threads of the second launch, are no more than a launch takes.
+constexpr int64_t kMostJoined = (int64_t)1 << 23;
 
 // Capacity up to which a workgroup of kShortWaves takes all slots of a sequence where there would be chunks to join: a token over 256 slots 9.3 ->
 // 6.5 us, over 512 9.3 -> 8.5, over 1031 9.7 -> 11.5.
@@ -136,15 +138,14 @@ structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, Ca
     chunks += rcs * std::max<int64_t>(1, ceil_div(cap, least));
     t->units[b + 1] = (int32_t)blocks;
   }
-  const bool cut = p->rows == 16 && cap >= kCut;
+  const bool cut = p->rows == 16 && cap >= kCut && (int64_t)t->cu_new[v.batch] * H < kMostJoined;
   const bool whole = !gather && p->rows == 16 && cap <= kWhole && blocks < std::min(chunks, kUnits / G);
   p->waves = whole ? kShortWaves : kAttendWaves;
   p->units = whole ? blocks : std::max(blocks, std::min(chunks, std::max(kUnits / G, cut ? 2 * blocks : 0)));
   const int64_t gathers = gather ? v.batch * ceil_div(block_slots(v), 64) + (int64_t)t->cu_new[v.batch] * H : 0;
   p->join = gather || p->units > blocks;
-  // (a launch takes fewer than 2^32 threads; the second one has a workgroup of 256 for each row at most, and for what it gathers)
-  const int64_t joins = p->join ? std::max(gathers, (int64_t)t->cu_new[v.batch] * H) : 0;
-  if (p->units * G * 64 * p->waves >> 32 || joins * 256 >> 32) return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
+  // (a launch takes fewer than 2^32 threads)
+  if (p->units * G * 64 * p->waves >> 32 || gathers >> 31) return fail(STRUCTKV_ERR_UNSUPPORTED, "too many workgroups for one launch");
   const int64_t each = std::max<int64_t>(p->min_chunk, ceil_div(cap * blocks, std::max<int64_t>(1, p->units)));
   p->most_chunks = blocks > 0 ? ceil_div(cap, each) : 0;
   const int64_t part = p->join ? p->units * G * p->rows : 0;

@@ -6,6 +6,8 @@
 // those that join the rows, and have the blocks' weights on their way meanwhile.  2081 slots 6.0 us (by two launches 4.3 + 11.2), eight of 64K to 128K 11.
 #include "paged.h"
 
+#include <algorithm>
+
 namespace skv {
 namespace {
 
@@ -37,19 +39,20 @@ __device__ __forceinline__ float wave_total(float x) {
 }
 
 constexpr int kAhead = 8;       // loads of a thread that are on their way at once
+constexpr int64_t kLaunchBlocks = (int64_t)1 << 23;
 constexpr int kStretch = 64;    // blocks whose weights a workgroup gathers: whole pages of any size
 
 template <class TAB, class T, int DP>
-__global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, AttendWork w, int row_blocks) {
+__global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, AttendWork w, int row_blocks, int first_block) {
   short_kernel_priority();
   constexpr int LANES = DP / 4, PARTS = 256 / LANES;
   __shared__ __attribute__((aligned(16))) float sh[256 * 4];
   __shared__ float zs[4];
   extern __shared__ float norms[];   // of the heads: M + log2 Z, and behind them each apart
   PagedUnit* apart_norms = reinterpret_cast<PagedUnit*>(norms + w.H);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if ((int)blockIdx.x < row_blocks) {   // a row: lane groups on shares of its chunks
-    const int r = (int)(blockIdx.x / (uint32_t)w.H), head = (int)blockIdx.x - r * w.H;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, place = first_block + (int)blockIdx.x;
+  if (place < row_blocks) {   // a row: lane groups on shares of its chunks
+    const int r = (int)((uint32_t)place / (uint32_t)w.H), head = place - r * w.H;
     const int b = sequence_of(tab, r);
     const int4 share = w.shares[b];
     const int g = token_of(w, head), mine = head - g * w.gs;   // (a single token's rows are its heads)
@@ -104,7 +107,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, A
   }
   // Blocks i0 .. i0 + 63 of sequence b, one in each lane; a wave takes every fourth head.
   const int lb = c.shift - 4, per = (int)((((int64_t)c.max_pages << lb) + kStretch - 1) / kStretch);
-  const int b = ((int)blockIdx.x - row_blocks) / per, i0 = (((int)blockIdx.x - row_blocks) - b * per) * kStretch;
+  const int b = (place - row_blocks) / per, i0 = (place - row_blocks - b * per) * kStretch;
   const int4 share = w.shares[b];
   const int n = share.w, blocks = (n + kBlock - 1) / kBlock;   // (0 where the fresh token is not there)
   if (tab.cu_new[b + 1] - tab.cu_new[b] != 1 || i0 >= blocks) return;
@@ -193,8 +196,11 @@ hipError_t launch_paged_join(const CacheTable& t, const PagedView& c, const Atte
     with_cache_table(t, [&](const auto& tab) {
       using TAB = std::decay_t<decltype(tab)>;
       const size_t lds = (sizeof(float) + sizeof(PagedUnit)) * w.H;
-      if (bf16) paged_join_kernel<TAB, uint16_t, DP><<<(unsigned)blocks, 256, lds, st>>>(tab, c, w, (int)w.rows);
-      else paged_join_kernel<TAB, float, DP><<<(unsigned)blocks, 256, lds, st>>>(tab, c, w, (int)w.rows);
+      for (int64_t first = 0; first < blocks; first += kLaunchBlocks) {   // (a launch takes fewer than 2^32 threads)
+        const unsigned now = (unsigned)std::min<int64_t>(kLaunchBlocks, blocks - first);
+        if (bf16) paged_join_kernel<TAB, uint16_t, DP><<<now, 256, lds, st>>>(tab, c, w, (int)w.rows, (int)first);
+        else paged_join_kernel<TAB, float, DP><<<now, 256, lds, st>>>(tab, c, w, (int)w.rows, (int)first);
+      }
     });
     return hipGetLastError();
   };

@@ -337,3 +337,30 @@ def test_append_of_more_than_one_launch(B):  # noqa: F811
     assert torch.equal(res[0][4], lens + torch.tensor(fresh, device="cuda").int()) and not res[0][5].any()
     for x, y in zip(*res):
         assert torch.equal(x, y)
+
+
+def test_gathering_over_a_capacity_of_many_launches(B):  # noqa: F811
+    """Stretches of 64 blocks of a capacity that more than 2^24 workgroups would go through: a few tokens in use, the last one's pages at the start."""
+    lens, cap = [40, 3], (1 << 31) - 2048
+    pages, n = table(lens, 256, np.random.default_rng(1))
+    c = R.make_pool(1, 16, 256, n, pages, lens, torch.bfloat16, 3)
+    batch, most = 9, cap // 256
+    on = OnGpu(B, c)
+    whole = torch.full((batch, most), -1, dtype=torch.int32, device="cuda")
+    lens9 = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    for b, to in ((0, 0), (1, 8)):
+        whole[to, :len(pages[b])] = on.pages[b, :len(pages[b])]
+        lens9[to] = lens[b]
+    mass = torch.ones(batch, most, device="cuda")
+    handle = B.make_paged(on.k, on.v, on.ks, on.vs, whole, lens9, torch.bfloat16, mass)
+    q = torch.randn(2, 1, 16, generator=torch.Generator().manual_seed(3)).bfloat16()
+    out, lse = torch.empty(2, 1, 16, dtype=torch.bfloat16, device="cuda"), torch.empty(2, 1, device="cuda")
+    ws = torch.empty(B.structkv_paged_workspace_bytes(handle, 1, 2), dtype=torch.uint8, device="cuda")
+    B.structkv_paged_attend(handle, 1, q.cuda(), [0, 1, 1, 1, 1, 1, 1, 1, 1, 2], out, lse, ws, lam=0.5)
+    want, want_lse, _ = run(B, c, 1, q, [1, 1], scale=0.0, lam=0.5)
+    within(out.cpu().double(), want.double(), 2.0 ** -7 * want.double().abs() + 2.0 ** -10, "out")
+    within(lse.cpu().double(), want_lse.double(), 2.0 ** -18 + 0 * want_lse.double(), "lse")
+    got = mass.cpu()
+    assert abs(float(got[0, 0]) - 1.5) <= 2.0 ** -18 and abs(float(got[8, 0]) - 1.5) <= 2.0 ** -18
+    got[0, 0] = got[8, 0] = 1.0
+    assert torch.all(got == 1.0)

@@ -20,15 +20,10 @@ def test_more_threads_than_a_launch_has(B):  # noqa: F811
     like = dict(n_kv_heads=64, head_dim=16, stride_tok=16, stride_head=256, stride_page=64 * 256)
     if not hasattr(B._lib, "structkv_stub_last_attend"):                                      # (the launcher's own check)
         assert append(1 << 23, **like) == 2, B.structkv_last_error()                          # 2^19 pages, 128 workgroups of 64 threads each
-    c = cache(B, batch=64, head_dim=256, stride_tok=256, stride_head=32 * 256, stride_page=2 * 32 * 256, dtype=0, max_pages=1 << 8, pages_stride=1 << 8)
+    # (4096 tokens of each of 64 sequences, 4096 KV heads: 2^25 workgroups of 256 threads)
+    c = cache(B, batch=64, head_dim=16, n_kv_heads=4096, stride_tok=16, stride_head=32 * 16, stride_page=4096 * 32 * 16)
     full = i64(*[4096 * b for b in range(65)])
-    def attend(H, cu=full, **changes):
-        for name, value in changes.items():
-            setattr(c, name, value)
-        return B._lib.structkv_paged_attend(ctypes.byref(c), H, 0.0, 0.0, P, H * 256, 256, cu, 0.9 if cu is not full else 0.0, P, P, P, 1 << 60, None)
-    assert attend(64) == 2, B.structkv_last_error()                                           # 2^24 rows to join
-    single = i64(*range(65))
-    assert attend(2, single, max_pages=1 << 24, pages_stride=1 << 24) == 2, B.structkv_last_error()   # 2^25 stretches whose weights are gathered
+    assert B._lib.structkv_paged_attend(ctypes.byref(c), 4096, 0.0, 0.0, P, 1 << 16, 16, full, 0.0, P, P, P, 1 << 60, None) == 2, B.structkv_last_error()
 
 
 def test_most_rows_of_a_rotation(B):  # noqa: F811
