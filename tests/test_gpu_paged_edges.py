@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import paged_precision as L
 import paged_reference as R
 from test_gpu_paged import B, EPS, OnGpu, cut, table, within  # noqa: F401  (B is the fixture)
 
@@ -364,3 +365,44 @@ def test_gathering_over_a_capacity_of_many_launches(B):  # noqa: F811
     assert abs(float(got[0, 0]) - 1.5) <= 2.0 ** -18 and abs(float(got[8, 0]) - 1.5) <= 2.0 ** -18
     got[0, 0] = got[8, 0] = 1.0
     assert torch.all(got == 1.0)
+
+
+@pytest.mark.parametrize("d", [16, 64, 80, 128, 256])
+@pytest.mark.parametrize("lens,T", [((500, 90), 3), ((1700, 90), 1), ((1700, 90), 20), ((60, 20), 20)])
+def test_precision_of_fp32(B, d, lens, T):  # noqa: F811
+    """The whole of out and lse against what roundings make of them: all of a query's 24 bits and 22 of the weights' are there."""
+    c, H, q, cu_new, scale = L.case(d, lens, T)
+    out, lse, mass = run(B, c, H, q, [T, T], scale=scale, lam=0.5 if T == 1 else 0.0)
+    ref, ref_lse, out_off, lse_off = L.attend(c, H, q, cu_new, scale)
+    assert L.worst(out, ref, out_off) <= L.MOST and L.worst(lse, ref_lse, lse_off) <= L.MOST
+    if T == 1:      # (weights of all heads to 2^-20: the norm and log2 of the blocks' sums, of numbers up to 32, and back)
+        _, _, ref_mass, _, _ = R.attend(c, H, q, cu_new, scale, 0.0, 0.5)
+        within(mass.double(), ref_mass, 2.0 ** -18 * ref_mass.abs() + H * 2.0 ** -24, "mass")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,H", [(1, 4), (1, 20), (7, 1), (9, 4)])
+@pytest.mark.parametrize("falling", [False, True])
+def test_scores_that_rise_and_rise(B, dtype, T, H, falling):  # noqa: F811
+    """Exact scores from -2^20 to 2^20, page by page (or the other way round), so that the reference is raised again and again; the slots of the highest page
+    are some units apart, and only they count.  Nothing but the weights' and the sums' roundings is left."""
+    lens, ps, d = [640, 640], 16, 64
+    pages, n = table(lens, ps, np.random.default_rng(2))
+    c = R.make_pool(1, d, ps, n, pages, lens, dtype, 47)
+    g = torch.Generator().manual_seed(5)
+    c.k[:] = 0
+    for b in range(2):
+        for j, p in enumerate(pages[b]):
+            i = 39 - j if falling else j
+            c.ks[p, 0] = 2.0 ** (15 - i) if i < 20 else 2.0 ** (i - 24)
+            c.k[p, 0, :, 0] = R.encode(torch.full((ps,), -8.0 if i < 20 else 8.0, dtype=torch.float64))
+            c.k[p, 0, :, 1] = R.encode(torch.randint(-15, 16, (ps,), generator=g).double())
+    q = torch.zeros(2 * T, H, d, dtype=dtype)
+    q[..., 0], q[..., 1] = 4.0, 2.0 ** -17
+    lam = 0.5 if T == 1 else 0.0
+    out, lse, mass = run(B, c, H, q, [T, T], lam=lam)
+    ref, ref_lse, ref_mass, size, top = R.attend(c, H, q, cut([T, T]), 1.0, 0.0, lam)
+    p_err = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -21
+    within(out.double(), ref, EPS[dtype] * ref.abs() + (p_err + 2.0 ** -19) * size + 640 * 2.0 ** -31 * top, "out")
+    within(lse.double(), ref_lse, 6 * 2.0 ** -24 * ref_lse.abs(), "lse")
+    within(mass.double(), ref_mass, 2.0 ** -17 * ref_mass.abs(), "mass")

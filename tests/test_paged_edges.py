@@ -2,6 +2,10 @@
 test_paged_abi.py, in the same manner."""
 import ctypes
 
+import pytest
+
+import paged_precision as L
+
 from test_paged_abi import B, P, Q, cache, i64, rotary  # noqa: F401  (B is the fixture)
 
 
@@ -30,3 +34,14 @@ def test_most_rows_of_a_rotation(B):  # noqa: F811
     def call(tokens, d):
         return B._lib.structkv_rotate(ctypes.byref(rotary(B, rot_dim=min(d, 64))), P, d, d, tokens, 1, d, 1, P, 0, Q, d, d, None)
     assert call(1 << 35, 2) == 2 and call(1 << 35, 256) == 2
+
+
+@pytest.mark.parametrize("d", [16, 64, 128, 256])
+def test_precision_tells_fewer_bits_apart(d):
+    """What test_gpu_paged_edges.py allows fp32 results is less than queries of two bf16 parts, or weights of one fp16 part, are off by."""
+    c, H, q, cu_new, scale = L.case(d)
+    ref, ref_lse, out_off, lse_off = L.attend(c, H, q, cu_new, scale)
+    out, lse, _, _ = L.attend(c, H, q, cu_new, scale, query_bits=16)
+    assert L.worst(out, ref, out_off) > 2 * L.MOST and L.worst(lse, ref_lse, lse_off) > 2 * L.MOST
+    out, _, _, _ = L.attend(c, H, q, cu_new, scale, weight_bits=11)
+    assert L.worst(out, ref, out_off) > 2 * L.MOST
