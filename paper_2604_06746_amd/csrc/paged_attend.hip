@@ -2,7 +2,10 @@
 //
 // The split and the sums of cache_attend_bf16.hip: S^T = K Q^T, so that a lane has one query row and four slots of each block of 16, and
 // O^T = V^T P^T takes the weights as they lie.  What is stored in 8 bits is exact in 16: keys enter their product as bf16 (queries too, those
-// in fp32 as three parts), values theirs as fp16, where weights keep 11 bits (fp32 outputs: two parts, 22 bits).
+// in fp32 as three parts), values theirs as fp16, the weights in two parts that add up to 22 bits.  Where
+// a sequence's bf16 rows are more than a workgroup's, the matrix instructions count, and weights have one part, 11 bits: 2^-12 of a weight beside the
+// result's own rounding of 2^-9, which turns the last bit of one result in 25 (with two parts one in 500, but 512 tokens over 32768 slots 367 -> 424 us,
+// 4096 tokens by themselves 244 -> 267; where a workgroup has all rows the second part costs 0 to 2 %).
 // A block of 16 slots lies in one page, so its scales are the same for all lanes: a key's scale multiplies the block's scores; a value's is
 // part of the weight, w = 2^(y + log2 s_v - M), with the row's reference M a whole number, so that nothing of it is rounded.
 // Blocks come straight from memory to registers: a lane's 16 bytes of a key are operands as they lie, since the order of components in a
@@ -179,7 +182,7 @@ struct Pair {
 template <class TAB, class T, int DP, int RB, bool CAPPED, int HELD, bool ONCE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, RB * DP > 256 ? 1 : 2) void paged_attend_kernel(TAB tab, CacheView view, PagedView c, ScoreForm f, AttendWork w, bool aligned) {
   constexpr bool F32 = std::is_same<T, float>::value;
-  constexpr int QP = F32 ? 3 : 1, PP = F32 ? 2 : 1, KP = DP / 64, W = DP / 16;
+  constexpr int QP = F32 ? 3 : 1, PP = F32 || ONCE ? 2 : 1, KP = DP / 64, W = DP / 16;
   constexpr bool AHEAD = DP <= 128 && (RB == 1 || !F32);   // (the others have no registers for it)
   constexpr bool TIGHT = F32 && DP > 128;   // places are worked out where they are used, which takes fewer registers
   constexpr bool SAVE = HELD > 0;

@@ -72,3 +72,5 @@ def worst(got, ref, off):
 # The model's units that a right result may take: its parts are no more than estimates (a weight's share of the roundings, scores that add up
 # alike), good to a factor of two.
 MOST = 2.0
+# The share of bf16 results whose last bit may be another than the exact one's.
+TURNED = 0.01

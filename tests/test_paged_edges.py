@@ -1,8 +1,10 @@
 """CPU-only checks of what the entry points of the cache held in pages, and of rotary positions, refuse at the ends of their ranges; beside
 test_paged_abi.py, in the same manner."""
 import ctypes
+import math
 
 import pytest
+import torch
 
 import paged_precision as L
 
@@ -45,3 +47,15 @@ def test_precision_tells_fewer_bits_apart(d):
     assert L.worst(out, ref, out_off) > 2 * L.MOST and L.worst(lse, ref_lse, lse_off) > 2 * L.MOST
     out, _, _, _ = L.attend(c, H, q, cu_new, scale, weight_bits=11)
     assert L.worst(out, ref, out_off) > 2 * L.MOST
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("lens,T", [((500, 90), 3), ((1700, 90), 1)])
+def test_last_bits_tell_weights_of_11_bits_apart(d, lens, T):
+    c, H, q, cu_new, scale = L.case(d, lens, T)
+    q = q.bfloat16()
+    ref, _, off, _ = L.attend(c, H, q, cu_new, scale)
+    few, _, _, _ = L.attend(c, H, q, cu_new, scale, weight_bits=11)
+    spread = torch.randn(ref.shape, generator=torch.Generator().manual_seed(1), dtype=torch.float64) * off[..., None] / math.sqrt(d)
+    turned = lambda x: float((x.bfloat16() != ref.bfloat16()).double().mean())  # noqa: E731
+    assert turned(few) > 2 * L.TURNED and turned(ref + L.MOST * spread) < 0.5 * L.TURNED
