@@ -1,43 +1,14 @@
 // The chunks of an attend call joined, and the single tokens' weights gathered.
 //
-// Chunk i of a row left (M_i, Z_i, O_i); with M = max M_i: Z = sum 2^(M_i - M) Z_i, out = sum 2^(M_i - M) O_i / Z, lse = ln 2 (M + log2 Z).
-// A workgroup per row.  The workgroups behind the rows' add the weights of a stretch of slots of one plane, 2^(x - lse) from the scores that
+// A workgroup per row (cache_join.h).  The workgroups behind the rows' add the weights of a stretch of slots of one plane, 2^(x - lse) from the scores that
 // the first launch left, so that the cache is read once.  Few bytes, so what counts is the chain of loads: the sequence's shares, which the
 // first launch left; then the chunks' M and Z beside the sums or the scores themselves, all at once; nothing is loaded after the norms are known.
-#include "cache.h"
+#include "cache_join.h"
 
 namespace skv {
 namespace {
 
-// over the 64 lanes, by moves inside the rows of 16 and then between them (six vector instructions; by shuffles six trips through the LDS
-// crossbar, which made a plane of 32 heads' norms take 5 us)
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float moved(float x, float without) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(without), __float_as_int(x), CTRL, ROWS, 0xF, false));
-}
-__device__ __forceinline__ float last_lane(float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); }
-__device__ __forceinline__ float wave_top(float x) {
-  x = fmaxf(x, moved<0x111, 0xF>(x, -INFINITY));
-  x = fmaxf(x, moved<0x112, 0xF>(x, -INFINITY));
-  x = fmaxf(x, moved<0x114, 0xF>(x, -INFINITY));
-  x = fmaxf(x, moved<0x118, 0xF>(x, -INFINITY));
-  x = fmaxf(x, moved<0x142, 0xA>(x, -INFINITY));
-  x = fmaxf(x, moved<0x143, 0xC>(x, -INFINITY));
-  return last_lane(x);
-}
-__device__ __forceinline__ float wave_total(float x) {
-  x += moved<0x111, 0xF>(x, 0.f);
-  x += moved<0x112, 0xF>(x, 0.f);
-  x += moved<0x114, 0xF>(x, 0.f);
-  x += moved<0x118, 0xF>(x, 0.f);
-  x += moved<0x142, 0xA>(x, 0.f);
-  x += moved<0x143, 0xC>(x, 0.f);
-  return last_lane(x);
-}
-typedef float __attribute__((ext_vector_type(2))) floatx2;
-
 constexpr int kSplitHeads = 16;   // from so many heads of a plane on, the waves share them
-constexpr int kAhead = 8;   // loads of a thread that are on their way at once
 
 // What joining a row needs to know; n: its slots.
 struct Row {
@@ -60,13 +31,6 @@ __device__ __forceinline__ Row row_of(const TAB& tab, const CacheView& c, const 
   row.written = share.y == 1 && !w.x;
   return row;
 }
-template <class T>
-__device__ __forceinline__ void put_row(const AttendWork& w, int64_t at, int d, int col, floatx4 o, float top, float z) {
-  const float inv = z != 0.f ? 1.f / z : 0.f;   // (NaN stays NaN)
-  for (int e = 0; e < 4 && col + e < d; ++e) put_out<T>((T*)w.out + at * d + col + e, o[e] * inv);
-  if (col == 0) w.lse[at] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
-}
-
 // FEW: a lane group of DP / 4 a row, for sequences that have some kFewChunks chunks when all are full (more, in rounds, where the others are
 // short); else a workgroup a row, its lane groups on shares of the chunks
 constexpr int kFewChunks = 8;
@@ -83,69 +47,25 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
     if (at >= w.rows) return;
     const Row row = row_of(tab, c, w, at, rows_wg);
     if (row.written) return;
-    const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + row.part0;
+    const joined_t* ml = reinterpret_cast<const joined_t*>(w.ml) + row.part0;
     const float* po = w.o + row.part0 * DP + col;
-    const int64_t step = row.step;
-    const bool mine = col < c.d;
-    floatx4 first[kAhead];
-    floatx2 stat[kAhead];
-    auto load = [&](int i0, int stride) __attribute__((always_inline)) {
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int i = i0 + k * stride;
-        stat[k] = i < row.live ? ml[i * step] : floatx2{kNothingSeen, 0.f};
-        first[k] = mine && i < row.live ? *reinterpret_cast<const floatx4*>(po + i * step * DP) : floatx4{0.f, 0.f, 0.f, 0.f};
-      }
-    };
-    float top = kNothingSeen, z = 0.f;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const float s = __builtin_amdgcn_exp2f(stat[k][0] - top);
-        z = fmaf(s, stat[k][1], z);
-        o += first[k] * s;
-      }
-    };
     if (FEW) {
+      float top = kNothingSeen, z = 0.f;
+      floatx4 o = {0.f, 0.f, 0.f, 0.f};
+      Chunks some;
       for (int i0 = 0; i0 < row.live; i0 += kAhead) {
-        load(i0, 1);
+        some.load(ml, po, row.step, DP, row.live, col < c.d, i0, 1);
         const float old = top;
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) top = fmaxf(top, stat[k][0]);
+        for (int k = 0; k < kAhead; ++k) top = fmaxf(top, some.stat[k][0]);
         const float shrink = __builtin_amdgcn_exp2f(old - top);
         z *= shrink;
         o *= shrink;
-        add();
+        some.add(top, z, o);
       }
-      if (mine) put_row<T>(w, at, c.d, col, o, top, z);
-      return;
-    }
-    load(part, PARTS);
-    for (int i = lane; i < row.live; i += 64) top = fmaxf(top, ml[i * step][0]);
-    top = wave_top(top);
-    add();
-    for (int i = part + kAhead * PARTS; i < row.live; i += PARTS) {
-      const floatx2 m = ml[i * step];
-      const float s = __builtin_amdgcn_exp2f(m[0] - top);
-      z = fmaf(s, m[1], z);
-      if (mine) o += *reinterpret_cast<const floatx4*>(po + i * step * DP) * s;
-    }
-    // the shares: lanes of a wave that have the same components, then the waves
-    for (int m = LANES; m < 64; m <<= 1) {
-      z += __shfl_xor(z, m);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m);
-    }
-    if (lane < LANES) *reinterpret_cast<floatx4*>(sh + (wave * LANES + lane) * 4) = o;
-    if (lane == 0) zs[wave] = z;
-    __syncthreads();
-    if ((int)threadIdx.x < LANES && mine) {
-      z = (zs[0] + zs[1]) + (zs[2] + zs[3]);
-      o = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o += *reinterpret_cast<const floatx4*>(sh + (i * LANES + threadIdx.x) * 4);
-      put_row<T>(w, at, c.d, col, o, top, z);
+      if (col < c.d) put_row<T>(w, at, c.d, col, o, top, z);
+    } else {
+      join_row<T, DP>(w, c.d, at, ml, po, row.step, row.live, sh, zs);
     }
     return;
   }
@@ -173,18 +93,13 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(TAB tab, CacheView c
   for (int k = 0; k < kAhead; ++k)
     ahead[k] = s < s1 && first_head + k * step < heads ? (held_some)*reinterpret_cast<const some*>(x + (first_head + k * step) * w.xs + s) : (held_some)(-INFINITY);
   for (int i0 = wave; i0 < heads; i0 += 4 * kAhead) {   // norms: a lane a chunk, the wave's heads at once
-    floatx2 a[kAhead];
+    joined_t a[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int i = i0 + 4 * j;
       const int head = plane * heads + i, g = token_of(w, head), r = head - g * w.gs;
-      const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + ((int64_t)(first + (r >> __builtin_ctz(rows_wg))) * c.G + g) * rows_wg + (r & (rows_wg - 1));
-      a[j] = i < heads && lane < live ? ml[lane * chunk_step] : floatx2{kNothingSeen, 0.f};
-      for (int k = lane + 64; i < heads && k < live; k += 64) {
-        const floatx2 m = ml[k * chunk_step];
-        const float top = fmaxf(a[j][0], m[0]);
-        a[j] = floatx2{top, a[j][1] * __builtin_amdgcn_exp2f(a[j][0] - top) + m[1] * __builtin_amdgcn_exp2f(m[0] - top)};
-      }
+      a[j] = joined_stat(reinterpret_cast<const joined_t*>(w.ml) + ((int64_t)(first + (r >> __builtin_ctz(rows_wg))) * c.G + g) * rows_wg + (r & (rows_wg - 1)), chunk_step, live,
+                         i < heads);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {

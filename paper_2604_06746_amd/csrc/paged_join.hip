@@ -4,6 +4,7 @@
 // The first launch also left each row's weight of each block of 16 slots, in the log2 domain: a page's mass takes 2^(x - lse2) of its
 // blocks and all heads, or, of weights in units of 2^u, 2^((u - M) + (x - log2 Z)), large numbers and small ones apart.  Few bytes, so what counts is the chain of loads; the workgroups that gather form the rows' norms themselves, beside
 // those that join the rows, and have the blocks' weights on their way meanwhile.  2081 slots 6.0 us (by two launches 4.3 + 11.2), eight of 64K to 128K 11.
+#include "cache_join.h"
 #include "paged.h"
 
 #include <algorithm>
@@ -11,41 +12,12 @@
 namespace skv {
 namespace {
 
-typedef float __attribute__((ext_vector_type(2))) floatx2;
-
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float moved(float x, float without) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(without), __float_as_int(x), CTRL, ROWS, 0xF, false));
-}
-__device__ __forceinline__ float last_lane(float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); }
-// over the 64 lanes, by moves inside the rows of 16 and then between them
-__device__ __forceinline__ float wave_top(float x) {
-  x = fmaxf(x, moved<0x111, 0xF>(x, -INFINITY));
-  x = fmaxf(x, moved<0x112, 0xF>(x, -INFINITY));
-  x = fmaxf(x, moved<0x114, 0xF>(x, -INFINITY));
-  x = fmaxf(x, moved<0x118, 0xF>(x, -INFINITY));
-  x = fmaxf(x, moved<0x142, 0xA>(x, -INFINITY));
-  x = fmaxf(x, moved<0x143, 0xC>(x, -INFINITY));
-  return last_lane(x);
-}
-__device__ __forceinline__ float wave_total(float x) {
-  x += moved<0x111, 0xF>(x, 0.f);
-  x += moved<0x112, 0xF>(x, 0.f);
-  x += moved<0x114, 0xF>(x, 0.f);
-  x += moved<0x118, 0xF>(x, 0.f);
-  x += moved<0x142, 0xA>(x, 0.f);
-  x += moved<0x143, 0xC>(x, 0.f);
-  return last_lane(x);
-}
-
-constexpr int kAhead = 8;       // loads of a thread that are on their way at once
 constexpr int64_t kLaunchBlocks = (int64_t)1 << 23;
 constexpr int kStretch = 64;    // blocks whose weights a workgroup gathers: whole pages of any size
 
 template <class TAB, class T, int DP>
 __global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, AttendWork w, int row_blocks, int first_block) {
   short_kernel_priority();
-  constexpr int LANES = DP / 4, PARTS = 256 / LANES;
   __shared__ __attribute__((aligned(16))) float sh[256 * 4];
   __shared__ float zs[4];
   extern __shared__ float norms[];   // of the heads: M + log2 Z, and behind them each apart
@@ -57,52 +29,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, A
     const int4 share = w.shares[b];
     const int g = token_of(w, head), mine = head - g * w.gs;   // (a single token's rows are its heads)
     const int64_t part0 = ((int64_t)(share.x + mine / 16) * c.G + g) * 16 + mine % 16, step = (int64_t)(tab.units[b + 1] - tab.units[b]) * c.G * 16;
-    const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + part0;
-    const int part = threadIdx.x / LANES, col = threadIdx.x % LANES * 4, live = share.z;
-    const bool in = col < c.d;
-    const float* po = w.o + part0 * DP + col;
-    floatx4 first[kAhead];
-    floatx2 stat[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int i = part + k * PARTS;
-      stat[k] = i < live ? ml[i * step] : floatx2{kNothingSeen, 0.f};
-      first[k] = in && i < live ? *reinterpret_cast<const floatx4*>(po + i * step * DP) : floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    float top = kNothingSeen, z = 0.f;
-    for (int i = lane; i < live; i += 64) top = fmaxf(top, ml[i * step][0]);
-    top = wave_top(top);
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const float s = __builtin_amdgcn_exp2f(stat[k][0] - top);
-      z = fmaf(s, stat[k][1], z);
-      o += first[k] * s;
-    }
-    for (int i = part + kAhead * PARTS; i < live; i += PARTS) {
-      const floatx2 m = ml[i * step];
-      const float s = __builtin_amdgcn_exp2f(m[0] - top);
-      z = fmaf(s, m[1], z);
-      if (in) o += *reinterpret_cast<const floatx4*>(po + i * step * DP) * s;
-    }
-    for (int m = LANES; m < 64; m <<= 1) {
-      z += __shfl_xor(z, m);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m);
-    }
-    if (lane < LANES) *reinterpret_cast<floatx4*>(sh + (wave * LANES + lane) * 4) = o;
-    if (lane == 0) zs[wave] = z;
-    __syncthreads();
-    if ((int)threadIdx.x < LANES && in) {
-      z = (zs[0] + zs[1]) + (zs[2] + zs[3]);
-      o = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o += *reinterpret_cast<const floatx4*>(sh + (i * LANES + threadIdx.x) * 4);
-      const float inv = z != 0.f ? 1.f / z : 0.f;   // (NaN stays NaN)
-      const int64_t at = (int64_t)r * w.H + head;
-      for (int e = 0; e < 4; ++e) put_out<T>((T*)w.out + at * c.d + col + e, o[e] * inv);
-      if (col == 0) w.lse[at] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.6931471806f : -INFINITY;
-    }
+    join_row<T, DP>(w, c.d, (int64_t)r * w.H + head, reinterpret_cast<const joined_t*>(w.ml) + part0, w.o + part0 * DP + threadIdx.x % (DP / 4) * 4, step, share.z, sh, zs);
     return;
   }
   // Blocks i0 .. i0 + 63 of sequence b, one in each lane; a wave takes every fourth head.
@@ -122,17 +49,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(TAB tab, PagedView c, A
   const float old = mine ? c.mass[b * c.pst + page] : 0.f;
   const int64_t chunk_step = (int64_t)(tab.units[b + 1] - tab.units[b]) * c.G * 16;
   for (int h0 = wave; h0 < w.H; h0 += 4 * kAhead) {   // norms: a lane a chunk
-    floatx2 a[kAhead];
+    joined_t a[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int h = h0 + 4 * j, g = token_of(w, h), r = h - g * w.gs;
-      const floatx2* ml = reinterpret_cast<const floatx2*>(w.ml) + ((int64_t)(share.x + r / 16) * c.G + g) * 16 + r % 16;
-      a[j] = h < w.H && lane < live ? ml[lane * chunk_step] : floatx2{kNothingSeen, 0.f};
-      for (int k = lane + 64; h < w.H && k < live; k += 64) {
-        const floatx2 m = ml[k * chunk_step];
-        const float top = fmaxf(a[j][0], m[0]);
-        a[j] = floatx2{top, a[j][1] * __builtin_amdgcn_exp2f(a[j][0] - top) + m[1] * __builtin_amdgcn_exp2f(m[0] - top)};
-      }
+      a[j] = joined_stat(reinterpret_cast<const joined_t*>(w.ml) + ((int64_t)(share.x + r / 16) * c.G + g) * 16 + r % 16, chunk_step, live, h < w.H);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
