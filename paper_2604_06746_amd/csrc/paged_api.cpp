@@ -108,7 +108,7 @@ constexpr int64_t kUnits = 512, kLeast = 128;
 // ... of 256 where a workgroup has 32 rows, whose partial results cost more to join: chains of 64 over 1000 slots 17.3 -> 14.2 us, of 13 over 4000
 // 16.2 -> 13.7, of 13 over 1000 12.4 -> 13.4 (512: 14.4, 14.3 and 14.9).
 constexpr int64_t kLeastRows = 256;
-// Mean slots of a block of rows from which on it is cut in two even where the blocks fill the chip.
+// Capacity from which on a block of rows is cut in two even where the blocks fill the chip.
 constexpr int64_t kCut = 4096;
 // ... while the rows, each of them a workgroup of 256 threads of the second launch, are no more than a launch takes.
 constexpr int64_t kMostJoined = (int64_t)1 << 23;
@@ -130,7 +130,11 @@ structkv_status plan_paged(const PagedView& v, int H, bool gather, bool bf16, Ca
   p->rows = gather || most_rows <= 16 || (!bf16 && v.d > 128) ? 16 : 32;   // (32 rows of 256 components in fp32: no registers for it)
   const int64_t least = p->rows == 16 ? kLeast : kLeastRows;
   p->min_chunk = (int)least;
-  p->stream = most_rows <= p->rows;   // nobody else reads the codes: past the caches (eight of 64K to 128K 304 -> 289 us, 64 of 2K 67 -> 61, four of 16K by 32 rows 31.4 -> 31.8)
+  // No other workgroup of the sequence reads the codes: past the caches (sixteen sequences of 32K slots 197 -> 181 us, 32 of 8K 107 -> 96; 64 of
+  // 2K in turns with other calls 67 -> 61, the same ones again and again 43 -> 47).
+  // Where sequences share a long prefix's pages, which only the table on the device knows, that costs what the caches would have kept (sixteen that
+  // share 32K 105 -> 124, four that share 64K 60 -> 90, 32 that share 8K 61 -> 62), and they are still read faster than pages of their own.
+  p->stream = most_rows <= p->rows;
   int64_t blocks = 0, chunks = 0;
   for (int b = 0; b < v.batch; ++b) {
     const int64_t rcs = ceil_div((int64_t)(t->cu_new[b + 1] - t->cu_new[b]) * gs, p->rows);

@@ -1,8 +1,8 @@
 // The chunks of an attend call over pages joined, and the single tokens' weights gathered by page, in one launch.
 //
-// Chunk i of a row left (M_i, Z_i, O_i); with M = max M_i: Z = sum 2^(M_i - M) Z_i, out = sum 2^(M_i - M) O_i / Z, lse = ln 2 (M + log2 Z).
-// The first launch also left each row's weight of each block of 16 slots, in the log2 domain: a page's mass takes 2^(x - lse2) of its
-// blocks and all heads, or, of weights in units of 2^u, 2^((u - M) + (x - log2 Z)), large numbers and small ones apart.  Few bytes, so what counts is the chain of loads; the workgroups that gather form the rows' norms themselves, beside
+// Rows as in cache_join.h.  The first launch also left each row's weight of each block of 16 slots, in the log2 domain: a page's mass takes 2^(x - lse2) of its
+// blocks and all heads, or, of weights in units of 2^u, 2^((u - M) + (x - log2 Z)), large numbers and small
+// ones apart.  Few bytes, so what counts is the chain of loads; the workgroups that gather form the rows' norms themselves, beside
 // those that join the rows, and have the blocks' weights on their way meanwhile.  2081 slots 6.0 us (by two launches 4.3 + 11.2), eight of 64K to 128K 11.
 #include "cache_join.h"
 #include "paged.h"

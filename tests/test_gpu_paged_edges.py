@@ -15,11 +15,17 @@ pytestmark = pytest.mark.gpu
 
 
 def run(B, c, H, q, fresh, *, scale=1.0, softcap=0.0, lam=0.0, on=None):  # noqa: F811
-    """(out, lse, mass) in host memory."""
-    on, new = on or OnGpu(B, c), sum(fresh)
-    out = torch.full((new, H, c.d), math.nan, dtype=c.dtype, device="cuda")
-    lse = torch.full((new, H), math.nan, device="cuda")
-    B.structkv_paged_attend(on.handle, H, q.cuda(), cut(fresh), out, lse, on.workspace(B, H, new), scale=scale, softcap=softcap, lam=lam)
+    """(out, lse, mass) in host memory; the call twice, from the same mass, with the workspace as it was left: the same bits."""
+    on, new, res = on or OnGpu(B, c), sum(fresh), []
+    ws, mass = on.workspace(B, H, new), on.mass.clone()
+    for _ in range(2):
+        out = torch.full((new, H, c.d), math.nan, dtype=c.dtype, device="cuda")
+        lse = torch.full((new, H), math.nan, device="cuda")
+        on.mass.copy_(mass)
+        B.structkv_paged_attend(on.handle, H, q.cuda(), cut(fresh), out, lse, ws, scale=scale, softcap=softcap, lam=lam)
+        res.append((out, lse, on.mass.clone()))
+    for x, y in zip(*res):
+        assert torch.equal(x.nan_to_num(7e30), y.nan_to_num(7e30))
     return out.cpu(), lse.cpu(), on.mass.cpu()
 
 
@@ -418,3 +424,31 @@ def test_bf16_results_are_the_nearest(B, d, lens, T):  # noqa: F811
     out, _, _ = run(B, c, H, q, [T, T], scale=scale)
     ref, _, _, _ = L.attend(c, H, q, cu_new, scale)
     assert float((out != ref.bfloat16()).double().mean()) <= L.TURNED
+
+
+@pytest.mark.parametrize("score", [1.0, 5.0 * 2.0 ** 9, 5.0 * 2.0 ** 26])
+@pytest.mark.parametrize("G,H,lens", [(5, 5, [45]), (1, 1, [3]), (32, 4096, [40, 17]), (3, 51, [77])])
+def test_gathering_at_odd_places(B, G, H, lens, score):  # noqa: F811
+    """As many heads as there may be, and pairs of unit and weight that begin at an odd word; what lies behind the workspace stays."""
+    pages, n = table(lens, 16, np.random.default_rng(G))
+    c = R.make_pool(G, 16, 16, n, pages, lens, torch.bfloat16, 5)
+    used = c.k[..., 0] != 127
+    c.ks[:] = 1.0
+    c.k[:] = 0
+    c.k[..., 0] = R.encode((torch.rand(n, G, 16, generator=torch.Generator().manual_seed(2)) < 0.1).double() + 1.0)
+    c.k[~used] = 127
+    new = len(lens)
+    q = torch.zeros(new, H, 16, dtype=torch.bfloat16)
+    q[..., 0] = score
+    on = OnGpu(B, c)
+    size = B.structkv_paged_workspace_bytes(on.handle, H, new)
+    ws = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty(new, H, 16, dtype=torch.bfloat16, device="cuda"), torch.empty(new, H, device="cuda")
+    B.structkv_paged_attend(on.handle, H, q.cuda(), list(range(new + 1)), out, lse, ws[:size], scale=1.0, lam=0.5)
+    ref, ref_lse, ref_mass, norm, top = R.attend(c, H, q, list(range(new + 1)), 1.0, 0.0, 0.5)
+    assert bool((ws[size:] == 0xA5).all())
+    # (where a KV head's rows are more than the 16 of a workgroup, weights have 11 bits: 2^-12 of each; else 22)
+    p_err = 2.0 ** -19 + (2.0 ** -12 if H // G > 16 else 0.0)
+    within(out.cpu().double(), ref, 2.0 ** -8 * ref.abs() + p_err * norm + 77 * 2.0 ** -31 * top, "out")
+    within(lse.cpu().double(), ref_lse, 6 * 2.0 ** -24 * ref_lse.abs() + 2.0 ** -20, "lse")
+    within(on.mass.cpu().double(), ref_mass, 2.0 ** -17 * ref_mass.abs(), "mass")
