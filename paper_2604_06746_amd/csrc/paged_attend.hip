@@ -13,10 +13,12 @@
 // The waves take shares of a chunk's blocks; a lane looks up one block's page, place and scales, and only blocks of pages that are there are
 // in the list that a wave goes by, so dropped pages cost nothing.
 //
-// Single tokens are bound by reading the codes: eight caches of 64K to 128K slots (1.6 GB) 264 us, 6.1 TB/s, past the caches (ONCE; through them
+// Single tokens are bound by reading the codes: eight caches of 64K to 128K slots (1.6 GB) 266 us, 6.1 TB/s, past the caches (ONCE; through them
 // 281); with two pairs of blocks in turns, where one at a time took 300.  256 workgroups more or 512 are no faster (268, 270).  Chunks of a prompt are bound by
-// the issue port, which two waves a SIMD keep busy for 64 % of the time: 512 tokens over 32768 slots 365 us, 750 TFLOP/s; of the 252 vector instructions that a
+// the issue port, which two waves a SIMD keep busy for 64 % of the time: 512 tokens over 32768 slots 366 us, 750 TFLOP/s; of the 252 vector instructions that a
 // tile of 32 rows and 32 slots takes, 80 decode and 32 are matrix instructions.  64 rows a wave (one wave a SIMD) 421 us.
+// Usual scores and scales take that loop; what fp32's range or bits do not bear in it is found there and done over with care, in a loop behind it
+// (inside the first one that code cost chains of eight over four caches of 16K slots 31 -> 42 us).
 #include "paged.h"
 
 namespace skv {

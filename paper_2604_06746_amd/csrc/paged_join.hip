@@ -3,7 +3,7 @@
 // Rows as in cache_join.h.  The first launch also left each row's weight of each block of 16 slots, in the log2 domain: a page's mass takes 2^(x - lse2) of its
 // blocks and all heads, or, of weights in units of 2^u, 2^((u - M) + (x - log2 Z)), large numbers and small
 // ones apart.  Few bytes, so what counts is the chain of loads; the workgroups that gather form the rows' norms themselves, beside
-// those that join the rows, and have the blocks' weights on their way meanwhile.  2081 slots 6.0 us (by two launches 4.3 + 11.2), eight of 64K to 128K 11.
+// those that join the rows, and have the blocks' weights on their way meanwhile.  2081 slots 6.2 us (by two launches 4.3 + 11.2), eight of 64K to 128K 12.
 #include "cache_join.h"
 #include "paged.h"
 

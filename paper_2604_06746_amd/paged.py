@@ -106,7 +106,7 @@ class PagedCache:
 
     def attend(self, q: torch.Tensor, cu_new: Sequence[int], lam: float = 0.0, scale: float = 0.0, softcap: float = 0.0):
         """Attention of the tokens appended last: (out [new, H_q, d], lse [new, H_q]).  lam > 0, single tokens: their weights are gathered by
-        page."""
+        page.  (Chains and a prompt's chunks leave `mass` as it is: pages are chosen by it after some tokens.)"""
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
         B.structkv_paged_attend(self.handle, self.Hq, q, cu_new, out, lse, self.workspace, scale, softcap, lam)
